@@ -356,6 +356,104 @@ int compact_attn_search_head(const ca_layout* layout, const float* mass, const i
                              int32_t num_groups, double tau, double lambda, int32_t pattern, ca_group* groups,
                              double* recall, double* kept_fraction);
 
+/* ---- Rotary positions, and norms of queries and keys -------------------------------------------------------
+ *
+ * What makes q and k of the attention calls: every token has a position on up to three axes (frame, row, column), every pair of
+ * channels belongs to one axis and is turned by position times the pair's frequency:
+ *   (a, b) -> magnitude * (a cos f - b sin f, a sin f + b cos f),  f = position * frequency.
+ * The first channels of the head are rotated, those of the frame axis first, the rest passes through.  */
+
+/* Which channels are a pair: CA_PAIRS_INTERLEAVED channels 2i and 2i + 1, CA_PAIRS_HALF channels i and i + R/2 of the R rotated ones
+ * (pair i belongs to the axis that holds channel 2i of the interleaved order). */
+typedef enum { CA_PAIRS_INTERLEAVED = 0, CA_PAIRS_HALF = 1 } ca_pairing;
+
+/* Frequencies of an axis of c channels, pair i of c/2: F_i = base^(-2i/c), and for contexts s = stretch times as long as trained:
+ *   CA_STRETCH_LINEAR  F_i / s
+ *   CA_STRETCH_BASE    base * s^(c/(c-2)) in the place of base (c = 2: base as it is)
+ *   CA_STRETCH_BANDS   g F_i + (1 - g) F_i / s, g = clamp((r - turns_low) / (turns_high - turns_low), 0, 1), where r = trained * F_i / (2 pi)
+ *                      is how often the pair turns over the positions trained on: fast pairs keep their frequency */
+typedef enum { CA_STRETCH_LINEAR = 0, CA_STRETCH_BASE = 1, CA_STRETCH_BANDS = 2 } ca_stretch;
+
+typedef struct {
+  int32_t channels;             /* even; 0 = the axis rotates nothing                              */
+  int32_t positions;            /* angles are tabulated for positions 0 .. positions - 1           */
+  double base, stretch;         /* > 0                                                             */
+  double trained;               /* > 0, CA_STRETCH_BANDS only                                      */
+  double turns_low, turns_high; /* low < high, CA_STRETCH_BANDS only                               */
+} ca_rotary_axis;
+
+typedef struct ca_rotary ca_rotary; /* opaque; immutable once built; may be shared by threads, layouts and streams */
+
+/* Tabulates the angles: sine and cosine are computed in 64 bits and stored as float32, so far positions are as exact as near ones.
+ *   axes  host pointer to three axes: frame, row, column.   *out  receives a table owned by the caller.
+ * Host-only work.  Errors: CA_ERR_INVALID_ARG (null, odd or no channels, figures out of range, more than 2^28 angles), CA_ERR_ALLOC. */
+int compact_attn_build_rotary(const ca_rotary_axis* axes, int32_t pairing, int32_t method, double magnitude, ca_rotary** out);
+
+/* Host view of one axis (0, 1, 2): *cos_sin -> float[positions][channels / 2][2]; NULL for an axis without channels.  Owned by the table. */
+int compact_attn_rotary_angles(const ca_rotary* rotary, int32_t axis, const float** cos_sin);
+
+/* Copies the table to the current HIP device.  Synchronous; idempotent.  The calls below do it on first use if it was not called (refused with
+ * CA_ERR_INVALID_ARG while their stream is being captured).  Errors: CA_ERR_ALLOC, CA_ERR_HIP. */
+int compact_attn_rotary_upload(ca_rotary* rotary);
+
+/* Releases a table (NULL is ignored).  The caller must make sure no enqueued work still reads it. */
+void compact_attn_free_rotary(ca_rotary* rotary);
+
+/* Where the elements of a natural-order tensor [batch, heads, N_real, D] lie: strides in elements, channels contiguous, every row 16-byte
+ * aligned.  A projection that leaves [batch, tokens, heads, D] behind is read, and its gradient written, in place.  A null pointer to
+ * one stands for the contiguous tensor.  Strides are not negative; rows of a tensor that is written must not share memory. */
+typedef struct {
+  int64_t batch, head, token;
+} ca_strides;
+
+/* Positions of the tokens.  positions NULL: the token at (t, y, x) of the grid has position origin + (t, y, x), of which every axis that has
+ * channels must lie in its table (CA_ERR_INVALID_ARG otherwise), and text tokens are not rotated.  Else int32[batch][N_real][3], device
+ * memory, 4-byte aligned, for all tokens, and origin is not read; a negative position leaves the channels of that axis as they are, and one past
+ * the table makes them NaN (it is looked at on the device; nothing is read out of range). */
+typedef struct {
+  int32_t origin[3];
+  const int32_t* positions;
+} ca_where;
+
+/* Rotary positions.
+ *   transpose = 0: src in natural order -> dst rotated, in tile order (tiled = 1; padding slots are written as zero) or natural order (tiled = 0).
+ *   transpose = 1: src in tile (tiled = 1) or natural order -> dst in natural order, every pair turned back (times the magnitude): the gradient
+ *                  of the former, and its inverse where the magnitude is 1.
+ * src_strides, dst_strides: of a natural-order tensor; must be NULL for one in tile order.  where may be NULL (origin 0, no positions).
+ * Sums are fp32, results rounded once.  dst must not overlap src.  bf16 and f32 layouts, any tile; head_dim up to 512 (bf16) or 256 (f32),
+ * CA_ERR_UNSUPPORTED beyond.  The layout's tile lists are not read. */
+int compact_attn_rotate(const void* src, const ca_strides* src_strides, void* dst, const ca_strides* dst_strides, const ca_layout* layout, ca_rotary* rotary,
+                        const ca_where* where, int32_t tiled, int32_t transpose, void* stream);
+
+/* What the norm calls work on.  Queries and keys go through one launch. */
+typedef struct {
+  const void *q, *k;                       /* natural order                                                     */
+  const ca_strides *q_strides, *k_strides; /* NULL: contiguous                                                  */
+  const void *q_weight, *k_weight;         /* [D] of the layout's type, 16-byte aligned, shared by all heads; NULL: ones */
+  ca_rotary* rotary;                       /* NULL: no rotation                                                 */
+  const ca_where* where;                   /* NULL: origin 0, no positions                                      */
+  float eps;                               /* >= 0                                                              */
+  int32_t tiled;                           /* the results are in tile order (1) or natural order (0)            */
+} ca_norm;
+
+/* Norm of every query and key head over its channels, and the rotation, in one pass:
+ *   y = R(p) (w * x * (mean(x^2) + eps)^-1/2)
+ * q_out, k_out: contiguous, in tile order (padding slots are written as zero) or natural order.  Sums are fp32, results rounded once.  Must not overlap the
+ * inputs or each other.  Supported and refused as compact_attn_rotate. */
+int compact_attn_norm_rotate(const ca_norm* norm, void* q_out, void* k_out, const ca_layout* layout, void* stream);
+
+/* Its gradients, from the gradients dq_out, dk_out of its results (contiguous, in tile or natural order) and the same inputs:
+ *   u = R^T dy, n = x r, r = (mean(x^2) + eps)^-1/2:  dx = r (w u - n mean(w u n)),  dw = sum over batch, heads and tokens of u n.
+ *   dq, dk   natural order, strides as given; rows must not share memory.
+ *   dq_weight, dk_weight  float32 [D], written in full (also where the weight is NULL); both may be NULL together.
+ * The sums over tokens are fp32 in a fixed order, so results are run-to-run identical.
+ *   compact_attn_norm_workspace: *workspace_bytes of device memory that the call needs where weight gradients are asked for.
+ *   workspace: 16-byte aligned, not overlapping the tensors; must not be used by anything else until the call's work on `stream` has run. */
+int compact_attn_norm_workspace(const ca_layout* layout, int64_t* workspace_bytes);
+int compact_attn_norm_rotate_backward(const ca_norm* norm, const void* dq_out, const void* dk_out, void* dq, const ca_strides* dq_strides, void* dk,
+                                      const ca_strides* dk_strides, float* dq_weight, float* dk_weight, const ca_layout* layout, void* workspace,
+                                      int64_t workspace_bytes, void* stream);
+
 /* Message of the last failure on the calling thread ("" if none); valid until the next call. */
 const char* compact_attn_last_error(void);
 

@@ -31,3 +31,13 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .rotary import (  # noqa: F401
+    Rotary,
+    compact_attn_build_rotary,
+    compact_attn_free_rotary,
+    compact_attn_norm_rotate,
+    compact_attn_norm_rotate_backward,
+    compact_attn_rotary_angles,
+    compact_attn_rotary_upload,
+    compact_attn_rotate,
+)

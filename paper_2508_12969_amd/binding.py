@@ -49,6 +49,14 @@ EXPORTED = (
     "compact_attn_tile_mass",
     "compact_attn_layout_mass_shares",
     "compact_attn_search_head",
+    "compact_attn_build_rotary",
+    "compact_attn_rotary_angles",
+    "compact_attn_rotary_upload",
+    "compact_attn_free_rotary",
+    "compact_attn_rotate",
+    "compact_attn_norm_rotate",
+    "compact_attn_norm_workspace",
+    "compact_attn_norm_rotate_backward",
     "compact_attn_last_error",
 )
 
@@ -83,6 +91,7 @@ class CompactAttnError(RuntimeError):
 
 
 _lib = None
+_declarations = []   # of the other modules of this package: argument types of their entry points
 
 
 def library_path():
@@ -134,6 +143,8 @@ def load_library():
     for name in EXPORTED:
         if name not in ("compact_attn_free_layout", "compact_attn_last_error"):
             getattr(lib, name).restype = ctypes.c_int
+    for declare in _declarations:
+        declare(lib)
     _lib = lib
     return lib
 

@@ -9,9 +9,16 @@
 #include <new>
 #include <vector>
 
+#include "api_common.h"
 #include "kernels.h"
 #include "layout.h"
 
+using ca::aligned16;
+using ca::elem_size;
+using ca::ensure_uploaded;
+using ca::fail;
+using ca::hip_fail;
+using ca::ranges_overlap;
 using ca::set_error;
 
 namespace {
@@ -37,21 +44,7 @@ ScratchState g_scratch[kMaxDevices];
 std::mutex g_scratch_mutex;
 std::atomic<uint64_t> g_next_serial{1};
 
-int fail(int status, const char* what) {
-  set_error("%s", what);
-  return status;
-}
-
-int hip_fail(hipError_t e, const char* where) {
-  set_error("%s: %s", where, hipGetErrorString(e));
-  return CA_ERR_HIP;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-int elem_size(int32_t dtype) { return dtype == CA_BF16 ? 2 : 4; }
 
 // A table of a layout and where its device address goes.
 struct Table {
@@ -106,10 +99,12 @@ void free_device_tables(ca::DeviceTables& d) {
   d = ca::DeviceTables{};
 }
 
+}  // namespace
+
 // Makes sure the layout's tables are on the current device.  The first call for a layout allocates
 // device memory and copies synchronously, which a stream under capture must not see: there the call
 // fails and names compact_attn_layout_upload instead.
-int ensure_uploaded(ca_layout* L, hipStream_t stream) {
+int ca::ensure_uploaded(ca_layout* L, hipStream_t stream) {
   std::lock_guard<std::mutex> lock(L->upload_mutex);
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
@@ -178,6 +173,8 @@ int ensure_uploaded(ca_layout* L, hipStream_t stream) {
   return CA_OK;
 }
 
+namespace {
+
 // The tile-mass kernel is launched with as many workgroups as the device holds at a time, each of which
 // takes groups of 128 queries by ticket and keeps two floats per (query, key tile) of the group it is
 // working on.  The workspace for that and the ticket counter are allocated at the first call
@@ -233,12 +230,6 @@ int ensure_mass_workspace(ca_layout* L, hipStream_t stream) {
   L->dev.mass_share_stats = L->dev.mass_partial + rows * L->n * ca::kMassQueries * 2;
   L->dev.mass_counter = reinterpret_cast<int32_t*>(static_cast<char*>(p) + bytes);
   return CA_OK;
-}
-
-// Do the byte ranges [a, a + na) and [b, b + nb) share a byte?
-bool ranges_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + (uintptr_t)nb && b0 < a0 + (uintptr_t)na;
 }
 
 int check_attn_support(const ca_layout* L) {

@@ -1,0 +1,441 @@
+// Rotary positions, and norms of queries and keys with the rotation in the same pass, forwards and backwards.
+//
+//   y = R (w n),  n = x r,  r = (mean(x^2) + eps)^-1/2;   R turns pairs of channels by position * frequency.
+//   Backwards: u = R^T dy,  dx = r (w u - n mean(w u n)),  dw = sum of u n;  R^T is R with the sines negated.
+//
+// Bound: HBM, every row (token, head) is read once and written once.  A row is held by D / 8 lanes (bf16; D / 4 for fp32), 16 bytes each, so
+// its sums are a few lane exchanges and its rounding is one.  A wave takes 64 / lanes tokens and walks over the heads and
+// over q and k with them: the angles (gathered from the small per-axis tables, which stay in L2) and their products with the weights are made
+// once per token and tensor, and several heads are loaded before the first is computed, so that enough bytes are in flight.  Tile order costs nothing
+// here: a token's place in it is a few integer operations per token, and no pass of its own.
+#include <algorithm>
+
+#include "rotary.h"
+
+namespace ca {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float floatx4;
+
+template <class T>
+struct Row;
+template <>
+struct Row<__bf16> {
+  static constexpr int kVec = 8;
+  typedef bf16x8 Chunk;
+};
+template <>
+struct Row<float> {
+  static constexpr int kVec = 4;
+  typedef floatx4 Chunk;
+};
+
+// Token of a row in natural order, -1 for a padding slot, and its coordinates (-1 for text).
+struct Token {
+  int64_t natural, place;  // place: in tile order
+  int at[3];
+};
+
+__device__ __forceinline__ Token token_of_natural(const RowArgs& a, uint32_t natural) {
+  Token k;
+  k.natural = natural;
+  k.at[0] = k.at[1] = k.at[2] = -1;
+  if (natural >= (uint64_t)a.N_video) {
+    k.place = a.n_vid * a.B + (natural - a.N_video);
+    return k;
+  }
+  const uint32_t row = natural / (uint32_t)a.W, x = natural - row * a.W, t = row / (uint32_t)a.H, y = row - t * a.H;
+  const uint32_t kt = t / (uint32_t)a.tt, kh = y / (uint32_t)a.th, kw = x / (uint32_t)a.tw;
+  k.at[0] = (int)t, k.at[1] = (int)y, k.at[2] = (int)x;
+  const uint32_t slot = ((t - kt * a.tt) * a.th + (y - kh * a.th)) * a.tw + (x - kw * a.tw);
+  k.place = (int64_t)((kt * a.nH + kh) * a.nW + kw) * a.B + slot;
+  return k;
+}
+
+__device__ __forceinline__ Token token_of_place(const RowArgs& a, uint32_t place) {
+  Token k;
+  k.place = place;
+  k.at[0] = k.at[1] = k.at[2] = -1;
+  const uint32_t tile = place / (uint32_t)a.B, slot = place - tile * a.B;
+  if (tile >= (uint64_t)a.n_vid) {
+    k.natural = a.N_video + (place - a.n_vid * a.B);
+    return k;
+  }
+  const uint32_t tr = tile / (uint32_t)a.nW, kw = tile - tr * a.nW, kt = tr / (uint32_t)a.nH, kh = tr - kt * a.nH;
+  const uint32_t sr = slot / (uint32_t)a.tw, dx = slot - sr * a.tw, dt = sr / (uint32_t)a.th, dy = sr - dt * a.th;
+  const int t = (int)(kt * a.tt + dt), y = (int)(kh * a.th + dy), x = (int)(kw * a.tw + dx);
+  const bool real = t < a.T && y < a.H && x < a.W;
+  k.natural = real ? ((int64_t)t * a.H + y) * a.W + x : -1;
+  if (real) k.at[0] = t, k.at[1] = y, k.at[2] = x;
+  return k;
+}
+
+// A lane's part of a row: channels first .. first + kVec - 1 (live: there are such channels).
+struct Part {
+  int lanes_log2;  // lanes of a row
+  int first;
+  int row;         // of the wave's rows
+  bool live;
+};
+template <class T>
+__device__ __forceinline__ Part part_of(const RowArgs& a, int lane) {
+  Part p;
+  const int chunks = a.D / Row<T>::kVec;
+  p.lanes_log2 = chunks > 1 ? 32 - __builtin_clz((unsigned)(chunks - 1)) : 0;
+  const int c = lane & ((1 << p.lanes_log2) - 1);
+  p.live = c < chunks;
+  p.first = (p.live ? c : 0) * Row<T>::kVec;
+  p.row = lane >> p.lanes_log2;
+  return p;
+}
+
+// Sum over the lanes of a row: within 16 lanes by lane exchanges on the vector ALU.
+__device__ __forceinline__ float row_sum(float x, int lanes_log2) {
+  auto dpp = [](float v, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  if (lanes_log2 > 0) x += dpp(x, std::integral_constant<int, 0xB1>());   // quad_perm 1 0 3 2
+  if (lanes_log2 > 1) x += dpp(x, std::integral_constant<int, 0x4E>());   // quad_perm 2 3 0 1
+  if (lanes_log2 > 2) x += dpp(x, std::integral_constant<int, 0x141>());  // the other quad of eight lanes
+  if (lanes_log2 > 3) x += dpp(x, std::integral_constant<int, 0x140>());  // the other eight of sixteen
+  if (lanes_log2 > 4) x += __shfl_xor(x, 16);
+  if (lanes_log2 > 5) x += __shfl_xor(x, 32);
+  return x;
+}
+
+// The rotation as the lane sees it: y[e] = c[e] x[e] + s[e] partner[e], where the partner of a channel is the other one of its pair.
+template <int kVec>
+struct Turn {
+  float c[kVec], s[kVec];
+};
+
+template <class T, bool kHalf>
+__device__ __forceinline__ void make_turn(const RowArgs& a, const Part& p, const Token& k, int64_t batch, Turn<Row<T>::kVec>& turn) {
+  constexpr int kVec = Row<T>::kVec;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) turn.c[e] = 1.f, turn.s[e] = 0.f;
+  if (!a.angles || k.natural < 0) return;
+  int at[3] = {k.at[0], k.at[1], k.at[2]};
+  if (a.where) {
+    const int32_t* w = a.where + (batch * a.N_real + k.natural) * 3;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) at[i] = w[i];
+  } else if (at[0] >= 0) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) at[i] += a.origin[i];
+  }
+  const int half = a.rotated / 2;
+#pragma unroll
+  for (int e = 0; e < kVec; e += kHalf ? 1 : 2) {
+    const int ch = p.first + e;
+    if (ch >= a.rotated) continue;
+    const int pair = kHalf ? (ch < half ? ch : ch - half) : ch >> 1;
+    const int axis = pair < a.pairs[0] ? 0 : pair < a.pairs[0] + a.pairs[1] ? 1 : 2;
+    const int within = pair - (axis == 0 ? 0 : axis == 1 ? a.pairs[0] : a.pairs[0] + a.pairs[1]);
+    const int pos = axis == 0 ? at[0] : axis == 1 ? at[1] : at[2];
+    const int pairs = axis == 0 ? a.pairs[0] : axis == 1 ? a.pairs[1] : a.pairs[2];
+    const int limit = axis == 0 ? a.positions[0] : axis == 1 ? a.positions[1] : a.positions[2];
+    const int64_t first = axis == 0 ? a.first[0] : axis == 1 ? a.first[1] : a.first[2];
+    float c = 1.f, s = 0.f;
+    if (pos >= limit) {
+      c = s = __builtin_nanf("");
+    } else if (pos >= 0) {
+      const float2 cs = reinterpret_cast<const float2*>(a.angles)[first + (int64_t)pos * pairs + within];
+      c = cs.x, s = cs.y * a.sign;
+    }
+    turn.c[e] = c;
+    if constexpr (kHalf) {
+      turn.s[e] = ch < half ? -s : s;
+    } else {
+      turn.c[e + 1] = c;
+      turn.s[e] = -s;
+      turn.s[e + 1] = s;
+    }
+  }
+}
+
+// Values of the pairs' other channels in memory (kHalf): a lane whose chunk lies in one half reads the chunk half the rotated channels away, which need
+// not be aligned; one whose chunk holds channels of both, or the end of the second, reads element by element.  Zero where there is no partner.
+enum Partner { kNone, kWhole, kSingle };
+template <class T>
+__device__ __forceinline__ Partner partner_kind(const RowArgs& a, const Part& p) {
+  const int half = a.rotated / 2, last = p.first + Row<T>::kVec;
+  if (!a.angles || p.first >= a.rotated) return kNone;
+  if (last <= half || (p.first >= half && last <= a.rotated)) return kWhole;
+  return kSingle;
+}
+template <class T>
+__device__ __forceinline__ typename Row<T>::Chunk load_partner(const RowArgs& a, const Part& p, Partner kind, const T* row) {
+  constexpr int kVec = Row<T>::kVec;
+  const int half = a.rotated / 2;
+  typename Row<T>::Chunk v;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) v[e] = (T)0.f;
+  if (kind == kWhole) {
+    __builtin_memcpy(&v, row + (p.first < half ? p.first + half : p.first - half), 16);
+  } else if (kind == kSingle) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const int ch = p.first + e;
+      if (ch < a.rotated) v[e] = row[ch < half ? ch + half : ch - half];
+    }
+  }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ void load_weights(const RowArgs& a, const Part& p, Partner kind, const void* weight, bool half, float (&w)[Row<T>::kVec], float (&wp)[Row<T>::kVec]) {
+  constexpr int kVec = Row<T>::kVec;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) w[e] = wp[e] = 1.f;
+  if (!weight) return;
+  const T* row = static_cast<const T*>(weight);
+  const auto own = *reinterpret_cast<const typename Row<T>::Chunk*>(row + p.first);
+  const auto other = half ? load_partner<T>(a, p, kind, row) : own;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) w[e] = (float)own[e], wp[e] = half ? (float)other[e] : (float)own[e ^ 1];
+}
+
+// Forward calls and the transposed rotation.  Rows are walked in the order of dst; heads are split over blockIdx.y where there are few tokens.
+// kHeads: rows that are loaded before the first of them is computed.  Measured at 75.6K tokens, 40 heads of 128 channels in bf16, q and k:
+// see launch_norm_rotate.
+template <class T, bool kHalf, bool kNorm, bool kBack>
+__global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_per_block) {
+  constexpr int kVec = Row<T>::kVec, kHeads = 4;
+  typedef typename Row<T>::Chunk Chunk;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Part p = part_of<T>(a, lane);
+  const int64_t count = !kBack && a.tiled ? a.N_pad : a.N_real, batch = blockIdx.z;
+  const int64_t row = (((int64_t)blockIdx.x * kRowWaves + wave) << (6 - p.lanes_log2)) + p.row;
+  const bool live = p.live && row < count;
+  const uint32_t at = (uint32_t)(row < count ? row : count - 1);
+  const Token k = !kBack && a.tiled ? token_of_place(a, at) : token_of_natural(a, at);
+  const bool real = k.natural >= 0;
+  const int h0 = blockIdx.y * heads_per_block, h1 = min(a.heads, h0 + heads_per_block);
+
+  Turn<kVec> turn;
+  make_turn<T, kHalf>(a, p, k, batch, turn);
+  const Partner kind = kHalf ? partner_kind<T>(a, p) : kNone;
+  const int64_t src_row = kBack && a.tiled ? k.place : k.natural, dst_row = !kBack && a.tiled ? k.place : k.natural;
+
+  for (int tensor = 0; tensor < a.tensors; ++tensor) {
+    const RowStrides ss = tensor ? a.src_strides1 : a.src_strides, ds = tensor ? a.dst_strides1 : a.dst_strides;
+    const T* __restrict__ src = static_cast<const T*>(tensor ? a.src[1] : a.src[0]) + batch * ss.batch + (real ? src_row : 0) * ss.token;
+    T* __restrict__ dst = static_cast<T*>(tensor ? a.dst[1] : a.dst[0]) + batch * ds.batch + dst_row * ds.token + p.first;
+    float own_c[kVec], other_c[kVec];  // y = own_c x + other_c partner (times r)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) own_c[e] = turn.c[e], other_c[e] = turn.s[e];
+    if constexpr (kNorm) {
+      float w[kVec], wp[kVec];
+      load_weights<T>(a, p, kind, tensor ? a.weight[1] : a.weight[0], kHalf, w, wp);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) own_c[e] *= w[e], other_c[e] *= wp[e];
+    }
+    for (int h = h0; h < h1; h += kHeads) {
+      Chunk own[kHeads], other[kHeads];
+#pragma unroll
+      for (int i = 0; i < kHeads; ++i) {
+        if (h + i < h1 && live && real) {
+          const T* r = src + (h + i) * ss.head;
+          own[i] = *reinterpret_cast<const Chunk*>(r + p.first);
+          if constexpr (kHalf) other[i] = load_partner<T>(a, p, kind, r);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) own[i][e] = other[i][e] = (T)0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kHeads; ++i) {
+        if (h + i >= h1) break;
+        float r = 1.f;
+        if constexpr (kNorm) {
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) sum += live ? (float)own[i][e] * (float)own[i][e] : 0.f;
+          r = rsqrtf(row_sum(sum, p.lanes_log2) / a.D + a.eps);
+        }
+        Chunk y;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const float x = (float)own[i][e], xp = kHalf ? (float)other[i][e] : (float)own[i][e ^ 1];
+          y[e] = (T)(r * (own_c[e] * x + other_c[e] * xp));
+        }
+        if (!real)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) y[e] = (T)0.f;  // (0 * r is NaN where eps is 0)
+        if (live) *reinterpret_cast<Chunk*>(dst + (h + i) * ds.head) = y;
+      }
+    }
+  }
+}
+
+// Gradients of the norm.  Rows are walked in natural order; a workgroup takes blocks of tokens in turn and adds up its share of the weight
+// gradients in registers, then over its waves in LDS, and leaves it in `partial`.
+template <class T, bool kHalf>
+__global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, int heads_per_block) {
+  constexpr int kVec = Row<T>::kVec, kHeads = 2;
+  typedef typename Row<T>::Chunk Chunk;
+  __shared__ float sums[2][kRowThreads * Row<T>::kVec];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Part p = part_of<T>(a, lane);
+  const int rows_log2 = 6 - p.lanes_log2;
+  const int64_t blocks_per_batch = (a.N_real + (kRowWaves << rows_log2) - 1) / (kRowWaves << rows_log2), blocks = blocks_per_batch * a.batch;
+  const int h0 = blockIdx.y * heads_per_block, h1 = min(a.heads, h0 + heads_per_block);
+  const Partner kind = kHalf ? partner_kind<T>(a, p) : kNone;
+  float dw[2][kVec];
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) dw[0][e] = dw[1][e] = 0.f;
+
+  for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+    const int64_t batch = block / blocks_per_batch, row = ((((block - batch * blocks_per_batch) * kRowWaves) + wave) << rows_log2) + p.row;
+    const bool live = p.live && row < a.N_real;
+    const Token k = token_of_natural(a, (uint32_t)(row < a.N_real ? row : a.N_real - 1));
+    Turn<kVec> turn;
+    make_turn<T, kHalf>(a, p, k, batch, turn);
+    const int64_t src_row = a.tiled ? k.place : k.natural;
+#pragma unroll
+    for (int tensor = 0; tensor < 2; ++tensor) {
+      const RowStrides ss = tensor ? a.src_strides1 : a.src_strides, ds = tensor ? a.dst_strides1 : a.dst_strides, xs = tensor ? a.x_strides1 : a.x_strides;
+      const T* __restrict__ src = static_cast<const T*>(a.src[tensor]) + batch * ss.batch + src_row * ss.token;
+      const T* __restrict__ xin = static_cast<const T*>(a.x[tensor]) + batch * xs.batch + k.natural * xs.token + p.first;
+      T* __restrict__ dst = static_cast<T*>(a.dst[tensor]) + batch * ds.batch + k.natural * ds.token + p.first;
+      float w[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) w[e] = 1.f;
+      if (a.weight[tensor]) {
+        const Chunk own = *reinterpret_cast<const Chunk*>(static_cast<const T*>(a.weight[tensor]) + p.first);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) w[e] = (float)own[e];
+      }
+      for (int h = h0; h < h1; h += kHeads) {
+        Chunk own[kHeads], other[kHeads], x[kHeads];
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+          if (h + i < h1 && live) {
+            const T* r = src + (h + i) * ss.head;
+            own[i] = *reinterpret_cast<const Chunk*>(r + p.first);
+            if constexpr (kHalf) other[i] = load_partner<T>(a, p, kind, r);
+            x[i] = *reinterpret_cast<const Chunk*>(xin + (h + i) * xs.head);
+          } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) own[i][e] = other[i][e] = x[i][e] = (T)0.f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+          if (h + i >= h1) break;
+          float u[kVec], squares = 0.f, dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const float xe = live ? (float)x[i][e] : 0.f, dyp = kHalf ? (float)other[i][e] : (float)own[i][e ^ 1];
+            u[e] = turn.c[e] * (float)own[i][e] + turn.s[e] * dyp;
+            squares += xe * xe;
+            dot += live ? w[e] * u[e] * xe : 0.f;
+          }
+          const float r = rsqrtf(row_sum(squares, p.lanes_log2) / a.D + a.eps);
+          const float lean = row_sum(dot, p.lanes_log2) / a.D * r * r;  // mean(w u n) / r * r: n mean(w u n) = x r * lean / r
+          Chunk dx;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const float xe = (float)x[i][e];
+            dx[e] = (T)(r * (w[e] * u[e] - xe * lean));
+            dw[tensor][e] += live ? u[e] * xe * r : 0.f;
+          }
+          if (live) *reinterpret_cast<Chunk*>(dst + (h + i) * ds.head) = dx;
+        }
+      }
+    }
+  }
+  if (!a.partial) return;
+#pragma unroll
+  for (int tensor = 0; tensor < 2; ++tensor)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) sums[tensor][(threadIdx.x >> p.lanes_log2 << p.lanes_log2) * kVec + (threadIdx.x & ((1 << p.lanes_log2) - 1)) * kVec + e] = dw[tensor][e];
+  __syncthreads();
+  // rows of the workgroup lie (lanes of a row) * kVec apart
+  const int stride = kVec << p.lanes_log2, rows = kRowThreads >> p.lanes_log2;
+  float* out = a.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.D;
+  for (int c = threadIdx.x; c < 2 * a.D; c += kRowThreads) {
+    const int tensor = c >= a.D, ch = c - tensor * a.D;
+    float sum = 0.f;
+    for (int r = 0; r < rows; ++r) sum += sums[tensor][r * stride + ch];
+    out[c] = sum;
+  }
+}
+
+// Adds up the workgroups' shares of the weight gradients: 16 channels a workgroup, 16 threads a channel, always in the same order.
+__global__ __launch_bounds__(256) void weight_gradient_kernel(const float* partial, int blocks, int D, float* dq, float* dk) {
+  __shared__ float sums[16][17];
+  const int channel = threadIdx.x & 15, part = threadIdx.x >> 4, c = blockIdx.x * 16 + channel;
+  float sum = 0.f;
+  if (c < 2 * D)
+    for (int b = part; b < blocks; b += 16) sum += partial[(int64_t)b * 2 * D + c];
+  sums[part][channel] = sum;
+  __syncthreads();
+  if (part == 0 && c < 2 * D) {
+    float all = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) all += sums[i][channel];
+    (c < D ? dq[c] : dk[c - D]) = all;
+  }
+}
+
+int lanes_log2(const RowArgs& a, bool bf16) {
+  const int chunks = a.D / (bf16 ? 8 : 4);
+  int log2 = 0;
+  while ((1 << log2) < chunks) ++log2;
+  return log2;
+}
+
+// Heads are split over workgroups until there are enough of these to fill the card (2048: eight of four waves on each CU).
+int head_blocks(int64_t workgroups, int heads) {
+  int blocks = 1;
+  while (blocks < heads && workgroups * blocks < 2048) blocks *= 2;
+  return std::min(blocks, heads);
+}
+
+template <bool kNorm, bool kBack>
+hipError_t launch_rows(const RowArgs& a, bool bf16, hipStream_t stream) {
+  const int rows = kRowWaves << (6 - lanes_log2(a, bf16));
+  const int64_t count = !kBack && a.tiled ? a.N_pad : a.N_real, blocks = (count + rows - 1) / rows;
+  int per = (a.heads + head_blocks(blocks * a.batch, a.heads) - 1) / head_blocks(blocks * a.batch, a.heads);
+  const dim3 grid((unsigned)blocks, (unsigned)((a.heads + per - 1) / per), (unsigned)a.batch);
+  if (grid.y > 65535 || grid.z > 65535) return hipErrorInvalidValue;
+  if (bf16) {
+    if (a.half) rows_kernel<__bf16, true, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
+    else rows_kernel<__bf16, false, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
+  } else {
+    if (a.half) rows_kernel<float, true, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
+    else rows_kernel<float, false, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const RowArgs& a, bool bf16, bool backward, hipStream_t stream) {
+  return backward ? launch_rows<false, true>(a, bf16, stream) : launch_rows<false, false>(a, bf16, stream);
+}
+
+hipError_t launch_norm_rotate(const RowArgs& a, bool bf16, hipStream_t stream) { return launch_rows<true, false>(a, bf16, stream); }
+
+hipError_t launch_norm_rotate_backward(const RowArgs& a, bool bf16, hipStream_t stream) {
+  const int rows = kRowWaves << (6 - lanes_log2(a, bf16));
+  const int64_t blocks = (a.N_real + rows - 1) / rows * a.batch;
+  const int split = (int)std::min<int64_t>(head_blocks(blocks, a.heads), std::max<int64_t>(1, kMaxGradientBlocks / std::min<int64_t>(blocks, kMaxGradientBlocks)));
+  const int per = (a.heads + split - 1) / split, head_groups = (a.heads + per - 1) / per;
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, kMaxGradientBlocks / head_groups), (unsigned)head_groups);
+  if (bf16) {
+    if (a.half) norm_backward_kernel<__bf16, true><<<grid, kRowThreads, 0, stream>>>(a, per);
+    else norm_backward_kernel<__bf16, false><<<grid, kRowThreads, 0, stream>>>(a, per);
+  } else {
+    if (a.half) norm_backward_kernel<float, true><<<grid, kRowThreads, 0, stream>>>(a, per);
+    else norm_backward_kernel<float, false><<<grid, kRowThreads, 0, stream>>>(a, per);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.partial) return e;
+  weight_gradient_kernel<<<(unsigned)((2 * a.D + 15) / 16), 256, 0, stream>>>(a.partial, (int)(grid.x * grid.y), a.D, a.dweight[0], a.dweight[1]);
+  return hipGetLastError();
+}
+
+}  // namespace ca
