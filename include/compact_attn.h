@@ -454,6 +454,48 @@ int compact_attn_norm_rotate_backward(const ca_norm* norm, const void* dq_out, c
                                       const ca_strides* dk_strides, float* dq_weight, float* dk_weight, const ca_layout* layout, void* workspace,
                                       int64_t workspace_bytes, void* stream);
 
+/* ---- Scored attention ----------------------------------------------------------------------------------------
+ *
+ * Sparse attention with scores that are capped, biased and masked beyond the tile lists, and its gradients:
+ *   s = scale * q.k;  s = cap * tanh(s / cap);  s = s - slope[head] * |position_q - position_k|
+ *   a query sees a key of its kept tiles iff their documents are equal and not negative, and position_k <= limit_q.
+ * With cap 0 and no arrays it is compact_attn_forward with a log-sum-exp and gradients.
+ *   cap        0 (none) or positive.
+ *   slopes     device pointer to num_heads floats, or NULL (no bias).  Needs positions.
+ *   positions  device pointers to int32[batch][N_real] in natural order, 4-byte aligned, or NULL.  A token's place on the line along which distances and
+ *   limits     limits are counted (a frame number, say); limits: the last position that the token sees, so limit = position is a causal
+ *   documents  order and limit = max(position, P - 1) one whose first P positions are seen by all (limits needs positions).  documents: tokens see tokens
+ *              of their own number; one below 0 is not there (a padded prompt): it sees and is seen by none.  Positions and limits of magnitude up
+ *              to 2^24 are exact, others are rounded to float.
+ * A query that sees no key has a zero result, log-sum-exp minus infinity, and no part in any gradient.  Values of tokens that are not seen must still be
+ * finite, and padding slots zero, as compact_attn_permute leaves them.  The arrays are read on the device at every call. */
+typedef struct {
+  float cap;
+  const float* slopes;
+  const int32_t *positions, *limits, *documents;
+} ca_scores;
+
+/* Bytes of device memory that a forward (backward = 0) or a backward call needs; 0 where it has no use for any. */
+int compact_attn_scored_workspace(const ca_layout* layout, const ca_scores* scores, int32_t backward, int64_t* workspace_bytes);
+
+/* out, lse = softmax(scores) v and log of the sum of exp(scores).
+ *   q, k, v, out  device pointers, [batch, heads, N_pad, D] in tile order; padding rows of out are written as zero.
+ *   lse           device pointer to float [batch, heads, N_pad]; minus infinity for padding and empty rows.
+ *   workspace     device memory of compact_attn_scored_workspace bytes, 16-byte aligned (may be NULL where that is 0); must not be used by
+ *                 anything else until the call's work on `stream` has run.
+ * out, lse and the workspace must not overlap each other or the inputs.  bf16 with (B, D) in {64,128} x {64,128}, otherwise CA_ERR_UNSUPPORTED.  Weights are
+ * rounded to bf16 before the product with v, sums are fp32, results are run-to-run identical. */
+int compact_attn_forward_scored(const void* q, const void* k, const void* v, ca_layout* layout, const ca_scores* scores, void* out, float* lse,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradients dq, dk, dv (tile order, bf16, padding rows zero) for the gradient dout of out, from the forward call's inputs and results and the same scores.
+ * dout: tile order, padding slots zero.  Weights and score gradients are rounded to bf16 as operands of the products, sums are fp32 in a fixed order.
+ * Slopes and positions get no gradient.  The first call for a layout makes its transposed lists and copies them to the device (refused with CA_ERR_INVALID_ARG on a
+ * stream under capture); compact_attn_layout_upload_backward does that up front. */
+int compact_attn_layout_upload_backward(ca_layout* layout);
+int compact_attn_backward_scored(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, ca_layout* layout,
+                                 const ca_scores* scores, void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Message of the last failure on the calling thread ("" if none); valid until the next call. */
 const char* compact_attn_last_error(void);
 

@@ -41,3 +41,8 @@ from .rotary import (  # noqa: F401
     compact_attn_rotary_upload,
     compact_attn_rotate,
 )
+from .scored import (  # noqa: F401
+    compact_attn_backward_scored,
+    compact_attn_forward_scored,
+    compact_attn_layout_upload_backward,
+)

@@ -57,6 +57,10 @@ EXPORTED = (
     "compact_attn_norm_rotate",
     "compact_attn_norm_workspace",
     "compact_attn_norm_rotate_backward",
+    "compact_attn_scored_workspace",
+    "compact_attn_forward_scored",
+    "compact_attn_layout_upload_backward",
+    "compact_attn_backward_scored",
     "compact_attn_last_error",
 )
 

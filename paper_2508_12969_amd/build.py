@@ -9,7 +9,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "libcompact_attn.so")
 SOURCES = ["layout.cpp", "search.cpp", "api.cpp", "permute.hip", "attn_f32.hip", "attn_f32_planes.hip", "attn_bf16.hip", "attn_bf16_pair.hip", "attn_bf16_ways.hip",
-           "attn_bf16_merge.hip", "tile_mass.hip", "api_rotary.cpp", "rotary.hip"]
+           "attn_bf16_merge.hip", "tile_mass.hip", "api_rotary.cpp", "rotary.hip", "api_scored.cpp", "attn_scored.hip",
+           "attn_scored_back.hip"]
 CALLS_PATH = os.path.join(PKG_DIR, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))   # of this Python
 PER_FILE_FLAGS = {}   # extra hipcc flags for single sources, if any
 ARCH = "gfx950"

@@ -150,14 +150,7 @@ int fill_rows(ca::RowArgs& a, const ca_layout* L, ca_rotary* r, const ca_where* 
   a.batch = p.batch;
   a.heads = p.num_heads;
   a.D = p.head_dim;
-  a.T = p.T; a.H = p.H; a.W = p.W;
-  a.tt = p.tt; a.th = p.th; a.tw = p.tw;
-  a.nH = L->nH; a.nW = L->nW;
-  a.B = (int32_t)L->B;
-  a.n_vid = L->n_vid;
-  a.N_real = L->N_real;
-  a.N_pad = L->N_pad;
-  a.N_video = (int64_t)p.T * p.H * p.W;
+  fill_grid(a, L);
   a.tiled = tiled;
   a.sign = 1.f;
   if (!r) return CA_OK;

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "compact_attn.h"
+#include "tokens.h"
 
 struct ca_rotary {
   ca_rotary_axis axes[3]{};
@@ -31,7 +32,7 @@ struct RowStrides {
 };
 
 // One launch over the rows (token, head) of one or two tensors.
-struct RowArgs {
+struct RowArgs : GridArgs {  // rows are walked in the order of dst, which is in tile order (tiled forward) or in natural order
   const void* src[2];
   void* dst[2];
   const void* x[2];            // norm, backward: the forward call's inputs
@@ -41,9 +42,6 @@ struct RowArgs {
   float* dweight[2];
   float eps;
   int32_t tensors, batch, heads, D;
-  // geometry: rows are walked in the order of dst, which is in tile order (tiled forward) or in natural order
-  int32_t T, H, W, tt, th, tw, nH, nW, B;
-  int64_t n_vid, N_real, N_pad, N_video;
   int32_t tiled;               // the tensor that is not the model's own is in tile order: dst of forward, src of backward calls
   // rotation
   const float* angles;         // (cos, sin) pairs; null: no rotation
