@@ -475,8 +475,14 @@ typedef struct {
   const int32_t *positions, *limits, *documents;
 } ca_scores;
 
-/* Bytes of device memory that a forward (backward = 0) or a backward call needs; 0 where it has no use for any. */
-int compact_attn_scored_workspace(const ca_layout* layout, const ca_scores* scores, int32_t backward, int64_t* workspace_bytes);
+/* Bytes of device memory that a forward (backward = 0) or a backward call needs; 0 where it has no use for any: the token arrays in tile order, two floats
+ * for a query (backward), and at most 128 MiB for partial sums where long lists are shared by several workgroups.  The first call for a layout makes the
+ * lists that scored attention walks over, on the host. */
+int compact_attn_scored_workspace(ca_layout* layout, const ca_scores* scores, int32_t backward, int64_t* workspace_bytes);
+
+/* Copies these lists to the current device, those of backward calls too if backward is 1.  Synchronous; idempotent.  The calls do it on first use
+ * if it was not called (refused with CA_ERR_INVALID_ARG while their stream is being captured). */
+int compact_attn_layout_upload_scored(ca_layout* layout, int32_t backward);
 
 /* out, lse = softmax(scores) v and log of the sum of exp(scores).
  *   q, k, v, out  device pointers, [batch, heads, N_pad, D] in tile order; padding rows of out are written as zero.
@@ -490,9 +496,7 @@ int compact_attn_forward_scored(const void* q, const void* k, const void* v, ca_
 
 /* Gradients dq, dk, dv (tile order, bf16, padding rows zero) for the gradient dout of out, from the forward call's inputs and results and the same scores.
  * dout: tile order, padding slots zero.  Weights and score gradients are rounded to bf16 as operands of the products, sums are fp32 in a fixed order.
- * Slopes and positions get no gradient.  The first call for a layout makes its transposed lists and copies them to the device (refused with CA_ERR_INVALID_ARG on a
- * stream under capture); compact_attn_layout_upload_backward does that up front. */
-int compact_attn_layout_upload_backward(ca_layout* layout);
+ * Slopes and positions get no gradient. */
 int compact_attn_backward_scored(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, ca_layout* layout,
                                  const ca_scores* scores, void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes, void* stream);
 

@@ -44,5 +44,5 @@ from .rotary import (  # noqa: F401
 from .scored import (  # noqa: F401
     compact_attn_backward_scored,
     compact_attn_forward_scored,
-    compact_attn_layout_upload_backward,
+    compact_attn_layout_upload_scored,
 )

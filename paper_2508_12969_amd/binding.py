@@ -59,7 +59,7 @@ EXPORTED = (
     "compact_attn_norm_rotate_backward",
     "compact_attn_scored_workspace",
     "compact_attn_forward_scored",
-    "compact_attn_layout_upload_backward",
+    "compact_attn_layout_upload_scored",
     "compact_attn_backward_scored",
     "compact_attn_last_error",
 )

@@ -96,7 +96,6 @@ int upload_tables(std::vector<Table>& tables, unsigned char** block) {
 void free_device_tables(ca::DeviceTables& d) {
   if (d.block) (void)hipFree(d.block);
   if (d.mass_partial) (void)hipFree(d.mass_partial);
-  if (d.transposed_block) (void)hipFree(d.transposed_block);
   d = ca::DeviceTables{};
 }
 

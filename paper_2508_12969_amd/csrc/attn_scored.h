@@ -4,8 +4,8 @@
 //   O = softmax(s) V,  L = log sum exp s
 //   P = exp(s - L),  dV = P^T dO,  dP = dO V^T,  dS = P (dP - rowsum(dO O)) (1 - tanh^2),  dQ = scale dS K,  dK = scale dS^T Q
 //
-// One shape of kernel serves all of them.  A workgroup owns a tile of queries (forward, dQ) or of keys (dK, dV), a wave 32 of its
-// tokens, one a lane: they are the columns of every product, and stay in registers.  The tokens of the other side stream through LDS in steps of two
+// One shape of kernel serves all of them.  A workgroup owns 128 queries (forward, dQ) or keys (dK, dV), a tile or two neighbours (ScoredWalk), a wave 32 of
+// them, one a lane: they are the columns of every product, and stay in registers.  The tokens of the other side stream through LDS in steps of two
 // tensors X and Y: keys and values, or queries and gradients dO.  With S^T = X own^T, a lane holds the scores of its token, so that the
 // weights, rounded to bf16, are register for register the second operand of the products that follow, which read X or Y transposed from LDS:
 //             own         X, Y     S        dP       sums
@@ -32,10 +32,10 @@ constexpr bool owns_keys(ScoredKernel k) { return k == kScoredDKV || k == kScore
 
 template <int B_, int D_>
 struct ScoredShape {
-  static constexpr int B = B_, D = D_;
-  static constexpr int kWaves = B / 32, kThreads = kWaves * 64;
-  // Tokens of a step: two buffers of X and Y take 64 KiB (B = 128, D = 128) or 32 KiB of LDS.
-  static constexpr int kStep = D == 64 ? 64 : B / 2;
+  static constexpr int B = B_, D = D_;               // B: tokens of a tile
+  static constexpr int kWaves = kGroupTokens / 32, kThreads = kWaves * 64;
+  static constexpr int kTiles = kGroupTokens / B;    // tiles of a group
+  static constexpr int kStep = 64;                   // streamed tokens of a step
   static constexpr int kHalves = B / kStep;          // steps of a tile
   static constexpr int kBlocks = kStep / 32;
   static constexpr int kRowBytes = D * 2, kChunksPerRow = D / 8, kRowsPerLoad = 1024 / kRowBytes;
@@ -43,7 +43,7 @@ struct ScoredShape {
   static constexpr int kLoads = kStepBytes / 1024 / kWaves;  // wave-wide copies of X (and of Y) per wave
   static constexpr int kContraction = D / 16, kDBlocks = D / 32;
   static constexpr int kInfoRows = 6;                // position, document, limit, -, log-sum-exp, delta
-  static constexpr int kListTiles = 512;             // tiles of a list cut into steps at a time
+  static constexpr int kListTiles = 512;             // words of a list cut into steps at a time
   static_assert(kLoads == 2 || kLoads == 4, "copies are written for two or four loads");
 };
 
@@ -51,7 +51,7 @@ template <class S>
 struct ScoredLds {
   char x[2][S::kStepBytes], y[2][S::kStepBytes];
   float info[2][S::kInfoRows][S::kStep];
-  uint32_t steps[S::kListTiles * S::kHalves + 2];
+  uint32_t steps[S::kListTiles * S::kHalves];
   int counts[S::kWaves];
 };
 
@@ -62,10 +62,10 @@ __device__ __forceinline__ int swizzle(int row) {
   return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-// A word of the step list: tile id, which part of the tile, and bits 25-31: its padding class (without arrays), or 1: compare (with).
+// A word of the step list: tile id, bit 24: which half of it, bits 25 and 26: the tiles of the group that visit it, bits 27-31: its padding class
+// (without arrays), or bits 27 and 28: the tiles of the group that have to compare (with).
 __device__ __forceinline__ int step_tile(uint32_t w) { return (int)(w & 0xffffffu); }
 __device__ __forceinline__ int step_half(uint32_t w) { return (int)(w >> 24) & 1; }
-__device__ __forceinline__ int step_kind(uint32_t w) { return (int)(w >> 25); }
 
 // Copies of a step's X and Y, asynchronous.
 template <class S>
@@ -103,22 +103,19 @@ struct StepCopy {
           : "memory");
     }
   }
-  // `rows` rows of kStep words, B words apart in memory, one after the other in LDS; a wave-wide load moves 64 words, and `wave_of` says whose turn it is.
-  // rows * kStep is a multiple of 64.
-  __device__ __forceinline__ void words(const float* from, uint32_t lds, int rows, int wave_of) const {
-    constexpr int kRowsAtOnce = 64 / S::kStep;
-    for (int r = 0; r < rows; r += kRowsAtOnce, ++wave_of) {
-      if (wave_of % S::kWaves != wave) continue;
-      const uint32_t off = (uint32_t)((lane / S::kStep) * S::B + lane % S::kStep) * 4u;
-      const float* sb = from + r * S::B;
-      const uint32_t m0 = lds + (uint32_t)(r * S::kStep) * 4u;
-      asm volatile(
-          "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
-          "global_load_lds_dword %[v], %[sb] offset:0\n\t"
-          :
-          : [m0] "s"(m0), [v] "v"(off), [sb] "s"(sb)
-          : "memory");
-    }
+  // `rows` rows of kStep = 64 words, B words apart in memory, one after the other in LDS: row r by wave first_wave + r.
+  __device__ __forceinline__ void words(const float* from, uint32_t lds, int rows, int first_wave) const {
+    static_assert(S::kStep == 64, "a row is a wave-wide load");
+    const int r = (wave - first_wave) & (S::kWaves - 1);
+    if (r >= rows) return;
+    const float* sb = from + r * S::B;
+    const uint32_t off = (uint32_t)lane * 4u, m0 = lds + (uint32_t)(r * S::kStep) * 4u;
+    asm volatile(
+        "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
+        "global_load_lds_dword %[v], %[sb] offset:0\n\t"
+        :
+        : [m0] "s"(m0), [v] "v"(off), [sb] "s"(sb)
+        : "memory");
   }
 };
 
@@ -130,9 +127,9 @@ __device__ __forceinline__ bool all_visible(const TileLine& q, const TileLine& k
   return q.doc_min == q.doc_max && k.doc_min == q.doc_min && k.doc_max == q.doc_min && k.pos_max <= q.limit_min;
 }
 
-// Cuts `count` tiles of a list into steps; the number of these.  All threads take part.
+// Cuts `count` words of a list into steps; the number of these.  All threads take part.  own: the group's tiles.
 template <class S, bool kLine, ScoredKernel K>
-__device__ __forceinline__ int cut_steps(const ScoredArgs& a, const int32_t* meta, int count, const TileLine& own, const TileLine* tiles, ScoredLds<S>& lds) {
+__device__ __forceinline__ int cut_steps(const ScoredArgs& a, const uint32_t* words, int count, const TileLine (&own)[2], const TileLine* tiles, ScoredLds<S>& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const auto mask = reinterpret_cast<const uint32_t*>(a.class_mask);
   int total = 0;
@@ -140,21 +137,26 @@ __device__ __forceinline__ int cut_steps(const ScoredArgs& a, const int32_t* met
     bool keep[2] = {false, false};
     uint32_t word = 0;
     if (first + tid < count) {
-      const uint32_t w = (uint32_t)meta[first + tid];
-      const int tile = (int)(w & 0xffffffu), cls = (int)(w >> 24) & 0x7f;
+      const uint32_t w = words[first + tid], tile = w & 0xffffffu, cls = (w >> 24) & 0x3fu;
+      uint32_t member = w >> 30, kind = cls;
+      if constexpr (kLine) {
+        const TileLine other = tiles[tile];
+        kind = 0;
+#pragma unroll
+        for (int t = 0; t < S::kTiles; ++t) {
+          const bool any = owns_keys(K) ? any_visible(other, own[t]) : any_visible(own[t], other);
+          const bool compare = owns_keys(K) ? !all_visible(other, own[t]) : !(other.whole && all_visible(own[t], other));
+          if (!any) member &= ~(1u << t);
+          if (compare) kind |= 1u << t;
+        }
+      }
+      word = tile | member << 25 | kind << 27;
 #pragma unroll
       for (int h = 0; h < S::kHalves; ++h) {
         uint32_t valid = 0;
 #pragma unroll
         for (int b = 0; b < S::kBlocks; ++b) valid |= mask[cls * 4 + h * S::kBlocks + b];
-        keep[h] = valid != 0;
-      }
-      word = (uint32_t)tile | (uint32_t)cls << 25;
-      if constexpr (kLine) {
-        const TileLine other = tiles[tile];
-        const bool compare = owns_keys(K) ? !all_visible(other, own) : !(other.whole && all_visible(own, other));
-        word = (uint32_t)tile | (compare ? 1u << 25 : 0u);
-        if (!(owns_keys(K) ? any_visible(other, own) : any_visible(own, other))) keep[0] = keep[1] = false;
+        keep[h] = valid != 0 && (member & (S::kTiles == 2 ? 3u : 1u)) != 0;
       }
     }
     const uint64_t b0 = __builtin_amdgcn_ballot_w64(keep[0]), b1 = __builtin_amdgcn_ballot_w64(keep[1]);
@@ -205,30 +207,30 @@ struct Fragments {
   }
 };
 
-// The scalars that turn products into scores, in raw units (before the scale): s' = s / scale.
+// The scalars that turn products q.k into scores.  Scores are held in a unit of their own, x, with log2(e) s = c2 x + offset: without a cap x is the
+// product itself, with one x = -1 / (2^(bend q.k) + 1), which is (tanh(s / cap) - 1) / 2: the last steps of the tanh are part of the factor and of an offset
+// that the softmax does not see.
 struct ScoreRule {
   bool capped, biased;
-  float bend, cap_raw;   // tanh(s / cap) = 1 - 2 / (2^(bend s') + 1)
-  float slope_raw;       // minus the slope, per position
-  float c2;              // scale log2(e)
+  float bend, c2, offset;
+  float slope;           // minus the slope, in units of x per position
   __device__ __forceinline__ ScoreRule(const ScoredArgs& a, int64_t head) {
-    c2 = a.scale * kLog2e;
     capped = a.cap > 0.f;
-    bend = capped ? 2.f * c2 / a.cap : 0.f;
-    cap_raw = a.cap / a.scale;
+    bend = capped ? 2.f * a.scale * kLog2e / a.cap : 0.f;
+    c2 = (capped ? 2.f * a.cap : a.scale) * kLog2e;
+    offset = capped ? a.cap * kLog2e : 0.f;
     biased = a.slopes != nullptr;
-    slope_raw = biased ? -a.slopes[head] / a.scale : 0.f;
+    slope = biased ? -a.slopes[head] / (capped ? 2.f * a.cap : a.scale) : 0.f;
   }
 };
 
-// Caps 16 scores; `steep` receives 1 - tanh^2 = 4 r (1 - r), r = 1 / (2^(bend s') + 1), where the caller wants it.
+// Caps 16 scores; `steep` receives 1 - tanh^2 = -4 x (1 + x) where the caller wants it.
 template <bool kSteep>
 __device__ __forceinline__ void cap_scores(const ScoreRule& rule, floatx16& s, floatx16& steep) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const float w = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * rule.bend) + 1.f);
-    s[r] = __builtin_fmaf(-2.f * rule.cap_raw, w, rule.cap_raw);
-    if constexpr (kSteep) steep[r] = 4.f * (w - w * w);
+    s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
+    if constexpr (kSteep) steep[r] = -4.f * __builtin_fmaf(s[r], s[r], s[r]);
   }
 }
 
@@ -255,24 +257,24 @@ __device__ __forceinline__ floatx4 read4(const float* row, int block, int i, int
 template <class S, ScoredKernel K>
 __device__ __forceinline__ void bias_and_compare(const ScoreRule& rule, floatx16& s, const float (&info)[S::kInfoRows][S::kStep], int block, int g, bool compare, float own_pos,
                                                  int own_doc, float own_limit) {
-  if (!rule.biased && !compare) return;
+  if (rule.biased)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const floatx4 pos = read4(info[kLinePosition], block, i, g);
-    if (rule.biased)
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 pos = read4(info[kLinePosition], block, i, g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[4 * i + e] = __builtin_fmaf(__builtin_fabsf(own_pos - pos[e]), rule.slope_raw, s[4 * i + e]);
-    if (compare) {
+      for (int e = 0; e < 4; ++e) s[4 * i + e] = __builtin_fmaf(__builtin_fabsf(own_pos - pos[e]), rule.slope, s[4 * i + e]);
+    }
+  if (compare)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 reach = read4(info[owns_keys(K) ? kLineLimit : kLinePosition], block, i, g);
       const intx4 doc = __builtin_bit_cast(intx4, read4(info[kLineDocument], block, i, g));
-      floatx4 limit;
-      if constexpr (owns_keys(K)) limit = read4(info[kLineLimit], block, i, g);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool reached = owns_keys(K) ? own_pos <= limit[e] : pos[e] <= own_limit;
-        s[4 * i + e] = reached && doc[e] == own_doc ? s[4 * i + e] : kMinusInf;
+        const bool seen = (int)(owns_keys(K) ? own_pos <= reach[e] : reach[e] <= own_limit) & (int)(doc[e] == own_doc);
+        s[4 * i + e] = seen ? s[4 * i + e] : kMinusInf;
       }
     }
-  }
 }
 
 __device__ __forceinline__ void rounded(const floatx16& p, bf16x8 (&out)[2]) {
@@ -324,11 +326,69 @@ __device__ __forceinline__ void block_sums(const Fragments<S>& f, LdsTile lds, i
     for (int db = 0; db < S::kDBlocks; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.transposed(lds, block, t, db), w[t], acc[db], 0, 0, 0);
 }
 
-// The softmax state of the lane's query and one step of it: see QueryWave::softmax for the lagging reference.  The row sum adds up the weights before they
+// The softmax state of the lane's query: see QueryWave::softmax for the lagging reference.  The row sum adds up the weights before they
 // are rounded, because the log-sum-exp is an output of its own (a sum of rounded weights is off by up to 2^-8 where a row has few keys).
 struct Softmax {
-  float ref = kMinusInf, sum = 0.f;  // reference in raw units; this lane's share of the sum
+  float ref = kMinusInf, sum = 0.f;  // reference in units of x; this lane's share of the sum
 };
+
+// The lane's token, and what becomes of its sums.
+template <class S, bool kLine>
+struct OwnToken {
+  int64_t tile, row;    // row: in the plane
+  bool active, there;   // the wave has tokens at all; the token is in the grid and has a document that is not negative
+  bool writes;          // it has a row
+  float pos = 0.f, limit = __builtin_inff();
+  int doc = 0;
+  __device__ __forceinline__ OwnToken(const ScoredArgs& a, int64_t batch, int64_t first_tile, int wave, int i) {
+    constexpr int kWavesPerTile = S::B / 32;
+    tile = first_tile + wave / kWavesPerTile;
+    writes = tile < a.n;
+    if (!writes) tile = a.n - 1;
+    const QuerySlot slot = query_slot<S::B>(a, tile, wave % kWavesPerTile * 32, i);
+    active = slot.wave_active && writes;
+    row = tile * S::B + slot.slot;
+    there = slot.real && writes;
+    if constexpr (kLine) {
+      const float* t = a.line + (batch * a.n + tile) * kLineRows * S::B + slot.slot;
+      pos = t[kLinePosition * S::B];
+      limit = t[kLineLimit * S::B];
+      doc = __builtin_bit_cast(int, t[kLineDocument * S::B]);
+      there = there && doc >= 0;
+      if (doc < 0) doc = -2;  // sees nothing, not even tokens without a document
+    }
+  }
+};
+
+template <class S, ScoredKernel K>
+constexpr int sums_of() {
+  return K == kScoredDKV ? 2 : 1;
+}
+
+// Writes a token's results; sum1, sum2 as in the kernel.
+template <class S, ScoredKernel K, class Token>
+__device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const Softmax& soft, const floatx16* sum1,
+                                              const floatx16* sum2) {
+  if (!own.writes) return;
+  const int64_t at = (plane * a.n * S::B + own.row) * S::kRowBytes;
+  using Sums = const floatx16(&)[S::kDBlocks];
+  if constexpr (K == kScoredForward) {
+    const float sum = sum_with_partner(soft.sum);
+    const bool empty = !own.there || sum == 0.f;
+    store_columns<S>(static_cast<char*>(a.out) + at, g, reinterpret_cast<Sums>(*sum2), 1.f / sum, !empty);
+    if (g == 0) a.lse[plane * a.n * S::B + own.row] = empty ? kMinusInf : (__builtin_fmaf(soft.ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+  if constexpr (K == kScoredDQ) store_columns<S>(static_cast<char*>(a.dq) + at, g, reinterpret_cast<Sums>(*sum1), a.scale, own.there);
+  if constexpr (K == kScoredDK || K == kScoredDKV) store_columns<S>(static_cast<char*>(a.dk) + at, g, reinterpret_cast<Sums>(*sum1), a.scale, own.there);
+  if constexpr (K == kScoredDV || K == kScoredDKV) store_columns<S>(static_cast<char*>(a.dv) + at, g, reinterpret_cast<Sums>(*sum2), 1.f, own.there);
+}
+
+// A wave's part of a share: floatx4 per lane, lane by lane, so that every store is whole lines.
+template <class S, ScoredKernel K>
+__device__ __forceinline__ float* share_at(const ScoredArgs& a, int64_t share, int wave) {
+  constexpr int64_t kWaveFloats = share_floats(S::D, sums_of<S, K>()) / S::kWaves;
+  return a.share_sums + (share * S::kWaves + wave) * kWaveFloats;
+}
 
 template <class S, bool kLine, ScoredKernel K>
 __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads), amdgpu_waves_per_eu(2, 2))) void scored_kernel(ScoredArgs a) {
@@ -336,9 +396,9 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   constexpr bool kSum1 = K == kScoredDQ || K == kScoredDKV || K == kScoredDK, kSum2 = kForward || K == kScoredDKV || K == kScoredDV;
   __shared__ __attribute__((aligned(1024))) ScoredLds<S> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
-  const int64_t rows = (int64_t)a.num_heads * a.n;
-  const int64_t linear = xcd_launch_order(blockIdx.x, gridDim.x, xcd_chunk(gridDim.x));
-  const int64_t batch = linear / rows, row = a.order[linear - batch * rows], head = row / a.n, tile = row - head * a.n;
+  const int64_t linear = xcd_launch_order(blockIdx.x, gridDim.x, xcd_chunk(gridDim.x)), batch = linear / a.num_items;
+  const ScoredItem item = a.items[linear - batch * a.num_items];
+  const int64_t groups = (a.n + S::kTiles - 1) / S::kTiles, head = item.group / groups, first_tile = (item.group - head * groups) * S::kTiles;
   const int64_t plane = batch * a.num_heads + head, plane_bytes = a.n * (int64_t)S::B * S::kRowBytes;
   const char* const X = static_cast<const char*>(kKeys ? a.q : a.k) + plane * plane_bytes;
   const char* const Y = static_cast<const char*>(kKeys ? a.dout : a.v) + plane * plane_bytes;
@@ -346,30 +406,19 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   const float* const stats = kForward ? nullptr : a.rows + plane * a.n * 2 * S::B;
   const ScoreRule rule(a, head);
 
-  // the lane's token
-  const QuerySlot slot = query_slot<S::B>(a, tile, wave * 32, i);
-  const bool active = slot.wave_active;
-  const int64_t own_row = tile * S::B + slot.slot;
-  bool there = slot.real;
-  float own_pos = 0.f, own_limit = __builtin_inff(), own_lse = 0.f, own_delta = 0.f;
-  int own_doc = 0;
-  if constexpr (kLine) {
-    const float* t = line + tile * kLineRows * S::B + slot.slot;
-    own_pos = t[kLinePosition * S::B];
-    own_limit = t[kLineLimit * S::B];
-    own_doc = __builtin_bit_cast(int, t[kLineDocument * S::B]);
-    there = there && own_doc >= 0;
-    if (own_doc < 0) own_doc = -2;  // sees nothing, not even tokens without a document
-  }
+  OwnToken<S, kLine> own(a, batch, first_tile, wave, i);
+  float own_lse = 0.f, own_delta = 0.f;
   bf16x8 own1[S::kContraction], own2[kSum1 ? S::kContraction : 1];
-  load_own<S>(static_cast<const char*>(kKeys ? a.k : a.q) + plane * plane_bytes + own_row * S::kRowBytes, g, own1);
-  if constexpr (kSum1) load_own<S>(static_cast<const char*>(kKeys ? a.v : a.dout) + plane * plane_bytes + own_row * S::kRowBytes, g, own2);
+  load_own<S>(static_cast<const char*>(kKeys ? a.k : a.q) + plane * plane_bytes + own.row * S::kRowBytes, g, own1);
+  if constexpr (kSum1) load_own<S>(static_cast<const char*>(kKeys ? a.v : a.dout) + plane * plane_bytes + own.row * S::kRowBytes, g, own2);
   if constexpr (K == kScoredDQ) {
-    own_lse = stats[tile * 2 * S::B + slot.slot];
-    own_delta = stats[tile * 2 * S::B + S::B + slot.slot];
+    const float* const t = stats + own.tile * 2 * S::B + (own.row - own.tile * S::B);
+    own_lse = t[0];
+    own_delta = t[S::B];
     asm volatile("" : "+v"(own_lse), "+v"(own_delta));
   }
-  asm volatile("" : "+v"(own_pos), "+v"(own_limit), "+v"(own_doc));
+  asm volatile("" : "+v"(own.pos), "+v"(own.limit), "+v"(own.doc));
+  const uint32_t member = 1u << (25 + wave / (S::B / 32)), compares = 1u << (27 + wave / (S::B / 32));  // the wave's tile in a step's word
 
   floatx16 sum1[kSum1 ? S::kDBlocks : 1], sum2[kSum2 ? S::kDBlocks : 1];
 #pragma unroll
@@ -391,19 +440,18 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     const int64_t first = (int64_t)step_tile(w) * S::B + step_half(w) * S::kStep;
     copy.tensor(X + first * S::kRowBytes, lds_x + buffer * S::kStepBytes);
     copy.tensor(Y + first * S::kRowBytes, lds_y + buffer * S::kStepBytes);
-    if constexpr (kLine)
-      copy.words(line + (int64_t)step_tile(w) * kLineRows * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes, kKeys ? 4 : 2, 0);
-    if constexpr (kKeys)
-      copy.words(stats + (int64_t)step_tile(w) * 2 * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes + 4 * S::kStep * 4, 2, 2);
+    if constexpr (kLine) copy.words(line + (int64_t)step_tile(w) * kLineRows * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes, kKeys ? 3 : 2, 0);
+    if constexpr (kKeys) copy.words(stats + (int64_t)step_tile(w) * 2 * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes + 4 * S::kStep * 4, 2, 2);
   };
 
   const TileLine* const tiles = kLine ? a.tiles + batch * a.n : nullptr;
-  TileLine own_tile{};
-  if constexpr (kLine) own_tile = tiles[tile];
-  const int64_t begin = a.row_ptr[row];
-  const int count = (int)(a.row_ptr[row + 1] - begin);
-  for (int first = 0; first < count; first += S::kListTiles) {
-    const int steps = cut_steps<S, kLine, K>(a, a.col_meta + begin + first, min(S::kListTiles, count - first), own_tile, tiles, lds);
+  TileLine own_tiles[2]{};
+  if constexpr (kLine) {
+    own_tiles[0] = tiles[first_tile];
+    if (S::kTiles == 2 && first_tile + 1 < a.n) own_tiles[1] = tiles[first_tile + 1];  // (else no word names it)
+  }
+  for (int first = 0; first < item.count; first += S::kListTiles) {
+    const int steps = cut_steps<S, kLine, K>(a, a.words + item.first + first, min(S::kListTiles, item.count - first), own_tiles, tiles, lds);
     if (steps == 0) continue;
     uint32_t word = __builtin_amdgcn_readfirstlane(lds.steps[0]), next = 0;
     if (steps > 1) next = __builtin_amdgcn_readfirstlane(lds.steps[1]);
@@ -416,11 +464,12 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
       WAIT_LGKMCNT0();
       BARRIER();  // the step's X and Y are there, and nobody reads the other buffer any more
       if (step + 1 < steps) issue(next, buffer ^ 1);
-      if (active) {
+      if (own.active && (word & member) != 0) {
         const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
         const float(&info)[S::kInfoRows][S::kStep] = lds.info[buffer];
-        const bool compare = kLine && step_kind(word) != 0;
-        const auto valid = CONST_PTR(uint32_t, a.class_mask) + (kLine ? 0 : step_kind(word) * 4 + step_half(word) * S::kBlocks);
+        const bool compare = kLine && (word & compares) != 0;
+        const int cls = kLine ? 0 : (int)(word >> 27);
+        const auto valid = CONST_PTR(uint32_t, a.class_mask) + (cls * 4 + step_half(word) * S::kBlocks);
         if constexpr (kForward) {
           floatx16 s[S::kBlocks], unused;
 #pragma unroll
@@ -430,8 +479,8 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
             for (int b = 0; b < S::kBlocks; ++b) cap_scores<false>(rule, s[b], unused);
           if constexpr (kLine) {
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) bias_and_compare<S, K>(rule, s[b], info, b, g, compare, own_pos, own_doc, own_limit);
-          } else if (step_kind(word) != 0) {
+            for (int b = 0; b < S::kBlocks; ++b) bias_and_compare<S, K>(rule, s[b], info, b, g, compare, own.pos, own.doc, own.limit);
+          } else if (cls != 0) {
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) mask_slots(s[b], __builtin_amdgcn_readfirstlane(valid[b]));
           }
@@ -471,8 +520,8 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
             floatx16 s = block_product<S>(frag, x, b, own1);
             if (rule.capped) cap_scores<kSum1>(rule, s, steep);
             if constexpr (kLine) {
-              bias_and_compare<S, K>(rule, s, info, b, g, compare, own_pos, own_doc, own_limit);
-            } else if (K == kScoredDQ && step_kind(word) != 0) {
+              bias_and_compare<S, K>(rule, s, info, b, g, compare, own.pos, own.doc, own.limit);
+            } else if (K == kScoredDQ && cls != 0) {
               mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
             }
 #pragma unroll
@@ -488,20 +537,20 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
               block_sums<S>(frag, y, b, p, sum2);
             }
             if constexpr (kSum1) {
-            const floatx16 dp = block_product<S>(frag, y, b, own2);
+              const floatx16 dp = block_product<S>(frag, y, b, own2);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              floatx4 delta;
-              if constexpr (kKeys) delta = read4(info[5], b, j, g);
+              for (int j = 0; j < 4; ++j) {
+                floatx4 delta;
+                if constexpr (kKeys) delta = read4(info[5], b, j, g);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s[4 * j + e] *= dp[4 * j + e] - (kKeys ? delta[e] : own_delta);
-            }
-            if (rule.capped)
+                for (int e = 0; e < 4; ++e) s[4 * j + e] *= dp[4 * j + e] - (kKeys ? delta[e] : own_delta);
+              }
+              if (rule.capped)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) s[r] *= steep[r];
-            bf16x8 ds[2];
-            rounded(s, ds);
-            block_sums<S>(frag, x, b, ds, sum1);
+                for (int r = 0; r < 16; ++r) s[r] *= steep[r];
+              bf16x8 ds[2];
+              rounded(s, ds);
+              block_sums<S>(frag, x, b, ds, sum1);
             }
           }
         }
@@ -513,34 +562,84 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     BARRIER();  // before the list and the buffers are filled again
   }
 
-  const int64_t at = plane * plane_bytes + own_row * S::kRowBytes;
-  if constexpr (kForward) {
-    const float sum = sum_with_partner(soft.sum);
-    const bool empty = !there || sum == 0.f;
-    store_columns<S>(static_cast<char*>(a.out) + at, g, sum2, 1.f / sum, !empty);
-    if (g == 0) a.lse[plane * a.n * S::B + own_row] = empty ? kMinusInf : (soft.ref * rule.c2 + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  if (item.share < 0) {
+    store_results<S, K>(a, rule, plane, own, g, soft, sum1, sum2);
+    return;
   }
-  if constexpr (K == kScoredDQ) store_columns<S>(static_cast<char*>(a.dq) + at, g, sum1, a.scale, there);
-  if constexpr (kKeys) {
-    if constexpr (kSum1) store_columns<S>(static_cast<char*>(a.dk) + at, g, sum1, a.scale, there);
-    if constexpr (kSum2) store_columns<S>(static_cast<char*>(a.dv) + at, g, sum2, 1.f, there);
-  }
+  floatx4* out = reinterpret_cast<floatx4*>(share_at<S, K>(a, batch * a.shares + item.share, wave));
+  reinterpret_cast<float2*>(out)[lane] = float2{soft.ref, soft.sum};
+  out += 32;
+  auto leave = [&](const floatx16* sums) {
+#pragma unroll
+    for (int j = 0; j < 4 * S::kDBlocks; ++j, out += 64) out[lane] = floatx4{sums[j / 4][j % 4 * 4], sums[j / 4][j % 4 * 4 + 1], sums[j / 4][j % 4 * 4 + 2], sums[j / 4][j % 4 * 4 + 3]};
+  };
+  if constexpr (kSum1) leave(sum1);
+  if constexpr (kSum2) leave(sum2);
 }
 
-template <ScoredKernel K, int B, int D>
-hipError_t launch_shape(const ScoredArgs& a, hipStream_t stream) {
-  using S = ScoredShape<B, D>;
-  const int64_t workgroups = (int64_t)a.batch * a.num_heads * a.n;
-  if (workgroups < 1 || workgroups > 0x7fffffff) return hipErrorInvalidValue;
-  if (a.line) scored_kernel<S, true, K><<<(unsigned)workgroups, S::kThreads, 0, stream>>>(a);
-  else scored_kernel<S, false, K><<<(unsigned)workgroups, S::kThreads, 0, stream>>>(a);
+// Adds up the shares of a group, in their order, and writes its results.  Bound: the shares, once.
+template <class S, bool kLine, ScoredKernel K>
+__global__ __launch_bounds__(S::kThreads) void scored_merge_kernel(ScoredArgs a) {
+  constexpr bool kForward = K == kScoredForward, kSum1 = K == kScoredDQ || K == kScoredDKV || K == kScoredDK, kSum2 = kForward || K == kScoredDKV || K == kScoredDV;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
+  const int64_t batch = blockIdx.x / a.num_merges;
+  const ScoredMerge merge = a.merges[blockIdx.x - batch * a.num_merges];
+  const int64_t groups = (a.n + S::kTiles - 1) / S::kTiles, head = merge.group / groups, first_tile = (merge.group - head * groups) * S::kTiles;
+  const int64_t plane = batch * a.num_heads + head;
+  const ScoreRule rule(a, head);
+  const OwnToken<S, kLine> own(a, batch, first_tile, wave, i);
+  floatx16 sums[2][S::kDBlocks];
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int db = 0; db < S::kDBlocks; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sums[which][db][r] = 0.f;
+  Softmax soft;
+  for (int share = 0; share < merge.shares; ++share) {
+    const floatx4* in = reinterpret_cast<const floatx4*>(share_at<S, K>(a, batch * a.shares + merge.first_share + share, wave));
+    float weight = 1.f;
+    if constexpr (kForward) {
+      const float2 s = reinterpret_cast<const float2*>(in)[lane];
+      const float ref = fmaxf(soft.ref, s.x);
+      const float old = soft.ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2);
+      weight = s.x == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((s.x - ref) * rule.c2);
+      soft.sum = soft.sum * old + s.y * weight;  // (a share without a finite score has no weight, but NaN stays)
+      soft.ref = ref;
+#pragma unroll
+      for (int db = 0; db < S::kDBlocks; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[1][db][r] *= old;
+    }
+    in += 32;
+    auto take = [&](floatx16* to) {
+#pragma unroll
+      for (int j = 0; j < 4 * S::kDBlocks; ++j, in += 64) {
+        const floatx4 v = in[lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[j / 4][j % 4 * 4 + e] = __builtin_fmaf(weight, v[e], to[j / 4][j % 4 * 4 + e]);
+      }
+    };
+    if constexpr (kSum1) take(sums[0]);
+    if constexpr (kSum2) take(sums[1]);
+  }
+  store_results<S, K>(a, rule, plane, own, g, soft, sums[0], sums[1]);
+}
+
+template <class S, bool kLine, ScoredKernel K>
+hipError_t launch_items(const ScoredArgs& a, hipStream_t stream) {
+  const int64_t items = a.batch * a.num_items, merges = a.batch * a.num_merges;
+  if (items < 1 || items > 0x7fffffff) return hipErrorInvalidValue;
+  scored_kernel<S, kLine, K><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
+  if (merges > 0) scored_merge_kernel<S, kLine, K><<<(unsigned)merges, S::kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <ScoredKernel K, int D>
 hipError_t launch_scored(const ScoredArgs& a, hipStream_t stream) {
   if (a.D != D || (a.B != 64 && a.B != 128)) return hipErrorInvalidValue;
-  return a.B == 64 ? launch_shape<K, 64, D>(a, stream) : launch_shape<K, 128, D>(a, stream);
+  if (a.line) return a.B == 64 ? launch_items<ScoredShape<64, D>, true, K>(a, stream) : launch_items<ScoredShape<128, D>, true, K>(a, stream);
+  return a.B == 64 ? launch_items<ScoredShape<64, D>, false, K>(a, stream) : launch_items<ScoredShape<128, D>, false, K>(a, stream);
 }
 
 }  // namespace

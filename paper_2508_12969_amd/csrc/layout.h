@@ -149,13 +149,9 @@ struct DeviceTables {
   int32_t mass_shares = 1;         // workgroups that share the key tiles of a row group
   float* mass_share_stats = nullptr;  // inside the same allocation, as the counter is
   int32_t* mass_counter = nullptr; // its ticket counter
-  // What the gradients of keys and values walk over: for every (head, key tile) the query tiles that keep it, ascending.  In a
-  // block of their own, made at the first backward call.
-  unsigned char* transposed_block = nullptr;
-  int64_t* transposed_row_ptr = nullptr;  // [num_heads*n + 1]
-  int32_t* transposed_meta = nullptr;     // query tile id | its padding class << 24
-  int32_t* transposed_order = nullptr;    // [num_heads*n] launch order
 };
+
+struct ScoredState;
 
 }  // namespace ca
 
@@ -199,6 +195,8 @@ struct ca_layout {
   bool closed_in_place = false, is_closed = false;
   double closed_us = 0;  // predicted time of dense calls, infinite if they are not priced
   mutable std::atomic<uint32_t> launch_seq{0};  // picks the pool counter of a launch
+
+  std::shared_ptr<ca::ScoredState> scored;  // what scored attention walks over (scored.h), made at its first call
 
   // device tables, created once
   std::mutex upload_mutex;

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <mutex>
+#include <vector>
 
 #include "layout.h"
 #include "tokens.h"
@@ -21,15 +23,52 @@ struct TileLine {
 // Rows of `line` per tile, of B words each.
 enum LineRow { kLinePosition = 0, kLineDocument = 1, kLineLimit = 2, kLineRows = 4 };
 
+// The columns of a workgroup are a group: 128 tokens of one head, a tile of 128 or two neighbours of 64.  What they walk over, the union of the tiles' lists
+// (rows of the layout for queries, columns for keys), is a run of words: tile id | padding class << 24 (six bits) | 1 << 30 if the first tile of the group keeps it |
+// 1 << 31 if the second does.  A workgroup takes an item, a group's run or a part of it; where a group has several, each leaves its sums as a share, which
+// a second kernel adds up in their order.
+constexpr int kGroupTokens = 128;
+struct ScoredItem {
+  int64_t first;               // of its words
+  int32_t count, group, share; // share: -1 for a group that is one item
+  int32_t unused;
+};
+struct ScoredMerge {
+  int32_t group, first_share, shares, unused;
+};
+struct ScoredPlan {
+  std::vector<ScoredItem> items;    // longest first
+  std::vector<ScoredMerge> merges;
+  int64_t shares = 0;               // of one batch entry
+  ScoredItem* dev_items = nullptr;
+  ScoredMerge* dev_merges = nullptr;
+};
+struct ScoredWalk {
+  std::vector<uint32_t> words;
+  ScoredPlan plans[2];         // of calls that visit all of a list; of calls whose documents and limits leave out an unknown part of it
+  bool made = false;
+  unsigned char* block = nullptr;  // device memory of all
+  uint32_t* dev_words = nullptr;
+};
+struct ScoredState {
+  std::mutex mutex;
+  ScoredWalk rows, columns;  // of the layout
+  ~ScoredState();
+};
+// Sums of a share, per 32-token wave: (reference, sum) of every lane, and one or two sums of D channels.
+constexpr int64_t share_floats(int64_t D, int sums) { return kGroupTokens / 32 * (2 * 64 + sums * D * 32); }
+
 struct ScoredArgs : GridArgs {
   const void *q, *k, *v, *dout, *o;  // [batch, heads, N_pad, D] tile order, bf16
   void *out, *dq, *dk, *dv;
   const float* lse_in;         // backward: the forward call's
   float* lse;                  // forward: [batch, heads, N_pad]
-  // the walk: for every row (head, tile) the tiles it visits; rows in launch order
-  const int64_t* row_ptr;
-  const int32_t* col_meta;     // tile id | padding class << 24 (bit 31 is not read)
-  const int32_t* order;
+  // the walk, see ScoredWalk
+  const uint32_t* words;
+  const ScoredItem* items;
+  const ScoredMerge* merges;
+  int64_t num_items, num_merges, shares;  // of one batch entry
+  float* share_sums;           // workspace: [batch * shares][sums of a share]
   const int32_t* tile_class;   // [n]
   const SlotMask* class_mask;
   const uint8_t* class_perm;   // [num_classes * 128]
@@ -50,13 +89,16 @@ inline int64_t line_bytes(int64_t batch, int64_t n, int64_t B) { return (batch *
 inline int64_t tile_line_bytes(int64_t batch, int64_t n) { return (batch * n * (int64_t)sizeof(TileLine) + 255) / 256 * 256; }
 inline int64_t row_stat_bytes(int64_t planes, int64_t n, int64_t B) { return planes * n * 2 * B * 4; }
 
+// How many sums a share of the kernel has: dK and dV come from one kernel at head dim 64, from two at 128.
+constexpr int kv_sums(int64_t D) { return D == 64 ? 2 : 1; }
+
 // fills a.line and a.tiles
 hipError_t launch_line(const ScoredArgs& a, hipStream_t stream);
 hipError_t launch_scored_forward(const ScoredArgs& a, hipStream_t stream);
 // fills a.rows
 hipError_t launch_row_stats(const ScoredArgs& a, hipStream_t stream);
 hipError_t launch_scored_dq(const ScoredArgs& a, hipStream_t stream);
-// `a` holds the transposed walk
+// `a` holds the walk over the layout's columns
 hipError_t launch_scored_dkv(const ScoredArgs& a, hipStream_t stream);
 
 }  // namespace ca

@@ -81,13 +81,14 @@ def compact_attn_backward_scored(dout, q, k, v, out, lse, layout, cap=0.0, slope
         _check_tiles(t, layout, name)
     workspace, need = _workspace(layout, scores, 1, q, stream)
     _check(load_library().compact_attn_backward_scored(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), layout.handle, scores,
-                                                       *(t.data_ptr() for t in grads), workspace.data_ptr(), need, _stream_ptr(stream)))
+                                                       *(t.data_ptr() for t in grads), None if workspace is None else workspace.data_ptr(), need, _stream_ptr(stream)))
     return tuple(grads)
 
 
-def compact_attn_layout_upload_backward(layout):
-    """Makes the lists that backward calls read and copies them to the device (the first call does it otherwise, but not under capture)."""
-    _check(load_library().compact_attn_layout_upload_backward(layout.handle))
+def compact_attn_layout_upload_scored(layout, backward=True):
+    """Makes the lists that scored calls walk over (backward: and those of the gradients) and copies them to the device (the first call does it otherwise, but not
+    under capture)."""
+    _check(load_library().compact_attn_layout_upload_scored(layout.handle, int(bool(backward))))
 
 
 def _declare(lib):
@@ -95,7 +96,7 @@ def _declare(lib):
     sc = ctypes.POINTER(ca_scores)
     lib.compact_attn_scored_workspace.argtypes = [vp, sc, ctypes.c_int32, ctypes.POINTER(i64)]
     lib.compact_attn_forward_scored.argtypes = [vp, vp, vp, vp, sc, vp, vp, vp, i64, vp]
-    lib.compact_attn_layout_upload_backward.argtypes = [vp]
+    lib.compact_attn_layout_upload_scored.argtypes = [vp, ctypes.c_int32]
     lib.compact_attn_backward_scored.argtypes = [vp, vp, vp, vp, vp, vp, vp, sc, vp, vp, vp, vp, i64, vp]
 
 

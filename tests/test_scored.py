@@ -376,8 +376,8 @@ def test_backward_lists_must_be_on_the_device_before_a_capture():
             ca.compact_attn_backward_scored(dout, q, k, v, out, lse, pb.layout, grads=grads)
         except ca.CompactAttnError as e:
             refused = e
-    assert refused is not None and refused.status == -1 and "upload_backward" in str(refused)
-    ca.compact_attn_layout_upload_backward(pb.layout)
+    assert refused is not None and refused.status == -1 and "upload_scored" in str(refused)
+    ca.compact_attn_layout_upload_scored(pb.layout)
     with torch.cuda.graph(torch.cuda.CUDAGraph()):
         ca.compact_attn_backward_scored(dout, q, k, v, out, lse, pb.layout, grads=grads)
 
