@@ -20,6 +20,8 @@ using ca::set_error;
 
 namespace {
 
+int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int check_scores(const ca_layout* L, const ca_scores* s) {
@@ -72,9 +74,6 @@ std::vector<Range> token_arrays(const ca_layout* L, const ca_scores* s) {
   return {{s->positions, bytes}, {s->limits, bytes}, {s->documents, bytes}, {s->slopes, (int64_t)L->prob.num_heads * 4}};
 }
 
-// Steps of 64 tokens that a workgroup's other work is worth (start, own tokens, results), and what a share adds; a workgroup's
-// places: two per compute unit.  From launches of one tile length: a row of no steps takes 9 to 11 us, a step 1.3 to 1.7.
-constexpr int64_t kItemSteps = 6, kShareSteps = 4, kMergeSteps = 5, kPlaces = 512;
 constexpr int64_t kMaxScoredShareBytes = (int64_t)128 << 20;
 
 // When the last workgroup ends, in steps, if runs longer than `target` are cut into equal parts of at most that.
@@ -84,11 +83,11 @@ int64_t end_of_launch(const std::vector<int64_t>& costs, int64_t batch, int64_t 
   for (int64_t c : costs) {
     const int64_t parts = std::max<int64_t>(1, (c + target - 1) / target);
     shares = shares || parts > 1;
-    for (int64_t i = 0; i < parts; ++i) pieces.push_back((c + parts - 1) / parts + kItemSteps + (parts > 1 ? kShareSteps : 0));
+    for (int64_t i = 0; i < parts; ++i) pieces.push_back((c + parts - 1) / parts + ca::kItemSteps + (parts > 1 ? ca::kShareSteps : 0));
   }
   std::sort(pieces.begin(), pieces.end(), std::greater<int64_t>());
   std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> places;
-  for (int64_t i = 0; i < kPlaces; ++i) places.push(0);
+  for (int64_t i = 0; i < ca::kPlaces; ++i) places.push(0);
   int64_t end = 0;
   for (int64_t b = 0; b < batch; ++b)
     for (int64_t c : pieces) {
@@ -97,36 +96,32 @@ int64_t end_of_launch(const std::vector<int64_t>& costs, int64_t batch, int64_t 
       places.push(at);
       end = std::max(end, at);
     }
-  return end + (shares ? kMergeSteps : 0);
+  return end + (shares ? ca::kMergeSteps : 0);
 }
 
-// Longest part of a run, in steps: runs are cut where the launch would end with a few long ones, or leave compute units without work.  masked: documents and
-// limits will leave out parts of the runs, which ones is not known here; the longest may stay whole while the others shrink, so runs are cut as if the launch
-// were half as much work.
-int64_t part_steps(const std::vector<int64_t>& costs, int64_t batch, int64_t share_bytes, bool masked) {
+// Longest part of a run, in steps: runs are cut where the launch would end with a few long ones, or leave compute units without work.
+int64_t part_steps(const std::vector<int64_t>& costs, int64_t batch, int64_t share_bytes) {
   const int64_t whole = (int64_t)1 << 40;
   int64_t total = 0;
   for (int64_t c : costs) total += c;
-  if ((int64_t)costs.size() * batch > 16 * kPlaces) return whole;  // (no run is long beside so many)
+  if ((int64_t)costs.size() * batch > 16 * ca::kPlaces) return whole;  // (no run is long beside so many)
   int64_t best = whole, best_end = end_of_launch(costs, batch, whole);
-  const int64_t ideal = std::max<int64_t>(1, total * batch / kPlaces);
-  for (int64_t divisor = masked ? 2 : 1; divisor <= 4; ++divisor) {
-    const int64_t target = std::max<int64_t>(8, (ideal + divisor - 1) / divisor);
+  const int64_t ideal = std::max<int64_t>(1, total * batch / ca::kPlaces);
+  for (int64_t divisor = 1; divisor <= 4; ++divisor) {
+    const int64_t target = std::max(ca::kLeastSteps, (ideal + divisor - 1) / divisor);
     int64_t shares = 0;
     for (int64_t c : costs) shares += c > target ? (c + target - 1) / target : 0;
-    if (shares == 0) break;
     if (shares * batch * share_bytes > kMaxScoredShareBytes) break;
-    if (masked) return target;
     const int64_t end = end_of_launch(costs, batch, target);
     if (20 * end < 19 * best_end) best = target, best_end = end;  // (not for a few per cent)
   }
   return best;
 }
 
-// The lists of the layout's rows (or columns), as groups, and the items of a launch.
+// The lists of the layout's rows (or columns), as runs of groups, and the items of a launch.
 int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
   if (L->class_mask.size() > 32) return fail(CA_ERR_UNSUPPORTED, "too many padding classes for scored attention");
-  const int64_t n = L->n, heads = L->prob.num_heads, rows = heads * n, tiles = ca::kGroupTokens / L->B, groups = (n + tiles - 1) / tiles;
+  const int64_t n = L->n, heads = L->prob.num_heads, rows = heads * n, tiles = ca::kGroupTokens / L->B, per_head = (n + tiles - 1) / tiles, groups = heads * per_head;
   std::vector<int64_t> ptr_t;
   std::vector<int32_t> idx_t;
   if (columns) {
@@ -141,39 +136,43 @@ int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
   }
   const int64_t* const ptr = columns ? ptr_t.data() : L->row_ptr.data();
   const int32_t* const idx = columns ? idx_t.data() : L->col_idx.data();
-  std::vector<int64_t> first(heads * groups + 1, 0), costs(heads * groups);
-  walk.words.reserve(L->col_idx.size());
-  for (int64_t g = 0; g < heads * groups; ++g) {
-    const int64_t row = g / groups * n + g % groups * tiles;
-    const bool second = tiles == 2 && g % groups * tiles + 1 < n;
+  bool has[32][2] = {};  // does half h of a tile of class c hold a token?
+  for (size_t c = 0; c < L->class_mask.size(); ++c)
+    for (int64_t h = 0; h < L->B / 64; ++h) has[c][h] = (L->class_mask[c].w[2 * h] | L->class_mask[c].w[2 * h + 1]) != 0;
+  std::vector<int64_t> costs(groups);
+  walk.first.assign(groups + 1, 0);
+  walk.steps.reserve(L->col_idx.size() * (L->B / 64) / tiles + 2);
+  for (int64_t g = 0; g < groups; ++g) {
+    const int64_t row = g / per_head * n + g % per_head * tiles;
+    const bool second = tiles == 2 && g % per_head * tiles + 1 < n;
     int64_t i = ptr[row], j = second ? ptr[row + 1] : 0;
     const int64_t i_end = ptr[row + 1], j_end = second ? ptr[row + 2] : 0;
     while (i < i_end || j < j_end) {
-      const int32_t a = i < i_end ? idx[i] : INT32_MAX, b = j < j_end ? idx[j] : INT32_MAX, t = std::min(a, b);
-      walk.words.push_back((uint32_t)t | (uint32_t)L->tile_class[t] << 24 | (a == t ? 1u << 30 : 0u) | (b == t ? 1u << 31 : 0u));
+      const int32_t a = i < i_end ? idx[i] : INT32_MAX, b = j < j_end ? idx[j] : INT32_MAX, t = std::min(a, b), cls = L->tile_class[t];
+      for (uint32_t h = 0; h < (uint32_t)(L->B / 64); ++h)
+        if (has[cls][h]) walk.steps.push_back((uint32_t)t | h << 24 | (uint32_t)cls << 25 | (a == t ? 1u << 30 : 0u) | (b == t ? 1u << 31 : 0u));
       i += a == t;
       j += b == t;
     }
-    first[g + 1] = (int64_t)walk.words.size();
-    if (first[g + 1] - first[g] > INT32_MAX / 2) return fail(CA_ERR_UNSUPPORTED, "a list is too long for scored attention");
-    costs[g] = (first[g + 1] - first[g]) * (L->B / 64);
+    walk.first[g + 1] = (int64_t)walk.steps.size();
+    costs[g] = walk.first[g + 1] - walk.first[g];
+    if (costs[g] > INT_MAX / 2) return fail(CA_ERR_UNSUPPORTED, "a list is too long for scored attention");
   }
+  walk.steps.push_back(0);  // the kernels fetch two words ahead
+  walk.steps.push_back(0);
   const int sums = columns ? ca::kv_sums(L->prob.head_dim) : 1;
-  for (int masked = 0; masked < 2; ++masked) {
-    ca::ScoredPlan& plan = walk.plans[masked];
-    const int64_t words_at_once = std::max<int64_t>(1, part_steps(costs, L->prob.batch, ca::share_floats(L->prob.head_dim, sums) * 4, masked) / (L->B / 64));
-    for (int64_t g = 0; g < heads * groups; ++g) {
-      const int64_t count = first[g + 1] - first[g], parts = std::max<int64_t>(1, (count + words_at_once - 1) / words_at_once), size = (count + parts - 1) / parts;
-      if (parts > 1) plan.merges.push_back({(int32_t)g, (int32_t)plan.shares, (int32_t)parts, 0});
-      for (int64_t i = 0; i < parts; ++i) {
-        const int64_t from = std::min(count, i * size), to = std::min(count, from + size);
-        plan.items.push_back({first[g] + from, (int32_t)(to - from), (int32_t)g, parts > 1 ? (int32_t)(plan.shares + i) : -1, 0});
-      }
-      plan.shares += parts > 1 ? parts : 0;
+  const int64_t most = part_steps(costs, L->prob.batch, ca::share_floats(L->prob.head_dim, sums) * 4);
+  for (int64_t g = 0; g < groups; ++g) {
+    const int64_t count = costs[g], parts = std::max<int64_t>(1, (count + most - 1) / most), size = (count + parts - 1) / parts;
+    if (parts > 1) walk.merges.push_back({(int32_t)g, (int32_t)walk.shares, (int32_t)parts, 0});
+    for (int64_t i = 0; i < parts; ++i) {
+      const int64_t from = std::min(count, i * size), to = std::min(count, from + size);
+      walk.items.push_back({walk.first[g] + from, (int32_t)(to - from), (int32_t)g, parts > 1 ? (int32_t)(walk.shares + i) : -1, 0});
     }
-    std::stable_sort(plan.items.begin(), plan.items.end(), [](const ca::ScoredItem& a, const ca::ScoredItem& b) { return a.count > b.count; });
-    if ((int64_t)plan.items.size() * L->prob.batch > 0x7fffffff) return fail(CA_ERR_UNSUPPORTED, "more than 2^31 - 1 workgroups");
+    walk.shares += parts > 1 ? parts : 0;
   }
+  std::stable_sort(walk.items.begin(), walk.items.end(), [](const ca::ScoredItem& a, const ca::ScoredItem& b) { return a.count > b.count; });
+  if (((int64_t)walk.items.size() + ca::kMostShares) * L->prob.batch > INT_MAX) return fail(CA_ERR_UNSUPPORTED, "more than 2^31 - 1 workgroups");
   walk.made = true;
   return CA_OK;
 }
@@ -218,72 +217,114 @@ int upload_walk(ca_layout* L, bool columns, hipStream_t stream, ca::ScoredWalk**
       return fail(CA_ERR_INVALID_ARG, "the lists of scored attention are not on the device yet and the stream is being captured: call compact_attn_layout_upload_scored "
                                       "before the capture");
   }
-  auto padded = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
-  size_t bytes = padded(w.words.size() * sizeof(uint32_t)), at[2][2];
-  for (int i = 0; i < 2; ++i) {
-    at[i][0] = bytes;
-    bytes += padded(w.plans[i].items.size() * sizeof(ca::ScoredItem));
-    at[i][1] = bytes;
-    bytes += padded(w.plans[i].merges.size() * sizeof(ca::ScoredMerge));
-  }
-  void* p = nullptr;
-  hipError_t e = hipMalloc(&p, bytes);
+  struct Part {
+    const void* from;
+    size_t bytes;
+    void** to;
+  };
+  const Part parts[] = {{w.steps.data(), w.steps.size() * sizeof(uint32_t), reinterpret_cast<void**>(&w.dev_steps)},
+                        {w.first.data(), w.first.size() * sizeof(int64_t), reinterpret_cast<void**>(&w.dev_first)},
+                        {w.items.data(), w.items.size() * sizeof(ca::ScoredItem), reinterpret_cast<void**>(&w.dev_items)},
+                        {w.merges.data(), w.merges.size() * sizeof(ca::ScoredMerge), reinterpret_cast<void**>(&w.dev_merges)}};
+  size_t bytes = 0;
+  for (const Part& p : parts) bytes += (size_t)padded256((int64_t)p.bytes);
+  void* block = nullptr;
+  hipError_t e = hipMalloc(&block, bytes);
   if (e != hipSuccess) {
     set_error("hipMalloc of %zu bytes for the lists of scored attention failed: %s", bytes, hipGetErrorString(e));
     (void)hipGetLastError();
     return CA_ERR_ALLOC;
   }
-  unsigned char* const d = static_cast<unsigned char*>(p);
-  auto put = [&](size_t to, const void* from, size_t size) {
-    if (e == hipSuccess && size) e = hipMemcpy(d + to, from, size, hipMemcpyHostToDevice);
-  };
-  put(0, w.words.data(), w.words.size() * sizeof(uint32_t));
-  for (int i = 0; i < 2; ++i) {
-    put(at[i][0], w.plans[i].items.data(), w.plans[i].items.size() * sizeof(ca::ScoredItem));
-    put(at[i][1], w.plans[i].merges.data(), w.plans[i].merges.size() * sizeof(ca::ScoredMerge));
+  unsigned char* at = static_cast<unsigned char*>(block);
+  for (const Part& p : parts) {
+    *p.to = at;
+    if (e == hipSuccess && p.bytes) e = hipMemcpy(at, p.from, p.bytes, hipMemcpyHostToDevice);
+    at += padded256((int64_t)p.bytes);
   }
   if (e != hipSuccess) {
-    (void)hipFree(p);
+    (void)hipFree(block);
     return hip_fail(e, "hipMemcpy of the lists of scored attention");
   }
-  w.dev_words = reinterpret_cast<uint32_t*>(d);
-  for (int i = 0; i < 2; ++i) {
-    w.plans[i].dev_items = reinterpret_cast<ca::ScoredItem*>(d + at[i][0]);
-    w.plans[i].dev_merges = reinterpret_cast<ca::ScoredMerge*>(d + at[i][1]);
-  }
-  w.block = d;
+  w.block = static_cast<unsigned char*>(block);
   return CA_OK;
 }
 
+// Do the arrays hide something, so that runs are made on the device?  (Slopes alone do not.)
 bool is_masked(const ca_scores* s) { return s->limits || s->documents; }
 
-void set_walk(ca::ScoredArgs& a, const ca::ScoredWalk& w, const ca_scores* s) {
-  const ca::ScoredPlan& plan = w.plans[is_masked(s)];
-  a.words = w.dev_words;
-  a.items = plan.dev_items;
-  a.merges = plan.dev_merges;
-  a.num_items = (int64_t)plan.items.size();
-  a.num_merges = (int64_t)plan.merges.size();
-  a.shares = plan.shares;
+// Parts of a call's workspace, in their order.
+struct Workspace {
+  int64_t line = 0, tiles = 0, rows = 0, steps[2] = {0, 0}, counts[2] = {0, 0}, items[2] = {0, 0}, merges[2] = {0, 0}, headers = 0, shares = 0;
+  int64_t bytes() const {
+    int64_t all = line + tiles + rows + headers + shares;
+    for (int i = 0; i < 2; ++i) all += steps[i] + counts[i] + items[i] + merges[i];
+    return all;
+  }
+};
+
+int64_t groups_of(const ca::ScoredWalk& w) { return (int64_t)w.first.size() - 1; }
+
+// Most shares that runs made on the device can have.
+int64_t most_shares(const ca::ScoredWalk& w, int64_t batch) {
+  int64_t all = 0;
+  for (int64_t g = 0; g < groups_of(w) && all < ca::kMostShares; ++g) {
+    const int64_t count = w.first[g + 1] - w.first[g];
+    if (count > ca::kLeastSteps) all += batch * ((count + ca::kLeastSteps - 1) / ca::kLeastSteps);
+  }
+  return std::min(all, ca::kMostShares);
 }
 
-int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-
-// Bytes of a call's workspace: the tokens' line, the row statistics, the shares.
-int workspace_bytes_of(ca_layout* L, const ca_scores* s, bool backward, int64_t* bytes) {
+int workspace_of(ca_layout* L, const ca_scores* s, bool backward, Workspace& w) {
   const ca_problem& p = L->prob;
-  ca::ScoredWalk *rows = nullptr, *columns = nullptr;
-  int st = walk_of(L, false, &rows);
-  if (st == CA_OK && backward) st = walk_of(L, true, &columns);
+  ca::ScoredWalk* walks[2] = {nullptr, nullptr};
+  int st = walk_of(L, false, &walks[0]);
+  if (st == CA_OK && backward) st = walk_of(L, true, &walks[1]);
   if (st != CA_OK) return st;
-  int64_t shares = p.batch * rows->plans[is_masked(s)].shares * ca::share_floats(p.head_dim, 1) * 4;
-  if (backward) shares = std::max(shares, p.batch * columns->plans[is_masked(s)].shares * ca::share_floats(p.head_dim, ca::kv_sums(p.head_dim)) * 4);
-  *bytes = (has_line(s) ? ca::line_bytes(p.batch, L->n, L->B) + ca::tile_line_bytes(p.batch, L->n) : 0) +
-           (backward ? padded256(ca::row_stat_bytes((int64_t)p.batch * p.num_heads, L->n, L->B)) : 0) + shares;
+  if (has_line(s)) {
+    w.line = ca::line_bytes(p.batch, L->n, L->B);
+    w.tiles = ca::tile_line_bytes(p.batch, L->n);
+  }
+  if (backward) w.rows = padded256(ca::row_stat_bytes((int64_t)p.batch * p.num_heads, L->n, L->B));
+  for (int i = 0; i < (backward ? 2 : 1); ++i) {
+    const ca::ScoredWalk& walk = *walks[i];
+    const int64_t groups = groups_of(walk), share_bytes = ca::share_floats(p.head_dim, i == 1 ? ca::kv_sums(p.head_dim) : 1) * 4;
+    if (is_masked(s)) {
+      w.steps[i] = padded256((p.batch * walk.first[groups] + 2) * 4);
+      w.counts[i] = padded256(p.batch * groups * 4);
+      w.items[i] = padded256((p.batch * groups + ca::kMostShares) * (int64_t)sizeof(ca::ScoredItem));
+      w.merges[i] = padded256(ca::kMostMerges * (int64_t)sizeof(ca::ScoredMerge));
+      w.headers = 256;
+      w.shares = std::max(w.shares, padded256(most_shares(walk, p.batch) * share_bytes));
+    } else {
+      w.shares = std::max(w.shares, padded256(p.batch * walk.shares * share_bytes));
+    }
+  }
   return CA_OK;
 }
 
-ca::ScoredArgs scored_args(const ca_layout* L, const ca_scores* s, bool backward, void* workspace) {
+// Where a walk's launches find their items.
+void set_walk(ca::ScoredArgs& a, const ca::ScoredWalk& w) {
+  a.steps = w.dev_steps;
+  a.items = w.dev_items;
+  a.merges = w.dev_merges;
+  a.header = nullptr;
+  a.num_items = (int64_t)w.items.size();
+  a.num_merges = (int64_t)w.merges.size();
+  a.shares = w.shares;
+}
+void set_walk(ca::ScoredArgs& a, const ca::Visits& v) {
+  a.steps = v.steps;
+  a.items = v.items;
+  a.merges = v.merges;
+  a.header = v.header;
+  a.num_items = a.batch * v.groups + ca::kMostShares;
+  a.num_merges = std::min(ca::kMostMerges, a.batch * v.groups);
+  a.shares = 0;
+}
+
+// Arguments of a call's launches; visits: the walks that are made on the device, one or two (0 where none is).
+ca::ScoredArgs scored_args(const ca_layout* L, const ca_scores* s, const Workspace& w, void* workspace, ca::ScoredWalk* const (&walks)[2], ca::Visits (&visits)[2],
+                           int& num_visits) {
   const ca_problem& p = L->prob;
   ca::ScoredArgs a{};
   ca::fill_grid(a, L);
@@ -300,19 +341,39 @@ ca::ScoredArgs scored_args(const ca_layout* L, const ca_scores* s, bool backward
   a.positions = s->positions;
   a.limits = s->limits;
   a.documents = s->documents;
-  unsigned char* w = static_cast<unsigned char*>(workspace);
-  if (has_line(s)) {
-    a.line = reinterpret_cast<float*>(w);
-    w += ca::line_bytes(p.batch, L->n, L->B);
-    a.tiles = reinterpret_cast<ca::TileLine*>(w);
-    w += ca::tile_line_bytes(p.batch, L->n);
+  unsigned char* at = static_cast<unsigned char*>(workspace);
+  auto take = [&](int64_t bytes) {
+    unsigned char* const here = bytes ? at : nullptr;
+    at += bytes;
+    return here;
+  };
+  a.line = reinterpret_cast<float*>(take(w.line));
+  a.tiles = reinterpret_cast<ca::TileLine*>(take(w.tiles));
+  a.rows = reinterpret_cast<float*>(take(w.rows));
+  ca::VisitCounts* const headers = reinterpret_cast<ca::VisitCounts*>(take(w.headers));
+  num_visits = 0;
+  for (int i = 0; i < 2 && walks[i] && headers; ++i) {
+    ca::Visits& v = visits[num_visits++];
+    v.from = walks[i]->dev_steps;
+    v.first = walks[i]->dev_first;
+    v.groups = groups_of(*walks[i]);
+    v.total = walks[i]->first[v.groups];
+    v.keys = i;
+    v.steps = reinterpret_cast<uint32_t*>(take(w.steps[i]));
+    v.counts = reinterpret_cast<int32_t*>(take(w.counts[i]));
+    v.items = reinterpret_cast<ca::ScoredItem*>(take(w.items[i]));
+    v.merges = reinterpret_cast<ca::ScoredMerge*>(take(w.merges[i]));
+    v.header = headers + i;
   }
-  if (backward) {
-    a.rows = reinterpret_cast<float*>(w);
-    w += padded256(ca::row_stat_bytes((int64_t)p.batch * p.num_heads, L->n, L->B));
-  }
-  a.share_sums = reinterpret_cast<float*>(w);
+  a.share_sums = reinterpret_cast<float*>(take(w.shares));
   return a;
+}
+
+// The token arrays in tile order, and the walks that depend on them.
+hipError_t launch_tokens(const ca::ScoredArgs& a, const ca::Visits (&visits)[2], int num_visits, hipStream_t stream) {
+  hipError_t e = a.line ? ca::launch_line(a, stream) : hipSuccess;
+  if (e == hipSuccess && num_visits > 0) e = ca::launch_visits(a, visits, num_visits, stream);
+  return e;
 }
 
 }  // namespace
@@ -328,9 +389,12 @@ int compact_attn_scored_workspace(ca_layout* L, const ca_scores* scores, int32_t
   ca::clear_error();
   if (!workspace_bytes) return fail(CA_ERR_INVALID_ARG, "null argument");
   if (backward != 0 && backward != 1) return fail(CA_ERR_INVALID_ARG, "backward must be 0 or 1");
-  const int st = check_scores(L, scores);
+  int st = check_scores(L, scores);
   if (st != CA_OK) return st;
-  return workspace_bytes_of(L, scores, backward != 0, workspace_bytes);
+  Workspace w;
+  st = workspace_of(L, scores, backward != 0, w);
+  *workspace_bytes = st == CA_OK ? w.bytes() : 0;
+  return st;
 }
 
 int compact_attn_layout_upload_scored(ca_layout* L, int32_t backward) {
@@ -351,9 +415,9 @@ int compact_attn_forward_scored(const void* q, const void* k, const void* v, ca_
   int st = check_scores(L, scores);
   if (st != CA_OK) return st;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(lse)) return fail(CA_ERR_INVALID_ARG, "tensors must be 16-byte aligned, lse 4-byte");
-  int64_t need = 0;
-  const int64_t bytes = ca::tensor_bytes(*L), lse_bytes = bytes / L->prob.head_dim * 2;
-  st = workspace_bytes_of(L, scores, false, &need);
+  Workspace w;
+  st = workspace_of(L, scores, false, w);
+  const int64_t need = w.bytes(), bytes = ca::tensor_bytes(*L), lse_bytes = bytes / L->prob.head_dim * 2;
   if (st == CA_OK) st = check_workspace(workspace, workspace_bytes, need);
   if (st != CA_OK) return st;
   try {
@@ -363,17 +427,19 @@ int compact_attn_forward_scored(const void* q, const void* k, const void* v, ca_
   } catch (const std::bad_alloc&) {
     return fail(CA_ERR_ALLOC, "out of host memory");
   }
-  ca::ScoredWalk* rows = nullptr;
-  if (st == CA_OK) st = upload_walk(L, false, (hipStream_t)stream, &rows);
+  ca::ScoredWalk* walks[2] = {nullptr, nullptr};
+  if (st == CA_OK) st = upload_walk(L, false, (hipStream_t)stream, &walks[0]);
   if (st != CA_OK) return st;
-  ca::ScoredArgs a = scored_args(L, scores, false, workspace);
-  set_walk(a, *rows, scores);
+  ca::Visits visits[2]{};
+  int num_visits = 0;
+  ca::ScoredArgs a = scored_args(L, scores, w, workspace, walks, visits, num_visits);
+  num_visits ? set_walk(a, visits[0]) : set_walk(a, *walks[0]);
   a.q = q;
   a.k = k;
   a.v = v;
   a.out = out;
   a.lse = lse;
-  hipError_t e = a.line ? ca::launch_line(a, (hipStream_t)stream) : hipSuccess;
+  hipError_t e = launch_tokens(a, visits, num_visits, (hipStream_t)stream);
   if (e == hipSuccess) e = ca::launch_scored_forward(a, (hipStream_t)stream);
   return e == hipSuccess ? CA_OK : hip_fail(e, "scored attention launch");
 }
@@ -387,9 +453,9 @@ int compact_attn_backward_scored(const void* dout, const void* q, const void* k,
   for (const void* t : {dout, q, k, v, out, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!aligned16(t)) return fail(CA_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
   if (!aligned4(lse)) return fail(CA_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-  int64_t need = 0;
-  const int64_t bytes = ca::tensor_bytes(*L), lse_bytes = bytes / L->prob.head_dim * 2;
-  st = workspace_bytes_of(L, scores, true, &need);
+  Workspace w;
+  st = workspace_of(L, scores, true, w);
+  const int64_t need = w.bytes(), bytes = ca::tensor_bytes(*L), lse_bytes = bytes / L->prob.head_dim * 2;
   if (st == CA_OK) st = check_workspace(workspace, workspace_bytes, need);
   if (st != CA_OK) return st;
   try {
@@ -400,12 +466,14 @@ int compact_attn_backward_scored(const void* dout, const void* q, const void* k,
   } catch (const std::bad_alloc&) {
     return fail(CA_ERR_ALLOC, "out of host memory");
   }
-  ca::ScoredWalk *rows = nullptr, *columns = nullptr;
-  if (st == CA_OK) st = upload_walk(L, false, (hipStream_t)stream, &rows);
-  if (st == CA_OK) st = upload_walk(L, true, (hipStream_t)stream, &columns);
+  ca::ScoredWalk* walks[2] = {nullptr, nullptr};
+  if (st == CA_OK) st = upload_walk(L, false, (hipStream_t)stream, &walks[0]);
+  if (st == CA_OK) st = upload_walk(L, true, (hipStream_t)stream, &walks[1]);
   if (st != CA_OK) return st;
-  ca::ScoredArgs a = scored_args(L, scores, true, workspace);
-  set_walk(a, *rows, scores);
+  ca::Visits visits[2]{};
+  int num_visits = 0;
+  ca::ScoredArgs a = scored_args(L, scores, w, workspace, walks, visits, num_visits);
+  num_visits ? set_walk(a, visits[0]) : set_walk(a, *walks[0]);
   a.q = q;
   a.k = k;
   a.v = v;
@@ -415,11 +483,11 @@ int compact_attn_backward_scored(const void* dout, const void* q, const void* k,
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  hipError_t e = a.line ? ca::launch_line(a, (hipStream_t)stream) : hipSuccess;
+  hipError_t e = launch_tokens(a, visits, num_visits, (hipStream_t)stream);
   if (e == hipSuccess) e = ca::launch_row_stats(a, (hipStream_t)stream);
   if (e == hipSuccess) e = ca::launch_scored_dq(a, (hipStream_t)stream);
   if (e == hipSuccess) {
-    set_walk(a, *columns, scores);
+    num_visits ? set_walk(a, visits[1]) : set_walk(a, *walks[1]);
     e = ca::launch_scored_dkv(a, (hipStream_t)stream);
   }
   return e == hipSuccess ? CA_OK : hip_fail(e, "scored attention gradient launch");

@@ -16,9 +16,8 @@
 //
 // A step of X and Y is copied straight into LDS while the one before is computed (two buffers, one barrier a step).  Both are read by rows and
 // transposed, so one swizzle of the 16-byte chunks serves both patterns (see swizzle).  What the scores need of the streamed tokens (position, document, limit;
-// log-sum-exp and delta backwards) is copied the same way.  The list of a row is cut into steps up front, 512 tiles at a time, by all threads: steps without a
-// token and, by the tiles' ranges of documents, positions and limits, tiles without a visible pair are left out, and tiles with nothing but visible pairs are marked, so
-// that the others alone compare anything.
+// log-sum-exp and delta backwards) is copied the same way.  Which steps there are is settled before (ScoredWalk): with token arrays, by the tiles' ranges of documents, positions and
+// limits, tiles without a visible pair are left out, and those with nothing but visible pairs are marked, so that the others alone compare anything.
 #pragma once
 
 #include "attn_bf16_common.h"
@@ -43,7 +42,6 @@ struct ScoredShape {
   static constexpr int kLoads = kStepBytes / 1024 / kWaves;  // wave-wide copies of X (and of Y) per wave
   static constexpr int kContraction = D / 16, kDBlocks = D / 32;
   static constexpr int kInfoRows = 6;                // position, document, limit, -, log-sum-exp, delta
-  static constexpr int kListTiles = 512;             // words of a list cut into steps at a time
   static_assert(kLoads == 2 || kLoads == 4, "copies are written for two or four loads");
 };
 
@@ -51,8 +49,6 @@ template <class S>
 struct ScoredLds {
   char x[2][S::kStepBytes], y[2][S::kStepBytes];
   float info[2][S::kInfoRows][S::kStep];
-  uint32_t steps[S::kListTiles * S::kHalves];
-  int counts[S::kWaves];
 };
 
 // Logical 16-byte chunk c of row r lies at physical chunk c ^ swizzle(r).  Read by rows (16 consecutive rows, one logical chunk) the 16 places are
@@ -62,10 +58,9 @@ __device__ __forceinline__ int swizzle(int row) {
   return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-// A word of the step list: tile id, bit 24: which half of it, bits 25 and 26: the tiles of the group that visit it, bits 27-31: its padding class
-// (without arrays), or bits 27 and 28: the tiles of the group that have to compare (with).
 __device__ __forceinline__ int step_tile(uint32_t w) { return (int)(w & 0xffffffu); }
 __device__ __forceinline__ int step_half(uint32_t w) { return (int)(w >> 24) & 1; }
+__device__ __forceinline__ int step_kind(uint32_t w) { return (int)(w >> 25) & 31; }  // padding class; with arrays: 1 to compare
 
 // Copies of a step's X and Y, asynchronous.
 template <class S>
@@ -82,7 +77,7 @@ struct StepCopy {
   __device__ __forceinline__ void tensor(const char* step, uint32_t lds) const {
     const uint32_t slice = (uint32_t)(wave * S::kLoads) * 1024u;
     const char* sb = step + slice;
-    const uint32_t m0 = lds + slice;
+    const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds + slice));
     if constexpr (S::kLoads == 4) {
       asm volatile(
           "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
@@ -109,7 +104,7 @@ struct StepCopy {
     const int r = (wave - first_wave) & (S::kWaves - 1);
     if (r >= rows) return;
     const float* sb = from + r * S::B;
-    const uint32_t off = (uint32_t)lane * 4u, m0 = lds + (uint32_t)(r * S::kStep) * 4u;
+    const uint32_t off = (uint32_t)lane * 4u, m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds + (uint32_t)(r * S::kStep) * 4u));
     asm volatile(
         "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
         "global_load_lds_dword %[v], %[sb] offset:0\n\t"
@@ -118,64 +113,6 @@ struct StepCopy {
         : "memory");
   }
 };
-
-// May any query of q see a key of k?  Does every query that is there see every slot of k?
-__device__ __forceinline__ bool any_visible(const TileLine& q, const TileLine& k) {
-  return q.doc_min <= k.doc_max && k.doc_min <= q.doc_max && k.pos_min <= q.limit_max;
-}
-__device__ __forceinline__ bool all_visible(const TileLine& q, const TileLine& k) {
-  return q.doc_min == q.doc_max && k.doc_min == q.doc_min && k.doc_max == q.doc_min && k.pos_max <= q.limit_min;
-}
-
-// Cuts `count` words of a list into steps; the number of these.  All threads take part.  own: the group's tiles.
-template <class S, bool kLine, ScoredKernel K>
-__device__ __forceinline__ int cut_steps(const ScoredArgs& a, const uint32_t* words, int count, const TileLine (&own)[2], const TileLine* tiles, ScoredLds<S>& lds) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const auto mask = reinterpret_cast<const uint32_t*>(a.class_mask);
-  int total = 0;
-  for (int first = 0; first < count; first += S::kThreads) {
-    bool keep[2] = {false, false};
-    uint32_t word = 0;
-    if (first + tid < count) {
-      const uint32_t w = words[first + tid], tile = w & 0xffffffu, cls = (w >> 24) & 0x3fu;
-      uint32_t member = w >> 30, kind = cls;
-      if constexpr (kLine) {
-        const TileLine other = tiles[tile];
-        kind = 0;
-#pragma unroll
-        for (int t = 0; t < S::kTiles; ++t) {
-          const bool any = owns_keys(K) ? any_visible(other, own[t]) : any_visible(own[t], other);
-          const bool compare = owns_keys(K) ? !all_visible(other, own[t]) : !(other.whole && all_visible(own[t], other));
-          if (!any) member &= ~(1u << t);
-          if (compare) kind |= 1u << t;
-        }
-      }
-      word = tile | member << 25 | kind << 27;
-#pragma unroll
-      for (int h = 0; h < S::kHalves; ++h) {
-        uint32_t valid = 0;
-#pragma unroll
-        for (int b = 0; b < S::kBlocks; ++b) valid |= mask[cls * 4 + h * S::kBlocks + b];
-        keep[h] = valid != 0 && (member & (S::kTiles == 2 ? 3u : 1u)) != 0;
-      }
-    }
-    const uint64_t b0 = __builtin_amdgcn_ballot_w64(keep[0]), b1 = __builtin_amdgcn_ballot_w64(keep[1]);
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    int at = total + __popcll(b0 & below) + __popcll(b1 & below);
-    if (lane == 0) lds.counts[wave] = __popcll(b0) + __popcll(b1);
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < S::kWaves; ++w) {
-      const int c = lds.counts[w];
-      if (w < wave) at += c;
-      total += c;
-    }
-    if (keep[0]) lds.steps[at++] = word;
-    if (keep[1]) lds.steps[at] = word | 1u << 24;
-    __syncthreads();
-  }
-  return __builtin_amdgcn_readfirstlane(total);
-}
 
 // LDS offsets of a lane's operand fragments.
 template <class S>
@@ -293,19 +230,6 @@ __device__ __forceinline__ void load_own(const char* row, int g, bf16x8 (&own)[S
   for (int s = 0; s < S::kContraction; ++s) asm volatile("" : "+v"(own[s]));
 }
 
-template <class S>
-__device__ __forceinline__ void store_columns(char* row, int g, const floatx16 (&acc)[S::kDBlocks], float factor, bool real) {
-#pragma unroll
-  for (int db = 0; db < S::kDBlocks; ++db)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      bf16x4 v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? acc[db][4 * r4 + e] * factor : 0.f);
-      *reinterpret_cast<bf16x4*>(row + (db * 32 + 8 * r4 + 4 * g) * 2) = v;
-    }
-}
-
 // S^T of a block: 32 streamed tokens x the lane's token
 template <class S>
 __device__ __forceinline__ floatx16 block_product(const Fragments<S>& f, LdsTile lds, int block, const bf16x8 (&own)[S::kContraction]) {
@@ -365,22 +289,51 @@ constexpr int sums_of() {
   return K == kScoredDKV ? 2 : 1;
 }
 
-// Writes a token's results; sum1, sum2 as in the kernel.
-template <class S, ScoredKernel K, class Token>
-__device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const Softmax& soft, const floatx16* sum1,
-                                              const floatx16* sum2) {
+// Results of a token: which tensor sum 1 or sum 2 goes to, and the factor.
+template <ScoredKernel K, int kSum>
+__device__ __forceinline__ char* result_of(const ScoredArgs& a) {
+  return static_cast<char*>(K == kScoredForward ? a.out : K == kScoredDQ ? a.dq : kSum == 1 ? a.dk : a.dv);
+}
+__device__ __forceinline__ float log_sum_exp(const ScoreRule& rule, const Softmax& soft, float sum) {
+  return (__builtin_fmaf(soft.ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+template <int kBlocks>
+__device__ __forceinline__ void store_columns(char* row, int g, int first_block, const floatx16* acc, float factor, bool real) {
+#pragma unroll
+  for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? acc[db][4 * r4 + e] * factor : 0.f);
+      *reinterpret_cast<bf16x4*>(row + ((first_block + db) * 32 + 8 * r4 + 4 * g) * 2) = v;
+    }
+}
+// Writes channel blocks first_block .. + kBlocks - 1 of a token's results.
+template <class S, ScoredKernel K, int kBlocks, class Token>
+__device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const Softmax& soft, int first_block,
+                                              const floatx16* sum1, const floatx16* sum2) {
   if (!own.writes) return;
   const int64_t at = (plane * a.n * S::B + own.row) * S::kRowBytes;
-  using Sums = const floatx16(&)[S::kDBlocks];
+  float factor = 1.f;
+  bool real = own.there;
   if constexpr (K == kScoredForward) {
     const float sum = sum_with_partner(soft.sum);
-    const bool empty = !own.there || sum == 0.f;
-    store_columns<S>(static_cast<char*>(a.out) + at, g, reinterpret_cast<Sums>(*sum2), 1.f / sum, !empty);
-    if (g == 0) a.lse[plane * a.n * S::B + own.row] = empty ? kMinusInf : (__builtin_fmaf(soft.ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    real = real && sum != 0.f;
+    factor = 1.f / sum;
+    if (g == 0 && first_block == 0) a.lse[plane * a.n * S::B + own.row] = real ? log_sum_exp(rule, soft, sum) : kMinusInf;
   }
-  if constexpr (K == kScoredDQ) store_columns<S>(static_cast<char*>(a.dq) + at, g, reinterpret_cast<Sums>(*sum1), a.scale, own.there);
-  if constexpr (K == kScoredDK || K == kScoredDKV) store_columns<S>(static_cast<char*>(a.dk) + at, g, reinterpret_cast<Sums>(*sum1), a.scale, own.there);
-  if constexpr (K == kScoredDV || K == kScoredDKV) store_columns<S>(static_cast<char*>(a.dv) + at, g, reinterpret_cast<Sums>(*sum2), 1.f, own.there);
+  if constexpr (K == kScoredDQ || K == kScoredDK || K == kScoredDKV) store_columns<kBlocks>(result_of<K, 1>(a) + at, g, first_block, sum1, a.scale, real);
+  if constexpr (K == kScoredForward || K == kScoredDV || K == kScoredDKV) store_columns<kBlocks>(result_of<K, 2>(a) + at, g, first_block, sum2, factor, real);
+}
+
+// An item, in scalar registers.
+__device__ __forceinline__ ScoredItem item_at(const ScoredItem* p) {
+  const auto w = CONST_PTR(uint32_t, p);
+  uint32_t v[6];
+#pragma unroll
+  for (int i = 0; i < 6; ++i) v[i] = __builtin_amdgcn_readfirstlane(w[i]);
+  return ScoredItem{(int64_t)((uint64_t)v[1] << 32 | v[0]), (int32_t)v[2], (int32_t)v[3], (int32_t)v[4], (int32_t)v[5]};
 }
 
 // A wave's part of a share: floatx4 per lane, lane by lane, so that every store is whole lines.
@@ -396,8 +349,11 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   constexpr bool kSum1 = K == kScoredDQ || K == kScoredDKV || K == kScoredDK, kSum2 = kForward || K == kScoredDKV || K == kScoredDV;
   __shared__ __attribute__((aligned(1024))) ScoredLds<S> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
-  const int64_t linear = xcd_launch_order(blockIdx.x, gridDim.x, xcd_chunk(gridDim.x)), batch = linear / a.num_items;
-  const ScoredItem item = a.items[linear - batch * a.num_items];
+  const int64_t total = a.header ? CONST_PTR(int32_t, &a.header->items)[0] : gridDim.x;
+  if (blockIdx.x >= total) return;  // (all of its threads)
+  const int64_t linear = xcd_launch_order(blockIdx.x, total, xcd_chunk(total)), entry = a.header ? 0 : linear / a.num_items;
+  const ScoredItem item = item_at(a.items + (linear - entry * a.num_items));
+  const int64_t batch = a.header ? item.batch : entry;
   const int64_t groups = (a.n + S::kTiles - 1) / S::kTiles, head = item.group / groups, first_tile = (item.group - head * groups) * S::kTiles;
   const int64_t plane = batch * a.num_heads + head, plane_bytes = a.n * (int64_t)S::B * S::kRowBytes;
   const char* const X = static_cast<const char*>(kKeys ? a.q : a.k) + plane * plane_bytes;
@@ -418,7 +374,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     asm volatile("" : "+v"(own_lse), "+v"(own_delta));
   }
   asm volatile("" : "+v"(own.pos), "+v"(own.limit), "+v"(own.doc));
-  const uint32_t member = 1u << (25 + wave / (S::B / 32)), compares = 1u << (27 + wave / (S::B / 32));  // the wave's tile in a step's word
+  const uint32_t member = 1u << (30 + wave / (S::B / 32));  // the wave's tile in a step's word
 
   floatx16 sum1[kSum1 ? S::kDBlocks : 1], sum2[kSum2 ? S::kDBlocks : 1];
 #pragma unroll
@@ -444,31 +400,23 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     if constexpr (kKeys) copy.words(stats + (int64_t)step_tile(w) * 2 * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes + 4 * S::kStep * 4, 2, 2);
   };
 
-  const TileLine* const tiles = kLine ? a.tiles + batch * a.n : nullptr;
-  TileLine own_tiles[2]{};
-  if constexpr (kLine) {
-    own_tiles[0] = tiles[first_tile];
-    if (S::kTiles == 2 && first_tile + 1 < a.n) own_tiles[1] = tiles[first_tile + 1];  // (else no word names it)
-  }
-  for (int first = 0; first < item.count; first += S::kListTiles) {
-    const int steps = cut_steps<S, kLine, K>(a, a.words + item.first + first, min(S::kListTiles, item.count - first), own_tiles, tiles, lds);
-    if (steps == 0) continue;
-    uint32_t word = __builtin_amdgcn_readfirstlane(lds.steps[0]), next = 0;
-    if (steps > 1) next = __builtin_amdgcn_readfirstlane(lds.steps[1]);
-    issue(word, 0);
-    for (int step = 0; step < steps; ++step) {
+  // words are fetched two steps ahead of their use (the runs are readable two words past their end)
+  const auto words = CONST_PTR(uint32_t, a.steps + item.first);
+  uint32_t word = words[0], next = words[1];
+  if (item.count > 0) issue(word, 0);
+  {
+    for (int step = 0; step < item.count; ++step) {
       const int buffer = step & 1;
-      uint32_t after = 0;
-      if (step + 2 < steps) after = lds.steps[step + 2];
+      const uint32_t after = words[step + 2];
       WAIT_VMCNT(0);
       WAIT_LGKMCNT0();
       BARRIER();  // the step's X and Y are there, and nobody reads the other buffer any more
-      if (step + 1 < steps) issue(next, buffer ^ 1);
+      if (step + 1 < item.count) issue(next, buffer ^ 1);
       if (own.active && (word & member) != 0) {
         const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
         const float(&info)[S::kInfoRows][S::kStep] = lds.info[buffer];
-        const bool compare = kLine && (word & compares) != 0;
-        const int cls = kLine ? 0 : (int)(word >> 27);
+        const bool compare = kLine && step_kind(word) != 0;
+        const int cls = kLine ? 0 : step_kind(word);
         const auto valid = CONST_PTR(uint32_t, a.class_mask) + (cls * 4 + step_half(word) * S::kBlocks);
         if constexpr (kForward) {
           floatx16 s[S::kBlocks], unused;
@@ -556,17 +504,15 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
         }
       }
       word = next;
-      next = __builtin_amdgcn_readfirstlane(after);
+      next = after;
     }
-    WAIT_LGKMCNT0();
-    BARRIER();  // before the list and the buffers are filled again
   }
 
   if (item.share < 0) {
-    store_results<S, K>(a, rule, plane, own, g, soft, sum1, sum2);
+    store_results<S, K, S::kDBlocks>(a, rule, plane, own, g, soft, 0, sum1, sum2);
     return;
   }
-  floatx4* out = reinterpret_cast<floatx4*>(share_at<S, K>(a, batch * a.shares + item.share, wave));
+  floatx4* out = reinterpret_cast<floatx4*>(share_at<S, K>(a, entry * a.shares + item.share, wave));
   reinterpret_cast<float2*>(out)[lane] = float2{soft.ref, soft.sum};
   out += 32;
   auto leave = [&](const floatx16* sums) {
@@ -577,61 +523,68 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   if constexpr (kSum2) leave(sum2);
 }
 
-// Adds up the shares of a group, in their order, and writes its results.  Bound: the shares, once.
+// Adds up the shares of a group, in their order, and writes its results: a workgroup takes 32 tokens, a wave 32 channels of them.  Bound: latency, and the shares
+// once.
 template <class S, bool kLine, ScoredKernel K>
-__global__ __launch_bounds__(S::kThreads) void scored_merge_kernel(ScoredArgs a) {
+__global__ __launch_bounds__(S::kDBlocks * 64) void scored_merge_kernel(ScoredArgs a) {
   constexpr bool kForward = K == kScoredForward, kSum1 = K == kScoredDQ || K == kScoredDKV || K == kScoredDK, kSum2 = kForward || K == kScoredDKV || K == kScoredDV;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
-  const int64_t batch = blockIdx.x / a.num_merges;
-  const ScoredMerge merge = a.merges[blockIdx.x - batch * a.num_merges];
+  constexpr int kAhead = 4;  // shares that are loaded before the first is added
+  const int lane = threadIdx.x & 63, block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
+  const int wave = blockIdx.x % S::kWaves;
+  const int64_t linear = blockIdx.x / S::kWaves, entry = a.header ? 0 : linear / a.num_merges;
+  if (a.header && linear >= CONST_PTR(int32_t, &a.header->merges)[0]) return;
+  const ScoredMerge merge = a.merges[linear - entry * a.num_merges];
+  const int64_t batch = a.header ? merge.batch : entry;
   const int64_t groups = (a.n + S::kTiles - 1) / S::kTiles, head = merge.group / groups, first_tile = (merge.group - head * groups) * S::kTiles;
   const int64_t plane = batch * a.num_heads + head;
   const ScoreRule rule(a, head);
   const OwnToken<S, kLine> own(a, batch, first_tile, wave, i);
-  floatx16 sums[2][S::kDBlocks];
+  floatx16 sum1, sum2;
 #pragma unroll
-  for (int which = 0; which < 2; ++which)
-#pragma unroll
-    for (int db = 0; db < S::kDBlocks; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sums[which][db][r] = 0.f;
+  for (int r = 0; r < 16; ++r) sum1[r] = sum2[r] = 0.f;
   Softmax soft;
-  for (int share = 0; share < merge.shares; ++share) {
-    const floatx4* in = reinterpret_cast<const floatx4*>(share_at<S, K>(a, batch * a.shares + merge.first_share + share, wave));
-    float weight = 1.f;
-    if constexpr (kForward) {
-      const float2 s = reinterpret_cast<const float2*>(in)[lane];
-      const float ref = fmaxf(soft.ref, s.x);
-      const float old = soft.ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2);
-      weight = s.x == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((s.x - ref) * rule.c2);
-      soft.sum = soft.sum * old + s.y * weight;  // (a share without a finite score has no weight, but NaN stays)
-      soft.ref = ref;
+  for (int first = 0; first < merge.shares; first += kAhead) {
+    float2 stats[kAhead];
+    floatx4 part1[kAhead][4], part2[kAhead][4];
 #pragma unroll
-      for (int db = 0; db < S::kDBlocks; ++db)
+    for (int k = 0; k < kAhead; ++k) {
+      if (first + k >= merge.shares) break;
+      const float* in = share_at<S, K>(a, entry * a.shares + merge.first_share + first + k, wave);
+      stats[k] = reinterpret_cast<const float2*>(in)[lane];
+      const floatx4* sums = reinterpret_cast<const floatx4*>(in + 128) + block * 256 + lane;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sums[1][db][r] *= old;
-    }
-    in += 32;
-    auto take = [&](floatx16* to) {
-#pragma unroll
-      for (int j = 0; j < 4 * S::kDBlocks; ++j, in += 64) {
-        const floatx4 v = in[lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) to[j / 4][j % 4 * 4 + e] = __builtin_fmaf(weight, v[e], to[j / 4][j % 4 * 4 + e]);
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (kSum1) part1[k][j] = sums[j * 64];
+        if constexpr (kSum2) part2[k][j] = sums[(kSum1 ? S::kDBlocks * 256 : 0) + j * 64];
       }
-    };
-    if constexpr (kSum1) take(sums[0]);
-    if constexpr (kSum2) take(sums[1]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (first + k >= merge.shares) break;
+      float weight = 1.f, old = 1.f;
+      if constexpr (kForward) {
+        const float ref = fmaxf(soft.ref, stats[k].x);
+        old = soft.ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2);
+        weight = stats[k].x == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((stats[k].x - ref) * rule.c2);
+        soft.sum = soft.sum * old + stats[k].y * weight;  // (a share without a finite score has no weight, but NaN stays)
+        soft.ref = ref;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (kSum1) sum1[r] += part1[k][r / 4][r % 4];
+        if constexpr (kSum2) sum2[r] = __builtin_fmaf(weight, part2[k][r / 4][r % 4], sum2[r] * old);
+      }
+    }
   }
-  store_results<S, K>(a, rule, plane, own, g, soft, sums[0], sums[1]);
+  store_results<S, K, 1>(a, rule, plane, own, g, soft, block, &sum1, &sum2);
 }
 
 template <class S, bool kLine, ScoredKernel K>
 hipError_t launch_items(const ScoredArgs& a, hipStream_t stream) {
-  const int64_t items = a.batch * a.num_items, merges = a.batch * a.num_merges;
+  const int64_t entries = a.header ? 1 : a.batch, items = entries * a.num_items, merges = entries * a.num_merges;
   if (items < 1 || items > 0x7fffffff) return hipErrorInvalidValue;
   scored_kernel<S, kLine, K><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
-  if (merges > 0) scored_merge_kernel<S, kLine, K><<<(unsigned)merges, S::kThreads, 0, stream>>>(a);
+  if (merges > 0) scored_merge_kernel<S, kLine, K><<<(unsigned)(merges * S::kWaves), S::kDBlocks * 64, 0, stream>>>(a);
   return hipGetLastError();
 }
 

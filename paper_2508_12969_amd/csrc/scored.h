@@ -24,39 +24,66 @@ struct TileLine {
 enum LineRow { kLinePosition = 0, kLineDocument = 1, kLineLimit = 2, kLineRows = 4 };
 
 // The columns of a workgroup are a group: 128 tokens of one head, a tile of 128 or two neighbours of 64.  What they walk over, the union of the tiles' lists
-// (rows of the layout for queries, columns for keys), is a run of words: tile id | padding class << 24 (six bits) | 1 << 30 if the first tile of the group keeps it |
-// 1 << 31 if the second does.  A workgroup takes an item, a group's run or a part of it; where a group has several, each leaves its sums as a share, which
-// a second kernel adds up in their order.
+// (rows of the layout for queries, columns for keys), is a run of steps of 64 tokens, one word each: tile id | half of the tile << 24 | its padding class << 25 (five
+// bits) | 1 << 30 if the first tile of the group keeps it | 1 << 31 if the second does.  Halves without a token are left out.
+//
+// Calls whose token arrays hide something are given runs of their own, made on the device from the arrays (visit_kernel): steps without a visible pair are
+// left out, and bit 25 says whether pairs have to be compared, in the place of the class.
+//
+// A workgroup takes an item, a group's run or a part of it; where a group has several, each leaves its sums as a share, which a second kernel adds up in
+// their order.
 constexpr int kGroupTokens = 128;
 struct ScoredItem {
-  int64_t first;               // of its words
+  int64_t first;               // of its steps
   int32_t count, group, share; // share: -1 for a group that is one item
-  int32_t unused;
+  int32_t batch;               // of items made on the device
 };
 struct ScoredMerge {
-  int32_t group, first_share, shares, unused;
-};
-struct ScoredPlan {
-  std::vector<ScoredItem> items;    // longest first
-  std::vector<ScoredMerge> merges;
-  int64_t shares = 0;               // of one batch entry
-  ScoredItem* dev_items = nullptr;
-  ScoredMerge* dev_merges = nullptr;
+  int32_t group, first_share, shares, batch;
 };
 struct ScoredWalk {
-  std::vector<uint32_t> words;
-  ScoredPlan plans[2];         // of calls that visit all of a list; of calls whose documents and limits leave out an unknown part of it
+  std::vector<uint32_t> steps;
+  std::vector<int64_t> first;       // [groups + 1] runs
+  // of calls that visit all of it: one batch entry
+  std::vector<ScoredItem> items;    // longest first
+  std::vector<ScoredMerge> merges;
+  int64_t shares = 0;
   bool made = false;
-  unsigned char* block = nullptr;  // device memory of all
-  uint32_t* dev_words = nullptr;
+  unsigned char* block = nullptr;   // device memory of all
+  uint32_t* dev_steps = nullptr;
+  int64_t* dev_first = nullptr;
+  ScoredItem* dev_items = nullptr;
+  ScoredMerge* dev_merges = nullptr;
 };
 struct ScoredState {
   std::mutex mutex;
   ScoredWalk rows, columns;  // of the layout
   ~ScoredState();
 };
+// Steps of 64 tokens that a workgroup's other work is worth (start, own tokens, results), and what a share adds; a workgroup's places: two per
+// compute unit.  From launches of one run length: a run of no steps takes about 10 us, a step 1.0 to 2.0.
+constexpr int64_t kItemSteps = 6, kShareSteps = 4, kMergeSteps = 4, kPlaces = 512, kLeastSteps = 8;
+// Items made on the device: runs longer than max(kLeastSteps, all steps / kPlaces) are cut, so there are fewer than kPlaces of them and at most twice as many shares.
+constexpr int64_t kMostMerges = kPlaces, kMostShares = 2 * kPlaces;
+
 // Sums of a share, per 32-token wave: (reference, sum) of every lane, and one or two sums of D channels.
 constexpr int64_t share_floats(int64_t D, int sums) { return kGroupTokens / 32 * (2 * 64 + sums * D * 32); }
+
+// Runs and items made on the device, in the workspace.
+struct VisitCounts {
+  int32_t items, merges;
+};
+struct Visits {
+  const uint32_t* from;        // the layout's steps
+  const int64_t* first;        // [groups + 1]
+  int64_t groups, total;       // of a batch entry: groups, steps
+  int32_t keys;                // groups are of keys
+  uint32_t* steps;             // [batch][total]
+  int32_t* counts;             // [batch * groups]
+  ScoredItem* items;           // [batch * groups + kMostShares]
+  ScoredMerge* merges;         // [kMostMerges]
+  VisitCounts* header;
+};
 
 struct ScoredArgs : GridArgs {
   const void *q, *k, *v, *dout, *o;  // [batch, heads, N_pad, D] tile order, bf16
@@ -64,11 +91,12 @@ struct ScoredArgs : GridArgs {
   const float* lse_in;         // backward: the forward call's
   float* lse;                  // forward: [batch, heads, N_pad]
   // the walk, see ScoredWalk
-  const uint32_t* words;
+  const uint32_t* steps;
   const ScoredItem* items;
   const ScoredMerge* merges;
-  int64_t num_items, num_merges, shares;  // of one batch entry
-  float* share_sums;           // workspace: [batch * shares][sums of a share]
+  const VisitCounts* header;   // where items were made on the device: how many there are; else null
+  int64_t num_items, num_merges, shares;  // of one batch entry, or (header) most of all
+  float* share_sums;           // workspace: [shares of all batch entries][sums of a share]
   const int32_t* tile_class;   // [n]
   const SlotMask* class_mask;
   const uint8_t* class_perm;   // [num_classes * 128]
@@ -94,6 +122,8 @@ constexpr int kv_sums(int64_t D) { return D == 64 ? 2 : 1; }
 
 // fills a.line and a.tiles
 hipError_t launch_line(const ScoredArgs& a, hipStream_t stream);
+// makes the runs and items of one or two walks
+hipError_t launch_visits(const ScoredArgs& a, const Visits* visits, int count, hipStream_t stream);
 hipError_t launch_scored_forward(const ScoredArgs& a, hipStream_t stream);
 // fills a.rows
 hipError_t launch_row_stats(const ScoredArgs& a, hipStream_t stream);
