@@ -476,7 +476,7 @@ typedef struct {
 } ca_scores;
 
 /* Bytes of device memory that a forward (backward = 0) or a backward call needs; 0 where it has no use for any: the token arrays in tile order, two floats
- * for a query (backward), and at most 128 MiB for partial sums where long lists are shared by several workgroups.  The first call for a layout makes the
+ * for a query (backward), and at most 140 MB for partial sums where long lists are shared by several workgroups.  The first call for a layout makes the
  * lists that scored attention walks over, on the host. */
 int compact_attn_scored_workspace(ca_layout* layout, const ca_scores* scores, int32_t backward, int64_t* workspace_bytes);
 

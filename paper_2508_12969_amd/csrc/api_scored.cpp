@@ -77,7 +77,7 @@ std::vector<Range> token_arrays(const ca_layout* L, const ca_scores* s) {
 constexpr int64_t kMaxScoredShareBytes = (int64_t)128 << 20;
 
 // When the last workgroup ends, in steps, if runs longer than `target` are cut into equal parts of at most that.
-int64_t end_of_launch(const std::vector<int64_t>& costs, int64_t batch, int64_t target) {
+int64_t end_of_launch(const std::vector<int64_t>& costs, int64_t batch, int64_t places_count, int64_t target) {
   std::vector<int64_t> pieces;
   bool shares = false;
   for (int64_t c : costs) {
@@ -87,7 +87,7 @@ int64_t end_of_launch(const std::vector<int64_t>& costs, int64_t batch, int64_t 
   }
   std::sort(pieces.begin(), pieces.end(), std::greater<int64_t>());
   std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> places;
-  for (int64_t i = 0; i < ca::kPlaces; ++i) places.push(0);
+  for (int64_t i = 0; i < places_count; ++i) places.push(0);
   int64_t end = 0;
   for (int64_t b = 0; b < batch; ++b)
     for (int64_t c : pieces) {
@@ -100,19 +100,19 @@ int64_t end_of_launch(const std::vector<int64_t>& costs, int64_t batch, int64_t 
 }
 
 // Longest part of a run, in steps: runs are cut where the launch would end with a few long ones, or leave compute units without work.
-int64_t part_steps(const std::vector<int64_t>& costs, int64_t batch, int64_t share_bytes) {
+int64_t part_steps(const std::vector<int64_t>& costs, int64_t batch, int64_t places, int64_t share_bytes) {
   const int64_t whole = (int64_t)1 << 40;
   int64_t total = 0;
   for (int64_t c : costs) total += c;
-  if ((int64_t)costs.size() * batch > 16 * ca::kPlaces) return whole;  // (no run is long beside so many)
-  int64_t best = whole, best_end = end_of_launch(costs, batch, whole);
-  const int64_t ideal = std::max<int64_t>(1, total * batch / ca::kPlaces);
+  if ((int64_t)costs.size() * batch > 16 * places) return whole;  // (no run is long beside so many)
+  int64_t best = whole, best_end = end_of_launch(costs, batch, places, whole);
+  const int64_t ideal = std::max<int64_t>(1, total * batch / places);
   for (int64_t divisor = 1; divisor <= 4; ++divisor) {
     const int64_t target = std::max(ca::kLeastSteps, (ideal + divisor - 1) / divisor);
     int64_t shares = 0;
     for (int64_t c : costs) shares += c > target ? (c + target - 1) / target : 0;
     if (shares * batch * share_bytes > kMaxScoredShareBytes) break;
-    const int64_t end = end_of_launch(costs, batch, target);
+    const int64_t end = end_of_launch(costs, batch, places, target);
     if (20 * end < 19 * best_end) best = target, best_end = end;  // (not for a few per cent)
   }
   return best;
@@ -120,7 +120,7 @@ int64_t part_steps(const std::vector<int64_t>& costs, int64_t batch, int64_t sha
 
 // The lists of the layout's rows (or columns), as runs of groups, and the items of a launch.
 int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
-  if (L->class_mask.size() > 32) return fail(CA_ERR_UNSUPPORTED, "too many padding classes for scored attention");
+  if (L->class_mask.size() > 16) return fail(CA_ERR_UNSUPPORTED, "too many padding classes for scored attention");
   const int64_t n = L->n, heads = L->prob.num_heads, rows = heads * n, tiles = ca::kGroupTokens / L->B, per_head = (n + tiles - 1) / tiles, groups = heads * per_head;
   std::vector<int64_t> ptr_t;
   std::vector<int32_t> idx_t;
@@ -136,7 +136,7 @@ int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
   }
   const int64_t* const ptr = columns ? ptr_t.data() : L->row_ptr.data();
   const int32_t* const idx = columns ? idx_t.data() : L->col_idx.data();
-  bool has[32][2] = {};  // does half h of a tile of class c hold a token?
+  bool has[16][2] = {};  // does half h of a tile of class c hold a token?
   for (size_t c = 0; c < L->class_mask.size(); ++c)
     for (int64_t h = 0; h < L->B / 64; ++h) has[c][h] = (L->class_mask[c].w[2 * h] | L->class_mask[c].w[2 * h + 1]) != 0;
   std::vector<int64_t> costs(groups);
@@ -160,8 +160,7 @@ int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
   }
   walk.steps.push_back(0);  // the kernels fetch two words ahead
   walk.steps.push_back(0);
-  const int sums = columns ? ca::kv_sums(L->prob.head_dim) : 1;
-  const int64_t most = part_steps(costs, L->prob.batch, ca::share_floats(L->prob.head_dim, sums) * 4);
+  const int64_t D = L->prob.head_dim, most = part_steps(costs, L->prob.batch, ca::scored_places(D), ca::share_floats(D, columns ? 2 : 1) * 4);
   for (int64_t g = 0; g < groups; ++g) {
     const int64_t count = costs[g], parts = std::max<int64_t>(1, (count + most - 1) / most), size = (count + parts - 1) / parts;
     if (parts > 1) walk.merges.push_back({(int32_t)g, (int32_t)walk.shares, (int32_t)parts, 0});
@@ -172,7 +171,7 @@ int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
     walk.shares += parts > 1 ? parts : 0;
   }
   std::stable_sort(walk.items.begin(), walk.items.end(), [](const ca::ScoredItem& a, const ca::ScoredItem& b) { return a.count > b.count; });
-  if (((int64_t)walk.items.size() + ca::kMostShares) * L->prob.batch > INT_MAX) return fail(CA_ERR_UNSUPPORTED, "more than 2^31 - 1 workgroups");
+  if (((int64_t)walk.items.size() + ca::most_shares(D)) * L->prob.batch > INT_MAX) return fail(CA_ERR_UNSUPPORTED, "more than 2^31 - 1 workgroups");
   walk.made = true;
   return CA_OK;
 }
@@ -265,13 +264,13 @@ struct Workspace {
 int64_t groups_of(const ca::ScoredWalk& w) { return (int64_t)w.first.size() - 1; }
 
 // Most shares that runs made on the device can have.
-int64_t most_shares(const ca::ScoredWalk& w, int64_t batch) {
+int64_t shares_made(const ca::ScoredWalk& w, int64_t batch, int64_t D) {
   int64_t all = 0;
-  for (int64_t g = 0; g < groups_of(w) && all < ca::kMostShares; ++g) {
+  for (int64_t g = 0; g < groups_of(w) && all < ca::most_shares(D); ++g) {
     const int64_t count = w.first[g + 1] - w.first[g];
     if (count > ca::kLeastSteps) all += batch * ((count + ca::kLeastSteps - 1) / ca::kLeastSteps);
   }
-  return std::min(all, ca::kMostShares);
+  return std::min(all, ca::most_shares(D));
 }
 
 int workspace_of(ca_layout* L, const ca_scores* s, bool backward, Workspace& w) {
@@ -287,14 +286,14 @@ int workspace_of(ca_layout* L, const ca_scores* s, bool backward, Workspace& w) 
   if (backward) w.rows = padded256(ca::row_stat_bytes((int64_t)p.batch * p.num_heads, L->n, L->B));
   for (int i = 0; i < (backward ? 2 : 1); ++i) {
     const ca::ScoredWalk& walk = *walks[i];
-    const int64_t groups = groups_of(walk), share_bytes = ca::share_floats(p.head_dim, i == 1 ? ca::kv_sums(p.head_dim) : 1) * 4;
+    const int64_t groups = groups_of(walk), share_bytes = ca::share_floats(p.head_dim, i == 1 ? 2 : 1) * 4;
     if (is_masked(s)) {
       w.steps[i] = padded256((p.batch * walk.first[groups] + 2) * 4);
       w.counts[i] = padded256(p.batch * groups * 4);
-      w.items[i] = padded256((p.batch * groups + ca::kMostShares) * (int64_t)sizeof(ca::ScoredItem));
-      w.merges[i] = padded256(ca::kMostMerges * (int64_t)sizeof(ca::ScoredMerge));
+      w.items[i] = padded256((p.batch * groups + ca::most_shares(p.head_dim)) * (int64_t)sizeof(ca::ScoredItem));
+      w.merges[i] = padded256(ca::most_merges(p.head_dim) * (int64_t)sizeof(ca::ScoredMerge));
       w.headers = 256;
-      w.shares = std::max(w.shares, padded256(most_shares(walk, p.batch) * share_bytes));
+      w.shares = std::max(w.shares, padded256(shares_made(walk, p.batch, p.head_dim) * share_bytes));
     } else {
       w.shares = std::max(w.shares, padded256(p.batch * walk.shares * share_bytes));
     }
@@ -317,8 +316,8 @@ void set_walk(ca::ScoredArgs& a, const ca::Visits& v) {
   a.items = v.items;
   a.merges = v.merges;
   a.header = v.header;
-  a.num_items = a.batch * v.groups + ca::kMostShares;
-  a.num_merges = std::min(ca::kMostMerges, a.batch * v.groups);
+  a.num_items = a.batch * v.groups + ca::most_shares(a.D);
+  a.num_merges = std::min(ca::most_merges(a.D), a.batch * v.groups);
   a.shares = 0;
 }
 

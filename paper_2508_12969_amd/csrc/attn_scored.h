@@ -26,29 +26,34 @@
 namespace ca {
 namespace {
 
-enum ScoredKernel { kScoredForward, kScoredDQ, kScoredDKV, kScoredDK, kScoredDV };
-constexpr bool owns_keys(ScoredKernel k) { return k == kScoredDKV || k == kScoredDK || k == kScoredDV; }
+enum ScoredKernel { kScoredForward, kScoredDQ, kScoredDKV };
 
-template <int B_, int D_>
+// Waves per SIMD that a kernel's registers leave room for.  Head dim 64, measured at 8K and 20K tokens, 12 heads: forward with two / four 311 / 294 and 745 / 664 us;
+// gradients with two and 64-token buffers / three, with half of those and the own operands in LDS 905 / 884 and 2054 / 1986 us.  Head dim 128 has registers for
+// two; the forward kernel with three and 32-token buffers takes the same time (20K tokens in all: the products' power is the limit).
+constexpr int scored_waves(ScoredKernel k, int D) { return D == 128 ? 2 : k == kScoredForward ? 4 : 3; }
+
+template <int B_, int D_, int kStep_ = 64>
 struct ScoredShape {
   static constexpr int B = B_, D = D_;               // B: tokens of a tile
   static constexpr int kWaves = kGroupTokens / 32, kThreads = kWaves * 64;
   static constexpr int kTiles = kGroupTokens / B;    // tiles of a group
-  static constexpr int kStep = 64;                   // streamed tokens of a step
-  static constexpr int kHalves = B / kStep;          // steps of a tile
+  static constexpr int kStep = kStep_;               // streamed tokens in a buffer: a step, or half of one
+  static constexpr int kSubs = 64 / kStep;
   static constexpr int kBlocks = kStep / 32;
   static constexpr int kRowBytes = D * 2, kChunksPerRow = D / 8, kRowsPerLoad = 1024 / kRowBytes;
   static constexpr int kStepBytes = kStep * kRowBytes;
   static constexpr int kLoads = kStepBytes / 1024 / kWaves;  // wave-wide copies of X (and of Y) per wave
   static constexpr int kContraction = D / 16, kDBlocks = D / 32;
   static constexpr int kInfoRows = 6;                // position, document, limit, -, log-sum-exp, delta
-  static_assert(kLoads == 2 || kLoads == 4, "copies are written for two or four loads");
+  static_assert(kLoads == 1 || kLoads == 2 || kLoads == 4, "copies are written for one, two or four loads");
 };
 
-template <class S>
+template <class S, int kOwnSteps>
 struct ScoredLds {
   char x[2][S::kStepBytes], y[2][S::kStepBytes];
-  float info[2][S::kInfoRows][S::kStep];
+  float info[2][S::kInfoRows][64];
+  bf16x8 own[kOwnSteps > 0 ? S::kWaves * kOwnSteps * 64 : 1];  // of the waves' own operands, see OwnOperand
 };
 
 // Logical 16-byte chunk c of row r lies at physical chunk c ^ swizzle(r).  Read by rows (16 consecutive rows, one logical chunk) the 16 places are
@@ -60,7 +65,8 @@ __device__ __forceinline__ int swizzle(int row) {
 
 __device__ __forceinline__ int step_tile(uint32_t w) { return (int)(w & 0xffffffu); }
 __device__ __forceinline__ int step_half(uint32_t w) { return (int)(w >> 24) & 1; }
-__device__ __forceinline__ int step_kind(uint32_t w) { return (int)(w >> 25) & 31; }  // padding class; with arrays: 1 to compare
+__device__ __forceinline__ int step_class(uint32_t w) { return (int)(w >> 25) & 15; }
+constexpr uint32_t kStepCompares = 1u << 29;
 
 // Copies of a step's X and Y, asynchronous.
 template <class S>
@@ -70,7 +76,7 @@ struct StepCopy {
   __device__ __forceinline__ StepCopy(int wave_, int lane_) : wave(wave_), lane(lane_) {
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
-      const int row = i * S::kRowsPerLoad + lane / S::kChunksPerRow, phys = lane % S::kChunksPerRow;  // (the wave's first row is a multiple of 16)
+      const int row = (wave * S::kLoads + i) * S::kRowsPerLoad + lane / S::kChunksPerRow, phys = lane % S::kChunksPerRow;
       voff[i] = (uint32_t)((lane / S::kChunksPerRow) * S::kRowBytes + ((phys ^ swizzle<S::D>(row)) << 4));
     }
   }
@@ -88,7 +94,7 @@ struct StepCopy {
           :
           : [m0] "s"(m0), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [v2] "v"(voff[2]), [v3] "v"(voff[3]), [sb] "s"(sb)
           : "memory");
-    } else {
+    } else if constexpr (S::kLoads == 2) {
       asm volatile(
           "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
           "global_load_lds_dwordx4 %[v0], %[sb] offset:0\n\t"
@@ -96,15 +102,16 @@ struct StepCopy {
           :
           : [m0] "s"(m0), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [sb] "s"(sb)
           : "memory");
+    } else {
+      copy_rows(m0, sb, voff[0]);
     }
   }
-  // `rows` rows of kStep = 64 words, B words apart in memory, one after the other in LDS: row r by wave first_wave + r.
+  // `rows` rows of a step's 64 words, B words apart in memory, one after the other in LDS: row r by wave first_wave + r.
   __device__ __forceinline__ void words(const float* from, uint32_t lds, int rows, int first_wave) const {
-    static_assert(S::kStep == 64, "a row is a wave-wide load");
     const int r = (wave - first_wave) & (S::kWaves - 1);
     if (r >= rows) return;
     const float* sb = from + r * S::B;
-    const uint32_t off = (uint32_t)lane * 4u, m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds + (uint32_t)(r * S::kStep) * 4u));
+    const uint32_t off = (uint32_t)lane * 4u, m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds + (uint32_t)(r * 64) * 4u));
     asm volatile(
         "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
         "global_load_lds_dword %[v], %[sb] offset:0\n\t"
@@ -192,7 +199,7 @@ __device__ __forceinline__ floatx4 read4(const float* row, int block, int i, int
 // Bias and comparison of a block's scores.  own_*: of the lane's token; info: rows of the step's tokens.  own_limit is the lane's where it is a query, the
 // streamed tokens' limits are read where they are.
 template <class S, ScoredKernel K>
-__device__ __forceinline__ void bias_and_compare(const ScoreRule& rule, floatx16& s, const float (&info)[S::kInfoRows][S::kStep], int block, int g, bool compare, float own_pos,
+__device__ __forceinline__ void bias_and_compare(const ScoreRule& rule, floatx16& s, const float (&info)[S::kInfoRows][64], int block, int g, bool compare, float own_pos,
                                                  int own_doc, float own_limit) {
   if (rule.biased)
 #pragma unroll
@@ -204,11 +211,11 @@ __device__ __forceinline__ void bias_and_compare(const ScoreRule& rule, floatx16
   if (compare)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const floatx4 reach = read4(info[owns_keys(K) ? kLineLimit : kLinePosition], block, i, g);
+      const floatx4 reach = read4(info[(K == kScoredDKV) ? kLineLimit : kLinePosition], block, i, g);
       const intx4 doc = __builtin_bit_cast(intx4, read4(info[kLineDocument], block, i, g));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool seen = (int)(owns_keys(K) ? own_pos <= reach[e] : reach[e] <= own_limit) & (int)(doc[e] == own_doc);
+        const bool seen = (int)((K == kScoredDKV) ? own_pos <= reach[e] : reach[e] <= own_limit) & (int)(doc[e] == own_doc);
         s[4 * i + e] = seen ? s[4 * i + e] : kMinusInf;
       }
     }
@@ -221,23 +228,33 @@ __device__ __forceinline__ void rounded(const floatx16& p, bf16x8 (&out)[2]) {
     for (int e = 0; e < 8; ++e) out[t][e] = (__bf16)p[8 * t + e];
 }
 
-template <class S>
-__device__ __forceinline__ void load_own(const char* row, int g, bf16x8 (&own)[S::kContraction]) {
+// A token's own operand: the fragments of its first kInRegisters contraction steps are held in registers, those of the others in LDS, lane by lane (read by the
+// wave that wrote them).
+template <class S, int kInRegisters>
+struct OwnOperand {
+  bf16x8 held[kInRegisters > 0 ? kInRegisters : 1];
+  const bf16x8* rest;
+  __device__ __forceinline__ OwnOperand(const char* row, int g, bf16x8* lds) : rest(lds) {
+    const bf16x8* from = reinterpret_cast<const bf16x8*>(row + g * 16);
 #pragma unroll
-  for (int s = 0; s < S::kContraction; ++s) own[s] = *reinterpret_cast<const bf16x8*>(row + s * 32 + g * 16);
-  // waited for here: in the loop the vector-memory counter belongs to the copies alone
+    for (int s = 0; s < kInRegisters; ++s) held[s] = from[2 * s];
 #pragma unroll
-  for (int s = 0; s < S::kContraction; ++s) asm volatile("" : "+v"(own[s]));
-}
+    for (int s = kInRegisters; s < S::kContraction; ++s) lds[(s - kInRegisters) * 64] = from[2 * s];
+    // waited for here: in the loop the vector-memory counter belongs to the copies alone
+#pragma unroll
+    for (int s = 0; s < kInRegisters; ++s) asm volatile("" : "+v"(held[s]));
+  }
+  __device__ __forceinline__ bf16x8 at(int s) const { return s < kInRegisters ? held[s < kInRegisters ? s : 0] : rest[(s - kInRegisters) * 64]; }
+};
 
 // S^T of a block: 32 streamed tokens x the lane's token
-template <class S>
-__device__ __forceinline__ floatx16 block_product(const Fragments<S>& f, LdsTile lds, int block, const bf16x8 (&own)[S::kContraction]) {
+template <class S, class Own>
+__device__ __forceinline__ floatx16 block_product(const Fragments<S>& f, LdsTile lds, int block, const Own& own) {
   floatx16 acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 #pragma unroll
-  for (int s = 0; s < S::kContraction; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.by_rows(lds, block, s), own[s], acc, 0, 0, 0);
+  for (int s = 0; s < S::kContraction; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.by_rows(lds, block, s), own.at(s), acc, 0, 0, 0);
   return acc;
 }
 
@@ -323,8 +340,8 @@ __device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRu
     factor = 1.f / sum;
     if (g == 0 && first_block == 0) a.lse[plane * a.n * S::B + own.row] = real ? log_sum_exp(rule, soft, sum) : kMinusInf;
   }
-  if constexpr (K == kScoredDQ || K == kScoredDK || K == kScoredDKV) store_columns<kBlocks>(result_of<K, 1>(a) + at, g, first_block, sum1, a.scale, real);
-  if constexpr (K == kScoredForward || K == kScoredDV || K == kScoredDKV) store_columns<kBlocks>(result_of<K, 2>(a) + at, g, first_block, sum2, factor, real);
+  if constexpr (K != kScoredForward) store_columns<kBlocks>(result_of<K, 1>(a) + at, g, first_block, sum1, a.scale, real);
+  if constexpr (K != kScoredDQ) store_columns<kBlocks>(result_of<K, 2>(a) + at, g, first_block, sum2, factor, real);
 }
 
 // An item, in scalar registers.
@@ -344,10 +361,15 @@ __device__ __forceinline__ float* share_at(const ScoredArgs& a, int64_t share, i
 }
 
 template <class S, bool kLine, ScoredKernel K>
-__global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads), amdgpu_waves_per_eu(2, 2))) void scored_kernel(ScoredArgs a) {
-  constexpr bool kForward = K == kScoredForward, kKeys = owns_keys(K);
-  constexpr bool kSum1 = K == kScoredDQ || K == kScoredDKV || K == kScoredDK, kSum2 = kForward || K == kScoredDKV || K == kScoredDV;
-  __shared__ __attribute__((aligned(1024))) ScoredLds<S> lds;
+__global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads), amdgpu_waves_per_eu(scored_waves(K, S::D), scored_waves(K, S::D)))) void scored_kernel(ScoredArgs a) {
+  constexpr bool kForward = K == kScoredForward, kKeys = (K == kScoredDKV);
+  constexpr bool kSum1 = K != kScoredForward, kSum2 = K != kScoredDQ;
+  // dK and dV: their sums and both own operands would be 192 registers at head dim 128, of 256; the value and a part of the key are kept in LDS, as much as two workgroups
+  // of a compute unit have room for (head dim 64: both, for three).  With the value alone there the kernel spills, and takes 1.2 times as long.
+  constexpr bool kTight = K == kScoredDKV;
+  constexpr int kHeld1 = kTight ? (S::D == 128 ? 5 : 0) : S::kContraction, kHeld2 = !kSum1 || kTight ? 0 : S::kContraction;
+  constexpr int kOwnSteps1 = S::kContraction - kHeld1, kOwnSteps2 = kSum1 ? S::kContraction - kHeld2 : 0;
+  __shared__ __attribute__((aligned(1024))) ScoredLds<S, kOwnSteps1 + kOwnSteps2> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   const int64_t total = a.header ? CONST_PTR(int32_t, &a.header->items)[0] : gridDim.x;
   if (blockIdx.x >= total) return;  // (all of its threads)
@@ -364,9 +386,13 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
 
   OwnToken<S, kLine> own(a, batch, first_tile, wave, i);
   float own_lse = 0.f, own_delta = 0.f;
-  bf16x8 own1[S::kContraction], own2[kSum1 ? S::kContraction : 1];
-  load_own<S>(static_cast<const char*>(kKeys ? a.k : a.q) + plane * plane_bytes + own.row * S::kRowBytes, g, own1);
-  if constexpr (kSum1) load_own<S>(static_cast<const char*>(kKeys ? a.v : a.dout) + plane * plane_bytes + own.row * S::kRowBytes, g, own2);
+  bf16x8* const own_lds = lds.own + wave * (kOwnSteps1 + kOwnSteps2) * 64 + lane;
+  const int64_t own_at = plane * plane_bytes + own.row * S::kRowBytes;
+  const OwnOperand<S, kHeld1> own1(static_cast<const char*>(kKeys ? a.k : a.q) + own_at, g, own_lds);
+  const std::conditional_t<kSum1, OwnOperand<S, kHeld2>, int> own2 = [&] {
+    if constexpr (kSum1) return OwnOperand<S, kHeld2>(static_cast<const char*>(kKeys ? a.v : a.dout) + own_at, g, own_lds + kOwnSteps1 * 64);
+    else return 0;
+  }();
   if constexpr (K == kScoredDQ) {
     const float* const t = stats + own.tile * 2 * S::B + (own.row - own.tile * S::B);
     own_lse = t[0];
@@ -391,33 +417,34 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   const Fragments<S> frag(lane);
   const uint32_t lds_x = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.x[0], lds_y = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.y[0];
   const uint32_t lds_info = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.info[0][0];
-  constexpr uint32_t kInfoBytes = S::kInfoRows * S::kStep * 4;
-  auto issue = [&](uint32_t w, int buffer) {
-    const int64_t first = (int64_t)step_tile(w) * S::B + step_half(w) * S::kStep;
+  constexpr uint32_t kInfoBytes = S::kInfoRows * 64 * 4;
+  auto issue = [&](uint32_t w, int sub, int buffer) {
+    const int64_t first = (int64_t)step_tile(w) * S::B + step_half(w) * 64 + sub * S::kStep;
     copy.tensor(X + first * S::kRowBytes, lds_x + buffer * S::kStepBytes);
     copy.tensor(Y + first * S::kRowBytes, lds_y + buffer * S::kStepBytes);
-    if constexpr (kLine) copy.words(line + (int64_t)step_tile(w) * kLineRows * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes, kKeys ? 3 : 2, 0);
-    if constexpr (kKeys) copy.words(stats + (int64_t)step_tile(w) * 2 * S::B + step_half(w) * S::kStep, lds_info + buffer * kInfoBytes + 4 * S::kStep * 4, 2, 2);
+    if (kLine && (rule.biased || (w & kStepCompares) != 0)) copy.words(line + (int64_t)step_tile(w) * kLineRows * S::B + step_half(w) * 64, lds_info + buffer * kInfoBytes, kKeys ? 3 : 2, 0);
+    if constexpr (kKeys) copy.words(stats + (int64_t)step_tile(w) * 2 * S::B + step_half(w) * 64, lds_info + buffer * kInfoBytes + 4 * 64 * 4, 2, 2);
   };
 
   // words are fetched two steps ahead of their use (the runs are readable two words past their end)
   const auto words = CONST_PTR(uint32_t, a.steps + item.first);
-  uint32_t word = words[0], next = words[1];
-  if (item.count > 0) issue(word, 0);
+  const int steps = item.count * S::kSubs;
+  uint32_t word = words[0], next = words[1 / S::kSubs];
+  if (steps > 0) issue(word, 0, 0);
   {
-    for (int step = 0; step < item.count; ++step) {
-      const int buffer = step & 1;
-      const uint32_t after = words[step + 2];
+    for (int step = 0; step < steps; ++step) {
+      const int buffer = step & 1, sub = S::kSubs == 1 ? 0 : step & 1, first_block = sub * S::kBlocks;
+      const uint32_t after = words[(step + 2) / S::kSubs];
       WAIT_VMCNT(0);
       WAIT_LGKMCNT0();
       BARRIER();  // the step's X and Y are there, and nobody reads the other buffer any more
-      if (step + 1 < item.count) issue(next, buffer ^ 1);
+      if (step + 1 < steps) issue(next, S::kSubs == 1 ? 0 : sub ^ 1, buffer ^ 1);
       if (own.active && (word & member) != 0) {
         const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
-        const float(&info)[S::kInfoRows][S::kStep] = lds.info[buffer];
-        const bool compare = kLine && step_kind(word) != 0;
-        const int cls = kLine ? 0 : step_kind(word);
-        const auto valid = CONST_PTR(uint32_t, a.class_mask) + (cls * 4 + step_half(word) * S::kBlocks);
+        const float(&info)[S::kInfoRows][64] = lds.info[buffer];
+        const bool compare = kLine && (word & kStepCompares) != 0;
+        const int cls = compare ? 0 : step_class(word);  // (padding slots have a document of their own)
+        const auto valid = CONST_PTR(uint32_t, a.class_mask) + (cls * 4 + step_half(word) * 2 + first_block);
         if constexpr (kForward) {
           floatx16 s[S::kBlocks], unused;
 #pragma unroll
@@ -425,10 +452,10 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
           if (rule.capped)
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) cap_scores<false>(rule, s[b], unused);
-          if constexpr (kLine) {
+          if constexpr (kLine)
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) bias_and_compare<S, K>(rule, s[b], info, b, g, compare, own.pos, own.doc, own.limit);
-          } else if (cls != 0) {
+            for (int b = 0; b < S::kBlocks; ++b) bias_and_compare<S, K>(rule, s[b], info, first_block + b, g, compare, own.pos, own.doc, own.limit);
+          if (cls != 0) {
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) mask_slots(s[b], __builtin_amdgcn_readfirstlane(valid[b]));
           }
@@ -464,42 +491,36 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
         } else {
 #pragma unroll
           for (int b = 0; b < S::kBlocks; ++b) {
-            floatx16 steep;
+            floatx16 steep, dp;
             floatx16 s = block_product<S>(frag, x, b, own1);
+            if constexpr (kSum1) dp = block_product<S>(frag, y, b, own2);
             if (rule.capped) cap_scores<kSum1>(rule, s, steep);
-            if constexpr (kLine) {
-              bias_and_compare<S, K>(rule, s, info, b, g, compare, own.pos, own.doc, own.limit);
-            } else if (K == kScoredDQ && cls != 0) {
-              mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
-            }
+            if constexpr (kLine) bias_and_compare<S, K>(rule, s, info, first_block + b, g, compare, own.pos, own.doc, own.limit);
+            if (K == kScoredDQ && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               floatx4 lse;
-              if constexpr (kKeys) lse = read4(info[4], b, j, g);
+              if constexpr (kKeys) lse = read4(info[4], first_block + b, j, g);
 #pragma unroll
               for (int e = 0; e < 4; ++e) s[4 * j + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * j + e], rule.c2, -(kKeys ? lse[e] : own_lse)));
             }
-            if constexpr (kSum2) {
-              bf16x8 p[2];
-              rounded(s, p);
-              block_sums<S>(frag, y, b, p, sum2);
-            }
+            bf16x8 p[2], ds[2];
+            if constexpr (kSum2) rounded(s, p);
             if constexpr (kSum1) {
-              const floatx16 dp = block_product<S>(frag, y, b, own2);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                floatx4 delta;
-                if constexpr (kKeys) delta = read4(info[5], b, j, g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[4 * j + e] *= dp[4 * j + e] - (kKeys ? delta[e] : own_delta);
-              }
               if (rule.capped)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] *= steep[r];
-              bf16x8 ds[2];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                floatx4 delta;
+                if constexpr (kKeys) delta = read4(info[5], first_block + b, j, g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[4 * j + e] *= dp[4 * j + e] - (kKeys ? delta[e] : own_delta);
+              }
               rounded(s, ds);
-              block_sums<S>(frag, x, b, ds, sum1);
             }
+            if constexpr (kSum2) block_sums<S>(frag, y, b, p, sum2);
+            if constexpr (kSum1) block_sums<S>(frag, x, b, ds, sum1);
           }
         }
       }
@@ -527,7 +548,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
 // once.
 template <class S, bool kLine, ScoredKernel K>
 __global__ __launch_bounds__(S::kDBlocks * 64) void scored_merge_kernel(ScoredArgs a) {
-  constexpr bool kForward = K == kScoredForward, kSum1 = K == kScoredDQ || K == kScoredDKV || K == kScoredDK, kSum2 = kForward || K == kScoredDKV || K == kScoredDV;
+  constexpr bool kForward = K == kScoredForward, kSum1 = K != kScoredForward, kSum2 = K != kScoredDQ;
   constexpr int kAhead = 4;  // shares that are loaded before the first is added
   const int lane = threadIdx.x & 63, block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   const int wave = blockIdx.x % S::kWaves;
@@ -588,11 +609,11 @@ hipError_t launch_items(const ScoredArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <ScoredKernel K, int D>
+template <ScoredKernel K, int D, int kStep = 64>
 hipError_t launch_scored(const ScoredArgs& a, hipStream_t stream) {
   if (a.D != D || (a.B != 64 && a.B != 128)) return hipErrorInvalidValue;
-  if (a.line) return a.B == 64 ? launch_items<ScoredShape<64, D>, true, K>(a, stream) : launch_items<ScoredShape<128, D>, true, K>(a, stream);
-  return a.B == 64 ? launch_items<ScoredShape<64, D>, false, K>(a, stream) : launch_items<ScoredShape<128, D>, false, K>(a, stream);
+  if (a.line) return a.B == 64 ? launch_items<ScoredShape<64, D, kStep>, true, K>(a, stream) : launch_items<ScoredShape<128, D, kStep>, true, K>(a, stream);
+  return a.B == 64 ? launch_items<ScoredShape<64, D, kStep>, false, K>(a, stream) : launch_items<ScoredShape<128, D, kStep>, false, K>(a, stream);
 }
 
 }  // namespace

@@ -26,7 +26,7 @@ __global__ void line_kernel(ScoredArgs a) {
   out[kLineLimit * a.B] = limit;
   out[3 * a.B] = 0.f;
   const float inf = __builtin_inff();
-  TileLine t{doc >= 0 ? doc : 0x7fffffff, doc >= 0 ? doc : -1, doc >= 0 ? pos : inf, doc >= 0 ? pos : -inf, doc >= 0 ? limit : inf, doc >= 0 ? limit : -inf, doc >= 0, 0};
+  TileLine t{doc >= 0 ? doc : 0x7fffffff, doc >= 0 ? doc : -1, doc >= 0 ? pos : inf, doc >= 0 ? pos : -inf, doc >= 0 ? limit : inf, doc >= 0 ? limit : -inf, k.natural < 0 || doc >= 0, 0};
   for (int step = 1; step < 64; step *= 2) {
     t.doc_min = min(t.doc_min, __shfl_xor(t.doc_min, step));
     t.doc_max = max(t.doc_max, __shfl_xor(t.doc_max, step));
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kVisitThreads) void visit_kernel(ScoredArgs a, Visi
         const bool all = v.keys ? all_visible(other, own[t]) : other.whole && all_visible(own[t], other);
         compare = compare || ((members >> t & 1) != 0 && !all);
       }
-      word = (word & 0x1ffffffu) | (compare ? 1u << 25 : 0u) | members << 30;
+      word = (word & 0x1fffffffu) | (compare ? 1u << 29 : 0u) | members << 30;
     }
     int all;
     const int at = kept + sum_up_to<kVisitThreads>(members != 0, waves, &all) - 1;
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kVisitThreads) void visit_kernel(ScoredArgs a, Visi
 
 // Items of a launch from the runs' lengths, by one workgroup a walk: long runs are cut into equal parts, and items put into the order of their lengths, in 256
 // classes (their order within a class changes nothing but who begins first).  Bound: latency; it reads the lengths three times.
-__global__ __launch_bounds__(kItemThreads) void items_kernel(VisitPair pair, int64_t batch) {
+__global__ __launch_bounds__(kItemThreads) void items_kernel(VisitPair pair, int64_t batch, int places) {
   __shared__ int waves[kItemThreads / 64], longest_shared, bucket[256];
   __shared__ unsigned long long total_shared;
   const Visits v = blockIdx.x ? pair.walk[1] : pair.walk[0];
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kItemThreads) void items_kernel(VisitPair pair, int
   }
   __syncthreads();
   longest = longest_shared;
-  const int64_t ideal = (int64_t)((total_shared + kPlaces - 1) / kPlaces);
+  const int64_t ideal = (int64_t)((total_shared + places - 1) / places);
   // a run may be a tenth longer than an even share of the work before it is worth cutting
   const int target = (int)(10 * (int64_t)longest <= 11 * ideal ? max(longest, 1) : max(kLeastSteps, ideal));
   const int per_class = max(1, (min(longest, target) + 255) / 256);
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kItemThreads) void items_kernel(VisitPair pair, int
   const int mine = tid < 256 ? bucket[tid] : 0, upto = sum_up_to<kItemThreads>(mine, waves, &all);
   if (tid < 256) bucket[tid] = upto - mine;
   if (tid == 0) v.header->items = all;
-  // Shares and merges are numbered in the order of the groups (at most kMostShares and kMostMerges: both fit one sum).
+  // Shares and merges are numbered in the order of the groups (below 2^16 and 2^15: both fit one sum).
   int before = 0;
   for (int64_t first = 0; first < n; first += kItemThreads) {
     const int64_t i = first + tid;
@@ -228,7 +228,7 @@ hipError_t launch_visits(const ScoredArgs& a, const Visits* visits, int count, h
   const VisitPair pair{visits[0], visits[count - 1]};
   if (a.B == 64) visit_kernel<64><<<grid, kVisitThreads, 0, stream>>>(a, pair);
   else visit_kernel<128><<<grid, kVisitThreads, 0, stream>>>(a, pair);
-  items_kernel<<<(unsigned)count, kItemThreads, 0, stream>>>(pair, a.batch);
+  items_kernel<<<(unsigned)count, kItemThreads, 0, stream>>>(pair, a.batch, (int)scored_places(a.D));
   return hipGetLastError();
 }
 

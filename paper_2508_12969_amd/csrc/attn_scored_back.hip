@@ -8,10 +8,7 @@ hipError_t launch_scored_dq(const ScoredArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_scored_dkv(const ScoredArgs& a, hipStream_t stream) {
-  // Head dim 128: the sums of dK and dV and the key's K and V alone are 192 registers, and both in one kernel spill; apart they take one product more.
-  if (a.D == 64) return launch_scored<kScoredDKV, 64>(a, stream);
-  const hipError_t e = launch_scored<kScoredDV, 128>(a, stream);
-  return e == hipSuccess ? launch_scored<kScoredDK, 128>(a, stream) : e;
+  return a.D == 64 ? launch_scored<kScoredDKV, 64, 32>(a, stream) : launch_scored<kScoredDKV, 128, 32>(a, stream);
 }
 
 }  // namespace ca

@@ -16,7 +16,7 @@ namespace ca {
 struct TileLine {
   int32_t doc_min, doc_max;      // min > max: none is there
   float pos_min, pos_max, limit_min, limit_max;
-  int32_t whole;                 // every slot holds one
+  int32_t whole;                 // every token of the grid is there
   int32_t unused;
 };
 
@@ -24,11 +24,11 @@ struct TileLine {
 enum LineRow { kLinePosition = 0, kLineDocument = 1, kLineLimit = 2, kLineRows = 4 };
 
 // The columns of a workgroup are a group: 128 tokens of one head, a tile of 128 or two neighbours of 64.  What they walk over, the union of the tiles' lists
-// (rows of the layout for queries, columns for keys), is a run of steps of 64 tokens, one word each: tile id | half of the tile << 24 | its padding class << 25 (five
-// bits) | 1 << 30 if the first tile of the group keeps it | 1 << 31 if the second does.  Halves without a token are left out.
+// (rows of the layout for queries, columns for keys), is a run of steps of 64 tokens, one word each: tile id | half of the tile << 24 | its padding class << 25 (four
+// bits) | 1 << 29 if pairs have to be compared | 1 << 30 if the first tile of the group keeps it | 1 << 31 if the second does.  Halves without a token are left out.
 //
 // Calls whose token arrays hide something are given runs of their own, made on the device from the arrays (visit_kernel): steps without a visible pair are
-// left out, and bit 25 says whether pairs have to be compared, in the place of the class.
+// left out, and those with nothing but visible pairs of tokens have bit 29 clear.
 //
 // A workgroup takes an item, a group's run or a part of it; where a group has several, each leaves its sums as a share, which a second kernel adds up in
 // their order.
@@ -60,11 +60,14 @@ struct ScoredState {
   ScoredWalk rows, columns;  // of the layout
   ~ScoredState();
 };
-// Steps of 64 tokens that a workgroup's other work is worth (start, own tokens, results), and what a share adds; a workgroup's places: two per
-// compute unit.  From launches of one run length: a run of no steps takes about 10 us, a step 1.0 to 2.0.
-constexpr int64_t kItemSteps = 6, kShareSteps = 4, kMergeSteps = 4, kPlaces = 512, kLeastSteps = 8;
-// Items made on the device: runs longer than max(kLeastSteps, all steps / kPlaces) are cut, so there are fewer than kPlaces of them and at most twice as many shares.
-constexpr int64_t kMostMerges = kPlaces, kMostShares = 2 * kPlaces;
+// Steps of 64 tokens that a workgroup's other work is worth (start, own tokens, results), and what a share adds, from launches of one run length: a run of
+// no steps takes about 10 us, a step 1.0 to 2.0.
+constexpr int64_t kItemSteps = 6, kShareSteps = 4, kMergeSteps = 4, kLeastSteps = 8;
+// Workgroups that the device holds at a time: two per compute unit at head dim 128, three (gradients) or four (forward) at 64.
+constexpr int64_t scored_places(int64_t D) { return D == 64 ? 768 : 512; }
+// Items made on the device: runs longer than max(kLeastSteps, all steps / places) are cut, so there are fewer than `places` of them and at most twice as many shares.
+constexpr int64_t most_merges(int64_t D) { return scored_places(D); }
+constexpr int64_t most_shares(int64_t D) { return 2 * scored_places(D); }
 
 // Sums of a share, per 32-token wave: (reference, sum) of every lane, and one or two sums of D channels.
 constexpr int64_t share_floats(int64_t D, int sums) { return kGroupTokens / 32 * (2 * 64 + sums * D * 32); }
@@ -80,8 +83,8 @@ struct Visits {
   int32_t keys;                // groups are of keys
   uint32_t* steps;             // [batch][total]
   int32_t* counts;             // [batch * groups]
-  ScoredItem* items;           // [batch * groups + kMostShares]
-  ScoredMerge* merges;         // [kMostMerges]
+  ScoredItem* items;           // [batch * groups + most_shares(D)]
+  ScoredMerge* merges;         // [most_merges(D)]
   VisitCounts* header;
 };
 
@@ -116,9 +119,6 @@ struct ScoredArgs : GridArgs {
 inline int64_t line_bytes(int64_t batch, int64_t n, int64_t B) { return (batch * n * kLineRows * B * 4 + 255) / 256 * 256; }
 inline int64_t tile_line_bytes(int64_t batch, int64_t n) { return (batch * n * (int64_t)sizeof(TileLine) + 255) / 256 * 256; }
 inline int64_t row_stat_bytes(int64_t planes, int64_t n, int64_t B) { return planes * n * 2 * B * 4; }
-
-// How many sums a share of the kernel has: dK and dV come from one kernel at head dim 64, from two at 128.
-constexpr int kv_sums(int64_t D) { return D == 64 ? 2 : 1; }
 
 // fills a.line and a.tiles
 hipError_t launch_line(const ScoredArgs& a, hipStream_t stream);
