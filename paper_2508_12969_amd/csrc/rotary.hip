@@ -116,51 +116,81 @@ __device__ __forceinline__ void make_turn(const RowArgs& a, const Part& p, const
   }
 }
 
-// Values of the pairs' other channels in memory (kHalf): a lane whose chunk lies in one half reads the chunk half the rotated channels away, which need
-// not be aligned; one whose chunk holds channels of both, or the end of the second, reads element by element.  Zero where there is no partner.
-enum Partner { kNone, kWhole, kSingle };
+// Pairings: neighbouring channels are in one lane.  Channels half the rotated ones apart are exchanged between the lanes of a row, word by word; where half of
+// them is an odd number of bf16 channels (kApart) they straddle words and are read from memory a second time, one by one.
+enum Pairing { kNeighbours, kHalves, kApart };
+
+typedef __attribute__((ext_vector_type(4))) int intx4;
+
+// Where the partners of a lane's four words are: in word (i + turn) % 4, or where that is odd and the partner lies below, (i - turn) % 4, of lane[i].
 template <class T>
-__device__ __forceinline__ Partner partner_kind(const RowArgs& a, const Part& p) {
-  const int half = a.rotated / 2, last = p.first + Row<T>::kVec;
-  if (!a.angles || p.first >= a.rotated) return kNone;
-  if (last <= half || (p.first >= half && last <= a.rotated)) return kWhole;
-  return kSingle;
-}
+struct Exchange {
+  int turn;           // wave-uniform
+  int lane[4];        // byte address of the lane for ds_bpermute
+  bool below[4], has[4];
+  __device__ __forceinline__ Exchange(const RowArgs& a, const Part& p, int wave_lane) {
+    constexpr int kPerWord = 4 / sizeof(T);
+    const int half = a.rotated / 2 / kPerWord;
+    turn = half & 3;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int word = p.first / kPerWord + i;
+      has[i] = a.angles && word < 2 * half;
+      below[i] = word >= half;
+      const int partner = has[i] ? (below[i] ? word - half : word + half) : word;
+      lane[i] = (((wave_lane >> p.lanes_log2) << p.lanes_log2) + (partner >> 2)) * 4;
+    }
+  }
+  __device__ __forceinline__ typename Row<T>::Chunk operator()(const typename Row<T>::Chunk& own) const {
+    intx4 v = __builtin_bit_cast(intx4, own);
+    if (turn & 1) v = __builtin_shufflevector(v, v, 1, 2, 3, 0);
+    if (turn & 2) v = __builtin_shufflevector(v, v, 2, 3, 0, 1);
+    intx4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      out[i] = __builtin_amdgcn_ds_bpermute(lane[i], v[i]);
+      if (turn & 1) {  // (i - turn) % 4 = (i + turn + 2) % 4
+        const int low = __builtin_amdgcn_ds_bpermute(lane[i], v[(i + 2) & 3]);
+        out[i] = below[i] ? low : out[i];
+      }
+      out[i] = has[i] ? out[i] : 0;
+    }
+    return __builtin_bit_cast(typename Row<T>::Chunk, out);
+  }
+};
+
+// The same from memory, zero where there is no partner.
 template <class T>
-__device__ __forceinline__ typename Row<T>::Chunk load_partner(const RowArgs& a, const Part& p, Partner kind, const T* row) {
+__device__ __forceinline__ typename Row<T>::Chunk load_partner(const RowArgs& a, const Part& p, const T* row) {
   constexpr int kVec = Row<T>::kVec;
   const int half = a.rotated / 2;
   typename Row<T>::Chunk v;
 #pragma unroll
-  for (int e = 0; e < kVec; ++e) v[e] = (T)0.f;
-  if (kind == kWhole) {
-    __builtin_memcpy(&v, row + (p.first < half ? p.first + half : p.first - half), 16);
-  } else if (kind == kSingle) {
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      const int ch = p.first + e;
-      if (ch < a.rotated) v[e] = row[ch < half ? ch + half : ch - half];
-    }
+  for (int e = 0; e < kVec; ++e) {
+    const int ch = p.first + e;
+    v[e] = a.angles && ch < a.rotated ? row[ch < half ? ch + half : ch - half] : (T)0.f;
   }
   return v;
 }
-template <class T>
-__device__ __forceinline__ void load_weights(const RowArgs& a, const Part& p, Partner kind, const void* weight, bool half, float (&w)[Row<T>::kVec], float (&wp)[Row<T>::kVec]) {
+
+template <class T, Pairing kPairing>
+__device__ __forceinline__ void load_weights(const RowArgs& a, const Part& p, const void* weight, float (&w)[Row<T>::kVec], float (&wp)[Row<T>::kVec]) {
   constexpr int kVec = Row<T>::kVec;
 #pragma unroll
   for (int e = 0; e < kVec; ++e) w[e] = wp[e] = 1.f;
   if (!weight) return;
   const T* row = static_cast<const T*>(weight);
   const auto own = *reinterpret_cast<const typename Row<T>::Chunk*>(row + p.first);
-  const auto other = half ? load_partner<T>(a, p, kind, row) : own;
+  typename Row<T>::Chunk other = own;
+  if constexpr (kPairing != kNeighbours) other = load_partner<T>(a, p, row);
 #pragma unroll
-  for (int e = 0; e < kVec; ++e) w[e] = (float)own[e], wp[e] = half ? (float)other[e] : (float)own[e ^ 1];
+  for (int e = 0; e < kVec; ++e) w[e] = (float)own[e], wp[e] = kPairing == kNeighbours ? (float)own[e ^ 1] : (float)other[e];
 }
 
 // Forward calls and the transposed rotation.  Rows are walked in the order of dst; heads are split over blockIdx.y where there are few tokens.
 // kHeads: rows that are loaded before the first of them is computed.  Measured at 75.6K tokens, 40 heads of 128 channels in bf16, q and k:
 // see launch_norm_rotate.
-template <class T, bool kHalf, bool kNorm, bool kBack>
+template <class T, Pairing kPairing, bool kNorm, bool kBack>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_per_block) {
   constexpr int kVec = Row<T>::kVec, kHeads = 4;
   typedef typename Row<T>::Chunk Chunk;
@@ -175,8 +205,8 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
   const int h0 = blockIdx.y * heads_per_block, h1 = min(a.heads, h0 + heads_per_block);
 
   Turn<kVec> turn;
-  make_turn<T, kHalf>(a, p, k, batch, turn);
-  const Partner kind = kHalf ? partner_kind<T>(a, p) : kNone;
+  make_turn<T, kPairing != kNeighbours>(a, p, k, batch, turn);
+  const Exchange<T> exchange(a, p, lane);
   const int64_t src_row = kBack && a.tiled ? k.place : k.natural, dst_row = !kBack && a.tiled ? k.place : k.natural;
 
   for (int tensor = 0; tensor < a.tensors; ++tensor) {
@@ -188,7 +218,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
     for (int e = 0; e < kVec; ++e) own_c[e] = turn.c[e], other_c[e] = turn.s[e];
     if constexpr (kNorm) {
       float w[kVec], wp[kVec];
-      load_weights<T>(a, p, kind, tensor ? a.weight[1] : a.weight[0], kHalf, w, wp);
+      load_weights<T, kPairing>(a, p, tensor ? a.weight[1] : a.weight[0], w, wp);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) own_c[e] *= w[e], other_c[e] *= wp[e];
     }
@@ -199,7 +229,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
         if (h + i < h1 && live && real) {
           const T* r = src + (h + i) * ss.head;
           own[i] = *reinterpret_cast<const Chunk*>(r + p.first);
-          if constexpr (kHalf) other[i] = load_partner<T>(a, p, kind, r);
+          if constexpr (kPairing == kApart) other[i] = load_partner<T>(a, p, r);
         } else {
 #pragma unroll
           for (int e = 0; e < kVec; ++e) own[i][e] = other[i][e] = (T)0.f;
@@ -208,6 +238,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
 #pragma unroll
       for (int i = 0; i < kHeads; ++i) {
         if (h + i >= h1) break;
+        if constexpr (kPairing == kHalves) other[i] = exchange(own[i]);
         float r = 1.f;
         if constexpr (kNorm) {
           float sum = 0.f;
@@ -218,7 +249,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
         Chunk y;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          const float x = (float)own[i][e], xp = kHalf ? (float)other[i][e] : (float)own[i][e ^ 1];
+          const float x = (float)own[i][e], xp = kPairing == kNeighbours ? (float)own[i][e ^ 1] : (float)other[i][e];
           y[e] = (T)(r * (own_c[e] * x + other_c[e] * xp));
         }
         if (!real)
@@ -232,7 +263,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
 
 // Gradients of the norm.  Rows are walked in natural order; a workgroup takes blocks of tokens in turn and adds up its share of the weight
 // gradients in registers, then over its waves in LDS, and leaves it in `partial`.
-template <class T, bool kHalf>
+template <class T, Pairing kPairing>
 __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, int heads_per_block) {
   constexpr int kVec = Row<T>::kVec, kHeads = 2;
   typedef typename Row<T>::Chunk Chunk;
@@ -242,7 +273,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
   const int rows_log2 = 6 - p.lanes_log2;
   const int64_t blocks_per_batch = (a.N_real + (kRowWaves << rows_log2) - 1) / (kRowWaves << rows_log2), blocks = blocks_per_batch * a.batch;
   const int h0 = blockIdx.y * heads_per_block, h1 = min(a.heads, h0 + heads_per_block);
-  const Partner kind = kHalf ? partner_kind<T>(a, p) : kNone;
+  const Exchange<T> exchange(a, p, lane);
   float dw[2][kVec];
 #pragma unroll
   for (int e = 0; e < kVec; ++e) dw[0][e] = dw[1][e] = 0.f;
@@ -252,7 +283,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
     const bool live = p.live && row < a.N_real;
     const Token k = token_of_natural(a, (uint32_t)(row < a.N_real ? row : a.N_real - 1));
     Turn<kVec> turn;
-    make_turn<T, kHalf>(a, p, k, batch, turn);
+    make_turn<T, kPairing != kNeighbours>(a, p, k, batch, turn);
     const int64_t src_row = a.tiled ? k.place : k.natural;
 #pragma unroll
     for (int tensor = 0; tensor < 2; ++tensor) {
@@ -275,7 +306,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
           if (h + i < h1 && live) {
             const T* r = src + (h + i) * ss.head;
             own[i] = *reinterpret_cast<const Chunk*>(r + p.first);
-            if constexpr (kHalf) other[i] = load_partner<T>(a, p, kind, r);
+            if constexpr (kPairing == kApart) other[i] = load_partner<T>(a, p, r);
             x[i] = *reinterpret_cast<const Chunk*>(xin + (h + i) * xs.head);
           } else {
 #pragma unroll
@@ -285,10 +316,11 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
           if (h + i >= h1) break;
+          if constexpr (kPairing == kHalves) other[i] = exchange(own[i]);
           float u[kVec], squares = 0.f, dot = 0.f;
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
-            const float xe = live ? (float)x[i][e] : 0.f, dyp = kHalf ? (float)other[i][e] : (float)own[i][e ^ 1];
+            const float xe = live ? (float)x[i][e] : 0.f, dyp = kPairing == kNeighbours ? (float)own[i][e ^ 1] : (float)other[i][e];
             u[e] = turn.c[e] * (float)own[i][e] + turn.s[e] * dyp;
             squares += xe * xe;
             dot += live ? w[e] * u[e] * xe : 0.f;
@@ -348,6 +380,22 @@ int lanes_log2(const RowArgs& a, bool bf16) {
   return log2;
 }
 
+// launch(element type, pairing) of the kernel that takes a's rows
+template <class Launch>
+void with_pairing(const RowArgs& a, bool bf16, Launch&& launch) {
+  using std::integral_constant;
+  if (!bf16) {
+    if (a.half) launch(float(), integral_constant<Pairing, kHalves>());
+    else launch(float(), integral_constant<Pairing, kNeighbours>());
+  } else if (!a.half) {
+    launch(__bf16(), integral_constant<Pairing, kNeighbours>());
+  } else if (a.rotated / 2 % 2 == 0) {
+    launch(__bf16(), integral_constant<Pairing, kHalves>());
+  } else {
+    launch(__bf16(), integral_constant<Pairing, kApart>());
+  }
+}
+
 // Heads are split over workgroups until there are enough of these to fill the card (2048: eight of four waves on each CU).
 int head_blocks(int64_t workgroups, int heads) {
   int blocks = 1;
@@ -362,13 +410,9 @@ hipError_t launch_rows(const RowArgs& a, bool bf16, hipStream_t stream) {
   int per = (a.heads + head_blocks(blocks * a.batch, a.heads) - 1) / head_blocks(blocks * a.batch, a.heads);
   const dim3 grid((unsigned)blocks, (unsigned)((a.heads + per - 1) / per), (unsigned)a.batch);
   if (grid.y > 65535 || grid.z > 65535) return hipErrorInvalidValue;
-  if (bf16) {
-    if (a.half) rows_kernel<__bf16, true, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
-    else rows_kernel<__bf16, false, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
-  } else {
-    if (a.half) rows_kernel<float, true, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
-    else rows_kernel<float, false, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
-  }
+  with_pairing(a, bf16, [&](auto type, auto pairing) {
+    rows_kernel<decltype(type), decltype(pairing)::value, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
+  });
   return hipGetLastError();
 }
 
@@ -386,13 +430,9 @@ hipError_t launch_norm_rotate_backward(const RowArgs& a, bool bf16, hipStream_t 
   const int split = (int)std::min<int64_t>(head_blocks(blocks, a.heads), std::max<int64_t>(1, kMaxGradientBlocks / std::min<int64_t>(blocks, kMaxGradientBlocks)));
   const int per = (a.heads + split - 1) / split, head_groups = (a.heads + per - 1) / per;
   const dim3 grid((unsigned)std::min<int64_t>(blocks, kMaxGradientBlocks / head_groups), (unsigned)head_groups);
-  if (bf16) {
-    if (a.half) norm_backward_kernel<__bf16, true><<<grid, kRowThreads, 0, stream>>>(a, per);
-    else norm_backward_kernel<__bf16, false><<<grid, kRowThreads, 0, stream>>>(a, per);
-  } else {
-    if (a.half) norm_backward_kernel<float, true><<<grid, kRowThreads, 0, stream>>>(a, per);
-    else norm_backward_kernel<float, false><<<grid, kRowThreads, 0, stream>>>(a, per);
-  }
+  with_pairing(a, bf16, [&](auto type, auto pairing) {
+    norm_backward_kernel<decltype(type), decltype(pairing)::value><<<grid, kRowThreads, 0, stream>>>(a, per);
+  });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.partial) return e;
   weight_gradient_kernel<<<(unsigned)((2 * a.D + 15) / 16), 256, 0, stream>>>(a.partial, (int)(grid.x * grid.y), a.D, a.dweight[0], a.dweight[1]);
