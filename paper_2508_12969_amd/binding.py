@@ -187,6 +187,7 @@ class Layout:
         self._wait = [0, 0]      # calls to be made without after a shortage
         self._without = [0, 0]   # of these, still to be made
         self._calls = None
+        self._scored_workspace = {}   # of scored attention: bytes per kind of call
 
     def _short_of_memory(self, dense):
         """No memory for a workspace.  torch has emptied its cache before it gave up, which not every later call shall pay for again.  Rows

@@ -188,8 +188,9 @@ __device__ __forceinline__ void load_weights(const RowArgs& a, const Part& p, co
 }
 
 // Forward calls and the transposed rotation.  Rows are walked in the order of dst; heads are split over blockIdx.y where there are few tokens.
-// kHeads: rows that are loaded before the first of them is computed.  Measured at 75.6K tokens, 40 heads of 128 channels in bf16, q and k:
-// see launch_norm_rotate.
+// kHeads: rows that are loaded before the first of them is computed (2 / 4 / 8: 20K tokens x 24 rows of 64 channels, forward and gradients 157 / 151 / 149 us; fp32, 7K
+// tokens x 16 rows 30 / 28 / 30 us).  Results are stored past the caches, inputs loaded through them: 33K tokens x 16 heads of 128, bf16, 47 us = 6.3 TB/s, both through them
+// 53, both past them 60; q and k of 75.6K tokens x 40 heads, tokens first, 640 us = 5.0 TB/s (a plain copy of 1 GiB: 4.8 TB/s).
 template <class T, Pairing kPairing, bool kNorm, bool kBack>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_per_block) {
   constexpr int kVec = Row<T>::kVec, kHeads = 4;
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
         if (!real)
 #pragma unroll
           for (int e = 0; e < kVec; ++e) y[e] = (T)0.f;  // (0 * r is NaN where eps is 0)
-        if (live) *reinterpret_cast<Chunk*>(dst + (h + i) * ds.head) = y;
+        if (live) __builtin_nontemporal_store(y, reinterpret_cast<Chunk*>(dst + (h + i) * ds.head));
       }
     }
   }
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
             dx[e] = (T)(r * (w[e] * u[e] - xe * lean));
             dw[tensor][e] += live ? u[e] * xe * r : 0.f;
           }
-          if (live) *reinterpret_cast<Chunk*>(dst + (h + i) * ds.head) = dx;
+          if (live) __builtin_nontemporal_store(dx, reinterpret_cast<Chunk*>(dst + (h + i) * ds.head));
         }
       }
     }
@@ -356,21 +357,22 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
   }
 }
 
-// Adds up the workgroups' shares of the weight gradients: 16 channels a workgroup, 16 threads a channel, always in the same order.
-__global__ __launch_bounds__(256) void weight_gradient_kernel(const float* partial, int blocks, int D, float* dq, float* dk) {
-  __shared__ float sums[16][17];
+// Adds up the workgroups' shares of the weight gradients: 16 channels a workgroup, 64 threads a channel, always in the same order.
+__global__ __launch_bounds__(1024) void weight_gradient_kernel(const float* partial, int blocks, int D, float* dq, float* dk) {
+  __shared__ float sums[64][17];
   const int channel = threadIdx.x & 15, part = threadIdx.x >> 4, c = blockIdx.x * 16 + channel;
   float sum = 0.f;
-  if (c < 2 * D)
-    for (int b = part; b < blocks; b += 16) sum += partial[(int64_t)b * 2 * D + c];
+  if (c < 2 * D) {
+#pragma unroll 8
+    for (int b = part; b < blocks; b += 64) sum += partial[(int64_t)b * 2 * D + c];
+  }
   sums[part][channel] = sum;
   __syncthreads();
-  if (part == 0 && c < 2 * D) {
-    float all = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) all += sums[i][channel];
-    (c < D ? dq[c] : dk[c - D]) = all;
+  for (int half = 32; half > 0; half /= 2) {
+    if (part < half) sums[part][channel] += sums[part + half][channel];
+    __syncthreads();
   }
+  if (part == 0 && c < 2 * D) (c < D ? dq[c] : dk[c - D]) = sums[0][channel];
 }
 
 int lanes_log2(const RowArgs& a, bool bf16) {
@@ -435,7 +437,7 @@ hipError_t launch_norm_rotate_backward(const RowArgs& a, bool bf16, hipStream_t 
   });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.partial) return e;
-  weight_gradient_kernel<<<(unsigned)((2 * a.D + 15) / 16), 256, 0, stream>>>(a.partial, (int)(grid.x * grid.y), a.D, a.dweight[0], a.dweight[1]);
+  weight_gradient_kernel<<<(unsigned)((2 * a.D + 15) / 16), 1024, 0, stream>>>(a.partial, (int)(grid.x * grid.y), a.D, a.dweight[0], a.dweight[1]);
   return hipGetLastError();
 }
 

@@ -91,7 +91,7 @@ def _on_current_device(t, name):
     import torch
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
@@ -112,19 +112,23 @@ def _check_rows(t, layout, padded, name):
 
 
 def _where(layout, origin, positions):
-    if positions is not None:
-        import torch
-        _on_current_device(positions, "positions")
-        expected = (layout.problem.batch, layout.n_tokens_real, 3)
-        if tuple(positions.shape) != expected or positions.dtype != torch.int32 or not positions.is_contiguous():
-            raise ValueError(f"positions must be a contiguous int32 tensor of shape {expected}")
-    return ca_where((ctypes.c_int32 * 3)(*origin), None if positions is None else positions.data_ptr())
+    if positions is None:
+        return None if origin == (0, 0, 0) else ca_where((ctypes.c_int32 * 3)(*origin), None)
+    import torch
+    _on_current_device(positions, "positions")
+    expected = (layout.problem.batch, layout.n_tokens_real, 3)
+    if positions.shape != expected or positions.dtype != torch.int32 or not positions.is_contiguous():
+        raise ValueError(f"positions must be a contiguous int32 tensor of shape {expected}")
+    return ca_where((ctypes.c_int32 * 3)(*origin), positions.data_ptr())
+
+
+_here = contextlib.nullcontext()
 
 
 def _on(stream, device):
     """Where results of a call on `stream` are allocated: from that stream's memory."""
     import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, device))
+    return _here if stream is None else torch.cuda.stream(_torch_stream(stream, device))
 
 
 def compact_attn_rotate(src, layout, rotary, origin=(0, 0, 0), positions=None, tiled=True, transpose=False, out=None, stream=None):
@@ -133,10 +137,12 @@ def compact_attn_rotate(src, layout, rotary, origin=(0, 0, 0), positions=None, t
     tiled, transpose = bool(tiled), bool(transpose)
     padded_in, padded_out = tiled and transpose, tiled and not transpose
     src_strides = _check_rows(src, layout, padded_in, "src")
-    if out is None:
+    dst_strides = None
+    if out is not None:
+        dst_strides = _check_rows(out, layout, padded_out, "out")
+    else:
         with _on(stream, src.device):
             out = src.new_empty(layout.shape(padded_out))
-    dst_strides = _check_rows(out, layout, padded_out, "out")
     where = _where(layout, origin, positions)
     _check(load_library().compact_attn_rotate(src.data_ptr(), src_strides, out.data_ptr(), dst_strides, layout.handle, rotary.handle, where, int(tiled),
                                               int(transpose), _stream_ptr(stream)))
@@ -152,8 +158,9 @@ def _norm(q, k, q_weight, k_weight, layout, rotary, eps, origin, positions, tile
                 raise ValueError(f"{name} must be a contiguous {_torch_dtype(layout)} tensor of {layout.problem.head_dim} elements")
     pointers = [None if s is None else ctypes.pointer(s) for s in strides]
     weights = [None if w is None else w.data_ptr() for w in (q_weight, k_weight)]
-    return ca_norm(q.data_ptr(), k.data_ptr(), *pointers, *weights, None if rotary is None else rotary.handle,
-                   ctypes.pointer(_where(layout, origin, positions)), eps, int(bool(tiled)))
+    where = _where(layout, origin, positions)
+    return ca_norm(q.data_ptr(), k.data_ptr(), *pointers, *weights, None if rotary is None else rotary.handle, None if where is None else ctypes.pointer(where), eps,
+                   int(bool(tiled)))
 
 
 def compact_attn_norm_rotate(q, k, q_weight, k_weight, layout, rotary, eps=1e-6, origin=(0, 0, 0), positions=None, tiled=True, out=None, stream=None):
@@ -163,9 +170,10 @@ def compact_attn_norm_rotate(q, k, q_weight, k_weight, layout, rotary, eps=1e-6,
     if out is None:
         with _on(stream, q.device):
             out = q.new_empty(layout.shape(tiled)), q.new_empty(layout.shape(tiled))
-    for name, t in zip(("q of out", "k of out"), out):
-        if _check_rows(t, layout, bool(tiled), name) is not None:
-            raise ValueError(f"{name} must be contiguous")
+    else:
+        for name, t in zip(("q of out", "k of out"), out, strict=True):
+            if _check_rows(t, layout, bool(tiled), name) is not None:
+                raise ValueError(f"{name} must be contiguous")
     _check(load_library().compact_attn_norm_rotate(norm, out[0].data_ptr(), out[1].data_ptr(), layout.handle, _stream_ptr(stream)))
     return tuple(out)
 
@@ -185,7 +193,7 @@ def compact_attn_norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, 
         if out is None:
             out = torch.empty_like(q), torch.empty_like(k)
         dw = q.new_empty((2, layout.problem.head_dim), dtype=torch.float32) if weighted else None
-    strides = [_check_rows(t, layout, False, name) for name, t in zip(("dq of out", "dk of out"), out)]
+    strides = [_check_rows(t, layout, False, name) for name, t in zip(("dq of out", "dk of out"), out, strict=True)]
     need, workspace = ctypes.c_int64(), None
     if weighted:
         _check(load_library().compact_attn_norm_workspace(layout.handle, need))

@@ -20,7 +20,7 @@ def _scores(layout, cap, slopes, positions, limits, documents):
         if t is None:
             continue
         _on_current_device(t, name)
-        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
     return ca_scores(cap, *(None if t is None else t.data_ptr() for t in (slopes, positions, limits, documents)))
 
@@ -33,19 +33,23 @@ def _check_tiles(t, layout, name):
 def _check_lse(t, layout, name):
     import torch
     _on_current_device(t, name)
-    if tuple(t.shape) != layout.shape(True)[:3] or t.dtype != torch.float32 or not t.is_contiguous():
+    if t.shape != layout.shape(True)[:3] or t.dtype != torch.float32 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape {layout.shape(True)[:3]}")
 
 
 def _workspace(layout, scores, backward, q, stream):
-    need = ctypes.c_int64()
-    _check(load_library().compact_attn_scored_workspace(layout.handle, scores, backward, need))
-    if need.value == 0:
+    kind = backward, bool(scores.slopes), bool(scores.limits or scores.documents)   # all that its size depends on
+    need = layout._scored_workspace.get(kind)
+    if need is None:
+        size = ctypes.c_int64()
+        _check(load_library().compact_attn_scored_workspace(layout.handle, scores, backward, size))
+        need = layout._scored_workspace[kind] = size.value
+    if need == 0:
         return None, 0
-    workspace = _lend(q, need.value, stream)
+    workspace = _lend(q, need, stream)
     if workspace is None or workspace is NotImplemented:
-        raise CompactAttnError(CA_ERR_ALLOC, f"no memory for a workspace of {need.value} bytes, or a capture that torch does not run")
-    return workspace, need.value
+        raise CompactAttnError(CA_ERR_ALLOC, f"no memory for a workspace of {need} bytes, or a capture that torch does not run")
+    return workspace, need
 
 
 def compact_attn_forward_scored(q, k, v, layout, cap=0.0, slopes=None, positions=None, limits=None, documents=None, out=None, stream=None):
@@ -59,8 +63,9 @@ def compact_attn_forward_scored(q, k, v, layout, cap=0.0, slopes=None, positions
         import torch
         with _on(stream, q.device):
             out = q.new_empty(q.shape), q.new_empty(q.shape[:3], dtype=torch.float32)
-    _check_tiles(out[0], layout, "out")
-    _check_lse(out[1], layout, "lse of out")
+    else:
+        _check_tiles(out[0], layout, "out")
+        _check_lse(out[1], layout, "lse of out")
     workspace, need = _workspace(layout, scores, 0, q, stream)
     _check(load_library().compact_attn_forward_scored(q.data_ptr(), k.data_ptr(), v.data_ptr(), layout.handle, scores, out[0].data_ptr(), out[1].data_ptr(),
                                                       None if workspace is None else workspace.data_ptr(), need, _stream_ptr(stream)))
@@ -77,8 +82,9 @@ def compact_attn_backward_scored(dout, q, k, v, out, lse, layout, cap=0.0, slope
     if grads is None:
         with _on(stream, q.device):
             grads = tuple(q.new_empty(q.shape) for _ in range(3))
-    for name, t in zip(("dq", "dk", "dv"), grads):
-        _check_tiles(t, layout, name)
+    else:
+        for name, t in zip(("dq", "dk", "dv"), grads, strict=True):
+            _check_tiles(t, layout, name)
     workspace, need = _workspace(layout, scores, 1, q, stream)
     _check(load_library().compact_attn_backward_scored(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), layout.handle, scores,
                                                        *(t.data_ptr() for t in grads), None if workspace is None else workspace.data_ptr(), need, _stream_ptr(stream)))
