@@ -160,7 +160,7 @@ int make_walk(const ca_layout* L, bool columns, ca::ScoredWalk& walk) {
   }
   walk.steps.push_back(0);  // the kernels fetch two words ahead
   walk.steps.push_back(0);
-  const int64_t D = L->prob.head_dim, most = part_steps(costs, L->prob.batch, ca::scored_places(D), ca::share_floats(D, columns ? 2 : 1) * 4);
+  const int64_t D = L->prob.head_dim, most = part_steps(costs, L->prob.batch, ca::scored_places(D), ca::share_floats(D, 2) * 4);
   for (int64_t g = 0; g < groups; ++g) {
     const int64_t count = costs[g], parts = std::max<int64_t>(1, (count + most - 1) / most), size = (count + parts - 1) / parts;
     if (parts > 1) walk.merges.push_back({(int32_t)g, (int32_t)walk.shares, (int32_t)parts, 0});
@@ -286,7 +286,7 @@ int workspace_of(ca_layout* L, const ca_scores* s, bool backward, Workspace& w) 
   if (backward) w.rows = padded256(ca::row_stat_bytes((int64_t)p.batch * p.num_heads, L->n, L->B));
   for (int i = 0; i < (backward ? 2 : 1); ++i) {
     const ca::ScoredWalk& walk = *walks[i];
-    const int64_t groups = groups_of(walk), share_bytes = ca::share_floats(p.head_dim, i == 1 ? 2 : 1) * 4;
+    const int64_t groups = groups_of(walk), share_bytes = ca::share_floats(p.head_dim, backward ? 2 : 1) * 4;
     if (is_masked(s)) {
       w.steps[i] = padded256((p.batch * walk.first[groups] + 2) * 4);
       w.counts[i] = padded256(p.batch * groups * 4);

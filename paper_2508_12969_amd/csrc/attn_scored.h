@@ -10,7 +10,7 @@
 // weights, rounded to bf16, are register for register the second operand of the products that follow, which read X or Y transposed from LDS:
 //             own         X, Y     S        dP       sums
 //   forward   q           k, v     X q^T    -        O^T  += Y^T P
-//   dQ        q, dO       k, v     X q^T    Y dO^T   dQ^T += X^T dS
+//   dQ        q, dO       k, v     X q^T    Y dO^T   dQ^T += X^T dS,  and X^T P (RowSums)
 //   dK, dV    k, v        q, dO    X k^T    Y v^T    dK^T += X^T dS,  dV^T += Y^T P
 // Sums over tokens are fp32 in the matrix accumulators; weights and dS are rounded to bf16 as their products' operands, as in the other bf16 kernels.
 //
@@ -158,6 +158,7 @@ struct ScoreRule {
   bool capped, biased;
   float bend, c2, offset;
   float slope;           // minus the slope, in units of x per position
+  float slope2;          // the same in powers of two
   __device__ __forceinline__ ScoreRule(const ScoredArgs& a, int64_t head) {
     capped = a.cap > 0.f;
     bend = capped ? 2.f * a.scale * kLog2e / a.cap : 0.f;
@@ -165,17 +166,14 @@ struct ScoreRule {
     offset = capped ? a.cap * kLog2e : 0.f;
     biased = a.slopes != nullptr;
     slope = biased ? -a.slopes[head] / (capped ? 2.f * a.cap : a.scale) : 0.f;
+    slope2 = biased ? -a.slopes[head] * kLog2e : 0.f;
   }
 };
 
-// Caps 16 scores; `steep` receives 1 - tanh^2 = -4 x (1 + x) where the caller wants it.
-template <bool kSteep>
-__device__ __forceinline__ void cap_scores(const ScoreRule& rule, floatx16& s, floatx16& steep) {
+// Caps 16 scores.
+__device__ __forceinline__ void cap_scores(const ScoreRule& rule, floatx16& s) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
-    if constexpr (kSteep) steep[r] = -4.f * __builtin_fmaf(s[r], s[r], s[r]);
-  }
+  for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
 }
 
 // Masks the padding slots of a block of 32 streamed keys (no arrays given), as QueryWave::mask_padding_keys does.
@@ -196,29 +194,31 @@ __device__ __forceinline__ floatx4 read4(const float* row, int block, int i, int
   return *reinterpret_cast<const floatx4*>(row + block * 32 + 8 * i + 4 * g);
 }
 
-// Bias and comparison of a block's scores.  own_*: of the lane's token; info: rows of the step's tokens.  own_limit is the lane's where it is a query, the
-// streamed tokens' limits are read where they are.
+// Bias of a block's scores.  own_pos: of the lane's token; info: rows of the step's tokens.
+template <class S>
+__device__ __forceinline__ void bias_scores(const ScoreRule& rule, floatx16& s, const float (&info)[S::kInfoRows][64], int block, int g, float own_pos) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const floatx4 pos = read4(info[kLinePosition], block, i, g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[4 * i + e] = __builtin_fmaf(__builtin_fabsf(own_pos - pos[e]), rule.slope, s[4 * i + e]);
+  }
+}
+
+// Documents and limits of a block: hidden pairs get minus infinity.  own_limit is the lane's where it is a query; else the streamed tokens' limits are read.
 template <class S, ScoredKernel K>
-__device__ __forceinline__ void bias_and_compare(const ScoreRule& rule, floatx16& s, const float (&info)[S::kInfoRows][64], int block, int g, bool compare, float own_pos,
-                                                 int own_doc, float own_limit) {
-  if (rule.biased)
+__device__ __forceinline__ void hide_scores(floatx16& s, const float (&info)[S::kInfoRows][64], int block, int g, float own_pos, int own_doc, float own_limit) {
+  constexpr bool kKeys = K == kScoredDKV;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 pos = read4(info[kLinePosition], block, i, g);
+  for (int i = 0; i < 4; ++i) {
+    const floatx4 reach = read4(info[kKeys ? kLineLimit : kLinePosition], block, i, g);
+    const intx4 doc = __builtin_bit_cast(intx4, read4(info[kLineDocument], block, i, g));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[4 * i + e] = __builtin_fmaf(__builtin_fabsf(own_pos - pos[e]), rule.slope, s[4 * i + e]);
+    for (int e = 0; e < 4; ++e) {
+      const bool seen = (int)(kKeys ? own_pos <= reach[e] : reach[e] <= own_limit) & (int)(doc[e] == own_doc);
+      s[4 * i + e] = seen ? s[4 * i + e] : kMinusInf;
     }
-  if (compare)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 reach = read4(info[(K == kScoredDKV) ? kLineLimit : kLinePosition], block, i, g);
-      const intx4 doc = __builtin_bit_cast(intx4, read4(info[kLineDocument], block, i, g));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool seen = (int)((K == kScoredDKV) ? own_pos <= reach[e] : reach[e] <= own_limit) & (int)(doc[e] == own_doc);
-        s[4 * i + e] = seen ? s[4 * i + e] : kMinusInf;
-      }
-    }
+  }
 }
 
 __device__ __forceinline__ void rounded(const floatx16& p, bf16x8 (&out)[2]) {
@@ -267,31 +267,67 @@ __device__ __forceinline__ void block_sums(const Fragments<S>& f, LdsTile lds, i
     for (int db = 0; db < S::kDBlocks; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.transposed(lds, block, t, db), w[t], acc[db], 0, 0, 0);
 }
 
+// The same for two sums of the same tensor.
+template <class S>
+__device__ __forceinline__ void block_sums(const Fragments<S>& f, LdsTile lds, int block, const bf16x8 (&w)[2], floatx16 (&acc)[S::kDBlocks], const bf16x8 (&w2)[2],
+                                           floatx16 (&acc2)[S::kDBlocks]) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int db = 0; db < S::kDBlocks; ++db) {
+      const bf16x8 v = f.transposed(lds, block, t, db);
+      acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[t], acc[db], 0, 0, 0);
+      acc2[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w2[t], acc2[db], 0, 0, 0);
+    }
+}
+
+__device__ __forceinline__ float sum_of_rounded(const bf16x8 (&w)[2], float sum) {
+  bf16x2 ones;
+  ones[0] = ones[1] = (__bf16)1.0f;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w[t], w[t], 0, 1), ones, sum, false);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w[t], w[t], 2, 3), ones, sum, false);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w[t], w[t], 4, 5), ones, sum, false);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w[t], w[t], 6, 7), ones, sum, false);
+  }
+  return sum;
+}
+
 // The softmax state of the lane's query: see QueryWave::softmax for the lagging reference.  The row sum adds up the weights before they
 // are rounded, because the log-sum-exp is an output of its own (a sum of rounded weights is off by up to 2^-8 where a row has few keys).
 struct Softmax {
   float ref = kMinusInf, sum = 0.f;  // reference in units of x; this lane's share of the sum
 };
 
+// What the lane's query of dQ adds up besides, over its share of the keys.  delta comes from the rounded result, and dS is rounded as an operand; both shift all of
+// a row's dS the same way, and such a shift meets the weighted mean of the keys, which is not small.  In exact arithmetic P (dP - delta) sums to zero over a row, and so the
+// row's sums say what the shift is: `lean` is by how much delta is off, `excess` what rounding added.  dQ is put right at the end by as much of
+// sum2 = sum of (P steep) K, and delta by lean, for dK.  (Relative error of dQ / dK at scores of a spread of 3: 3.6e-3 / 2.7e-3 without, 2.2e-3 / 2.2e-3 with, of which 1.7e-3 is the
+// rounding of the result.  It is one product more, of seven: 36K tokens, dense, forwards not counted, 17.0 / 18.4 ms at head dim 128 and 9.0 / 10.3 at 64.)
+struct RowSums {
+  float lean = 0.f, excess = 0.f, weight = 0.f;  // sums of P (dP - delta), of dS rounded less dS, of P steep; without a cap dS sums to lean, which is not taken off, and the weight is 1
+};
+
 // The lane's token, and what becomes of its sums.
 template <class S, bool kLine>
 struct OwnToken {
-  int64_t tile, row;    // row: in the plane
+  int32_t tile, row;    // row: in the plane
   bool active, there;   // the wave has tokens at all; the token is in the grid and has a document that is not negative
   bool writes;          // it has a row
   float pos = 0.f, limit = __builtin_inff();
   int doc = 0;
   __device__ __forceinline__ OwnToken(const ScoredArgs& a, int64_t batch, int64_t first_tile, int wave, int i) {
     constexpr int kWavesPerTile = S::B / 32;
-    tile = first_tile + wave / kWavesPerTile;
+    tile = (int32_t)first_tile + wave / kWavesPerTile;
     writes = tile < a.n;
-    if (!writes) tile = a.n - 1;
+    if (!writes) tile = (int32_t)a.n - 1;
     const QuerySlot slot = query_slot<S::B>(a, tile, wave % kWavesPerTile * 32, i);
     active = slot.wave_active && writes;
     row = tile * S::B + slot.slot;
     there = slot.real && writes;
     if constexpr (kLine) {
-      const float* t = a.line + (batch * a.n + tile) * kLineRows * S::B + slot.slot;
+      const float* t = a.line + ((batch * a.n + tile) * kLineRows * S::B + slot.slot);
       pos = t[kLinePosition * S::B];
       limit = t[kLineLimit * S::B];
       doc = __builtin_bit_cast(int, t[kLineDocument * S::B]);
@@ -303,14 +339,9 @@ struct OwnToken {
 
 template <class S, ScoredKernel K>
 constexpr int sums_of() {
-  return K == kScoredDKV ? 2 : 1;
+  return K == kScoredForward ? 1 : 2;
 }
 
-// Results of a token: which tensor sum 1 or sum 2 goes to, and the factor.
-template <ScoredKernel K, int kSum>
-__device__ __forceinline__ char* result_of(const ScoredArgs& a) {
-  return static_cast<char*>(K == kScoredForward ? a.out : K == kScoredDQ ? a.dq : kSum == 1 ? a.dk : a.dv);
-}
 __device__ __forceinline__ float log_sum_exp(const ScoreRule& rule, const Softmax& soft, float sum) {
   return (__builtin_fmaf(soft.ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
@@ -326,22 +357,34 @@ __device__ __forceinline__ void store_columns(char* row, int g, int first_block,
       *reinterpret_cast<bf16x4*>(row + ((first_block + db) * 32 + 8 * r4 + 4 * g) * 2) = v;
     }
 }
-// Writes channel blocks first_block .. + kBlocks - 1 of a token's results.
-template <class S, ScoredKernel K, int kBlocks, class Token>
-__device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const Softmax& soft, int first_block,
-                                              const floatx16* sum1, const floatx16* sum2) {
+// Writes channel blocks first_block .. + kBlocks - 1 of a token's results.  state: Softmax (forward) or RowSums (dQ).
+template <class S, ScoredKernel K, int kBlocks, class Token, class State>
+__device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const State& state, int first_block,
+                                              floatx16* sum1, const floatx16* sum2) {
   if (!own.writes) return;
   const int64_t at = (plane * a.n * S::B + own.row) * S::kRowBytes;
-  float factor = 1.f;
-  bool real = own.there;
   if constexpr (K == kScoredForward) {
-    const float sum = sum_with_partner(soft.sum);
-    real = real && sum != 0.f;
-    factor = 1.f / sum;
-    if (g == 0 && first_block == 0) a.lse[plane * a.n * S::B + own.row] = real ? log_sum_exp(rule, soft, sum) : kMinusInf;
+    const float sum = sum_with_partner(state.sum);
+    const bool real = own.there && sum != 0.f;
+    if (g == 0 && first_block == 0) a.lse[plane * a.n * S::B + own.row] = real ? log_sum_exp(rule, state, sum) : kMinusInf;
+    store_columns<kBlocks>(static_cast<char*>(a.out) + at, g, first_block, sum2, 1.f / sum, real);
+  } else if constexpr (K == kScoredDQ) {
+    const float lean = sum_with_partner(state.lean), excess = sum_with_partner(state.excess);
+    float shift = excess;
+    if (rule.capped) {
+      const float weight = sum_with_partner(state.weight);
+      shift = lean + (weight > 0.f ? excess / weight : 0.f);
+    }
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum1[db][r] = __builtin_fmaf(-shift, sum2[db][r], sum1[db][r]);
+    store_columns<kBlocks>(static_cast<char*>(a.dq) + at, g, first_block, sum1, a.scale, own.there);
+    if (g == 0 && first_block == 0) a.rows[(plane * a.n * 2 + own.tile + 1) * S::B + own.row] += lean;  // (tile * 2 * B + B + slot)
+  } else {
+    store_columns<kBlocks>(static_cast<char*>(a.dk) + at, g, first_block, sum1, a.scale, own.there);
+    store_columns<kBlocks>(static_cast<char*>(a.dv) + at, g, first_block, sum2, 1.f, own.there);
   }
-  if constexpr (K != kScoredForward) store_columns<kBlocks>(result_of<K, 1>(a) + at, g, first_block, sum1, a.scale, real);
-  if constexpr (K != kScoredDQ) store_columns<kBlocks>(result_of<K, 2>(a) + at, g, first_block, sum2, factor, real);
 }
 
 // An item, in scalar registers.
@@ -360,15 +403,14 @@ __device__ __forceinline__ float* share_at(const ScoredArgs& a, int64_t share, i
   return a.share_sums + (share * S::kWaves + wave) * kWaveFloats;
 }
 
-template <class S, bool kLine, ScoredKernel K>
+// kCapped: of gradients, whose registers a branch more costs (it spills 25 of them at head dim 64, and takes 1.7 times as long); the forward kernel asks the rule.
+template <class S, bool kLine, ScoredKernel K, bool kCapped>
 __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads), amdgpu_waves_per_eu(scored_waves(K, S::D), scored_waves(K, S::D)))) void scored_kernel(ScoredArgs a) {
   constexpr bool kForward = K == kScoredForward, kKeys = (K == kScoredDKV);
-  constexpr bool kSum1 = K != kScoredForward, kSum2 = K != kScoredDQ;
-  // dK and dV: their sums and both own operands would be 192 registers at head dim 128, of 256; the value and a part of the key are kept in LDS, as much as two workgroups
-  // of a compute unit have room for (head dim 64: both, for three).  With the value alone there the kernel spills, and takes 1.2 times as long.
-  constexpr bool kTight = K == kScoredDKV;
-  constexpr int kHeld1 = kTight ? (S::D == 128 ? 5 : 0) : S::kContraction, kHeld2 = !kSum1 || kTight ? 0 : S::kContraction;
-  constexpr int kOwnSteps1 = S::kContraction - kHeld1, kOwnSteps2 = kSum1 ? S::kContraction - kHeld2 : 0;
+  // Gradients: two sums and both own operands would be 192 registers at head dim 128, of 256; the second operand and a part of the first are kept in LDS, as much as two
+  // workgroups of a compute unit have room for (head dim 64: both, for three).  With the second alone there the kernel of dK and dV spills, and takes 1.2 times as long.
+  constexpr int kHeld1 = kForward ? S::kContraction : S::D == 128 ? 5 : 0;
+  constexpr int kOwnSteps1 = S::kContraction - kHeld1, kOwnSteps2 = kForward ? 0 : S::kContraction;
   __shared__ __attribute__((aligned(1024))) ScoredLds<S, kOwnSteps1 + kOwnSteps2> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   const int64_t total = a.header ? CONST_PTR(int32_t, &a.header->items)[0] : gridDim.x;
@@ -387,14 +429,14 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   OwnToken<S, kLine> own(a, batch, first_tile, wave, i);
   float own_lse = 0.f, own_delta = 0.f;
   bf16x8* const own_lds = lds.own + wave * (kOwnSteps1 + kOwnSteps2) * 64 + lane;
-  const int64_t own_at = plane * plane_bytes + own.row * S::kRowBytes;
+  const int64_t own_at = plane * plane_bytes + (int64_t)own.row * S::kRowBytes;
   const OwnOperand<S, kHeld1> own1(static_cast<const char*>(kKeys ? a.k : a.q) + own_at, g, own_lds);
-  const std::conditional_t<kSum1, OwnOperand<S, kHeld2>, int> own2 = [&] {
-    if constexpr (kSum1) return OwnOperand<S, kHeld2>(static_cast<const char*>(kKeys ? a.v : a.dout) + own_at, g, own_lds + kOwnSteps1 * 64);
-    else return 0;
+  const std::conditional_t<kForward, int, OwnOperand<S, 0>> own2 = [&] {
+    if constexpr (kForward) return 0;
+    else return OwnOperand<S, 0>(static_cast<const char*>(kKeys ? a.v : a.dout) + own_at, g, own_lds + kOwnSteps1 * 64);
   }();
   if constexpr (K == kScoredDQ) {
-    const float* const t = stats + own.tile * 2 * S::B + (own.row - own.tile * S::B);
+    const float* const t = stats + ((int64_t)own.tile * S::B + own.row);  // (tile * 2 * B + slot)
     own_lse = t[0];
     own_delta = t[S::B];
     asm volatile("" : "+v"(own_lse), "+v"(own_delta));
@@ -402,7 +444,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   asm volatile("" : "+v"(own.pos), "+v"(own.limit), "+v"(own.doc));
   const uint32_t member = 1u << (30 + wave / (S::B / 32));  // the wave's tile in a step's word
 
-  floatx16 sum1[kSum1 ? S::kDBlocks : 1], sum2[kSum2 ? S::kDBlocks : 1];
+  floatx16 sum1[kForward ? 1 : S::kDBlocks], sum2[S::kDBlocks];
 #pragma unroll
   for (auto& t : sum1)
 #pragma unroll
@@ -412,6 +454,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
 #pragma unroll
     for (int r = 0; r < 16; ++r) t[r] = 0.f;
   Softmax soft;
+  RowSums row;
 
   const StepCopy<S> copy(wave, lane);
   const Fragments<S> frag(lane);
@@ -446,15 +489,18 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
         const int cls = compare ? 0 : step_class(word);  // (padding slots have a document of their own)
         const auto valid = CONST_PTR(uint32_t, a.class_mask) + (cls * 4 + step_half(word) * 2 + first_block);
         if constexpr (kForward) {
-          floatx16 s[S::kBlocks], unused;
+          floatx16 s[S::kBlocks];
 #pragma unroll
           for (int b = 0; b < S::kBlocks; ++b) s[b] = block_product<S>(frag, x, b, own1);
           if (rule.capped)
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) cap_scores<false>(rule, s[b], unused);
-          if constexpr (kLine)
+            for (int b = 0; b < S::kBlocks; ++b) cap_scores(rule, s[b]);
+          if (kLine && rule.biased)
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) bias_and_compare<S, K>(rule, s[b], info, first_block + b, g, compare, own.pos, own.doc, own.limit);
+            for (int b = 0; b < S::kBlocks; ++b) bias_scores<S>(rule, s[b], info, first_block + b, g, own.pos);
+          if (kLine && compare)
+#pragma unroll
+            for (int b = 0; b < S::kBlocks; ++b) hide_scores<S, K>(s[b], info, first_block + b, g, own.pos, own.doc, own.limit);
           if (cls != 0) {
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) mask_slots(s[b], __builtin_amdgcn_readfirstlane(valid[b]));
@@ -491,36 +537,50 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
         } else {
 #pragma unroll
           for (int b = 0; b < S::kBlocks; ++b) {
-            floatx16 steep, dp;
-            floatx16 s = block_product<S>(frag, x, b, own1);
-            if constexpr (kSum1) dp = block_product<S>(frag, y, b, own2);
-            if (rule.capped) cap_scores<kSum1>(rule, s, steep);
-            if constexpr (kLine) bias_and_compare<S, K>(rule, s, info, first_block + b, g, compare, own.pos, own.doc, own.limit);
-            if (K == kScoredDQ && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              floatx4 lse;
-              if constexpr (kKeys) lse = read4(info[4], first_block + b, j, g);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[4 * j + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * j + e], rule.c2, -(kKeys ? lse[e] : own_lse)));
-            }
-            bf16x8 p[2], ds[2];
-            if constexpr (kSum2) rounded(s, p);
-            if constexpr (kSum1) {
-              if (rule.capped)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] *= steep[r];
+            floatx16 s = block_product<S>(frag, x, b, own1), dp = block_product<S>(frag, y, b, own2);
+            // Both products end here.  Without it the compiler begins the weights while registers still hold the products' operands, and up to 36 values go to memory at
+            // head dim 128 (20K tokens, forward and backward 4176 / 3998 us); at head dim 64 there is room.
+            if constexpr (S::D == 128) __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kCapped) cap_scores(rule, s);
+            if (kLine && compare) hide_scores<S, K>(s, info, first_block + b, g, own.pos, own.doc, own.limit);
+            if (!kKeys && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
+            // s -> P (dQ: P steep), dp -> dS.  One value at a time, so that nothing else is held: steep = 1 - tanh^2 = -4 x (1 + x) is made from x when it is used, the bias goes into
+            // the exponent.
+            auto weigh = [&](auto biased) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                floatx4 delta;
-                if constexpr (kKeys) delta = read4(info[5], first_block + b, j, g);
+                floatx4 lse, delta, pos;
+                if constexpr (kKeys) lse = read4(info[4], first_block + b, j, g), delta = read4(info[5], first_block + b, j, g);
+                if constexpr (biased) pos = read4(info[kLinePosition], first_block + b, j, g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[4 * j + e] *= dp[4 * j + e] - (kKeys ? delta[e] : own_delta);
+                for (int e = 0; e < 4; ++e) {
+                  const float v = s[4 * j + e];
+                  float shift = kKeys ? -lse[e] : -own_lse;
+                  if constexpr (biased) shift = __builtin_fmaf(__builtin_fabsf(own.pos - pos[e]), rule.slope2, shift);
+                  float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, rule.c2, shift)), t = p * (dp[4 * j + e] - (kKeys ? delta[e] : own_delta));
+                  if constexpr (!kKeys) row.lean += t;
+                  if constexpr (kCapped) {
+                    const float bent = fmaxf(v, -1.f), steep = -4.f * __builtin_fmaf(bent, bent, bent);  // (a hidden score is minus infinity)
+                    t *= steep;
+                    if constexpr (!kKeys) row.excess -= t, row.weight += p *= steep;
+                  }
+                  s[4 * j + e] = p;
+                  dp[4 * j + e] = t;
+                }
               }
-              rounded(s, ds);
+            };
+            if (kLine && rule.biased) weigh(std::bool_constant<kLine>());
+            else weigh(std::false_type());
+            bf16x8 p[2], ds[2];
+            rounded(s, p);
+            rounded(dp, ds);
+            if constexpr (kKeys) {
+              block_sums<S>(frag, y, b, p, sum2);
+              block_sums<S>(frag, x, b, ds, sum1);
+            } else {
+              row.excess = sum_of_rounded(ds, row.excess);
+              block_sums<S>(frag, x, b, ds, sum1, p, sum2);
             }
-            if constexpr (kSum2) block_sums<S>(frag, y, b, p, sum2);
-            if constexpr (kSum1) block_sums<S>(frag, x, b, ds, sum1);
           }
         }
       }
@@ -529,26 +589,30 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     }
   }
 
+  const auto state = [&] {
+    if constexpr (kForward) return soft;
+    else return row;
+  }();
   if (item.share < 0) {
-    store_results<S, K, S::kDBlocks>(a, rule, plane, own, g, soft, 0, sum1, sum2);
+    store_results<S, K, S::kDBlocks>(a, rule, plane, own, g, state, 0, sum1, sum2);
     return;
   }
-  floatx4* out = reinterpret_cast<floatx4*>(share_at<S, K>(a, entry * a.shares + item.share, wave));
-  reinterpret_cast<float2*>(out)[lane] = float2{soft.ref, soft.sum};
-  out += 32;
+  floatx4* out = reinterpret_cast<floatx4*>(share_at<S, K>(a, entry * a.shares + item.share, wave)) + lane;
+  *out = kForward ? floatx4{soft.ref, soft.sum, 0.f, 0.f} : floatx4{row.lean, row.excess, row.weight, 0.f};
+  out += 64;
   auto leave = [&](const floatx16* sums) {
 #pragma unroll
-    for (int j = 0; j < 4 * S::kDBlocks; ++j, out += 64) out[lane] = floatx4{sums[j / 4][j % 4 * 4], sums[j / 4][j % 4 * 4 + 1], sums[j / 4][j % 4 * 4 + 2], sums[j / 4][j % 4 * 4 + 3]};
+    for (int j = 0; j < 4 * S::kDBlocks; ++j, out += 64) *out = floatx4{sums[j / 4][j % 4 * 4], sums[j / 4][j % 4 * 4 + 1], sums[j / 4][j % 4 * 4 + 2], sums[j / 4][j % 4 * 4 + 3]};
   };
-  if constexpr (kSum1) leave(sum1);
-  if constexpr (kSum2) leave(sum2);
+  if constexpr (!kForward) leave(sum1);
+  leave(sum2);
 }
 
 // Adds up the shares of a group, in their order, and writes its results: a workgroup takes 32 tokens, a wave 32 channels of them.  Bound: latency, and the shares
 // once.
 template <class S, bool kLine, ScoredKernel K>
 __global__ __launch_bounds__(S::kDBlocks * 64) void scored_merge_kernel(ScoredArgs a) {
-  constexpr bool kForward = K == kScoredForward, kSum1 = K != kScoredForward, kSum2 = K != kScoredDQ;
+  constexpr bool kForward = K == kScoredForward;
   constexpr int kAhead = 4;  // shares that are loaded before the first is added
   const int lane = threadIdx.x & 63, block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   const int wave = blockIdx.x % S::kWaves;
@@ -564,19 +628,19 @@ __global__ __launch_bounds__(S::kDBlocks * 64) void scored_merge_kernel(ScoredAr
 #pragma unroll
   for (int r = 0; r < 16; ++r) sum1[r] = sum2[r] = 0.f;
   Softmax soft;
+  RowSums row;
   for (int first = 0; first < merge.shares; first += kAhead) {
-    float2 stats[kAhead];
-    floatx4 part1[kAhead][4], part2[kAhead][4];
+    floatx4 stats[kAhead], part1[kAhead][4], part2[kAhead][4];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (first + k >= merge.shares) break;
-      const float* in = share_at<S, K>(a, entry * a.shares + merge.first_share + first + k, wave);
-      stats[k] = reinterpret_cast<const float2*>(in)[lane];
-      const floatx4* sums = reinterpret_cast<const floatx4*>(in + 128) + block * 256 + lane;
+      const floatx4* in = reinterpret_cast<const floatx4*>(share_at<S, K>(a, entry * a.shares + merge.first_share + first + k, wave)) + lane;
+      stats[k] = *in;
+      in += 64 + block * 256;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (kSum1) part1[k][j] = sums[j * 64];
-        if constexpr (kSum2) part2[k][j] = sums[(kSum1 ? S::kDBlocks * 256 : 0) + j * 64];
+        if constexpr (!kForward) part1[k][j] = in[j * 64];
+        part2[k][j] = in[(kForward ? 0 : S::kDBlocks * 256) + j * 64];
       }
     }
 #pragma unroll
@@ -584,27 +648,33 @@ __global__ __launch_bounds__(S::kDBlocks * 64) void scored_merge_kernel(ScoredAr
       if (first + k >= merge.shares) break;
       float weight = 1.f, old = 1.f;
       if constexpr (kForward) {
-        const float ref = fmaxf(soft.ref, stats[k].x);
+        const float ref = fmaxf(soft.ref, stats[k][0]);
         old = soft.ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2);
-        weight = stats[k].x == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((stats[k].x - ref) * rule.c2);
-        soft.sum = soft.sum * old + stats[k].y * weight;  // (a share without a finite score has no weight, but NaN stays)
+        weight = stats[k][0] == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((stats[k][0] - ref) * rule.c2);
+        soft.sum = soft.sum * old + stats[k][1] * weight;  // (a share without a finite score has no weight, but NaN stays)
         soft.ref = ref;
+      } else {
+        row.lean += stats[k][0];
+        row.excess += stats[k][1];
+        row.weight += stats[k][2];
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        if constexpr (kSum1) sum1[r] += part1[k][r / 4][r % 4];
-        if constexpr (kSum2) sum2[r] = __builtin_fmaf(weight, part2[k][r / 4][r % 4], sum2[r] * old);
+        if constexpr (!kForward) sum1[r] += part1[k][r / 4][r % 4];
+        sum2[r] = __builtin_fmaf(weight, part2[k][r / 4][r % 4], sum2[r] * old);
       }
     }
   }
-  store_results<S, K, 1>(a, rule, plane, own, g, soft, block, &sum1, &sum2);
+  if constexpr (kForward) store_results<S, K, 1>(a, rule, plane, own, g, soft, block, &sum1, &sum2);
+  else store_results<S, K, 1>(a, rule, plane, own, g, row, block, &sum1, &sum2);
 }
 
 template <class S, bool kLine, ScoredKernel K>
 hipError_t launch_items(const ScoredArgs& a, hipStream_t stream) {
   const int64_t entries = a.header ? 1 : a.batch, items = entries * a.num_items, merges = entries * a.num_merges;
   if (items < 1 || items > 0x7fffffff) return hipErrorInvalidValue;
-  scored_kernel<S, kLine, K><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
+  if (K != kScoredForward && a.cap > 0.f) scored_kernel<S, kLine, K, K != kScoredForward><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
+  else scored_kernel<S, kLine, K, false><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
   if (merges > 0) scored_merge_kernel<S, kLine, K><<<(unsigned)(merges * S::kWaves), S::kDBlocks * 64, 0, stream>>>(a);
   return hipGetLastError();
 }

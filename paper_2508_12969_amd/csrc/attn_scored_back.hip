@@ -4,7 +4,7 @@
 namespace ca {
 
 hipError_t launch_scored_dq(const ScoredArgs& a, hipStream_t stream) {
-  return a.D == 64 ? launch_scored<kScoredDQ, 64>(a, stream) : launch_scored<kScoredDQ, 128>(a, stream);
+  return a.D == 64 ? launch_scored<kScoredDQ, 64, 32>(a, stream) : launch_scored<kScoredDQ, 128, 32>(a, stream);
 }
 
 hipError_t launch_scored_dkv(const ScoredArgs& a, hipStream_t stream) {

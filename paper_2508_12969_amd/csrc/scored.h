@@ -69,8 +69,8 @@ constexpr int64_t scored_places(int64_t D) { return D == 64 ? 768 : 512; }
 constexpr int64_t most_merges(int64_t D) { return scored_places(D); }
 constexpr int64_t most_shares(int64_t D) { return 2 * scored_places(D); }
 
-// Sums of a share, per 32-token wave: (reference, sum) of every lane, and one or two sums of D channels.
-constexpr int64_t share_floats(int64_t D, int sums) { return kGroupTokens / 32 * (2 * 64 + sums * D * 32); }
+// Sums of a share, per 32-token wave: four figures of every lane, and one (forward) or two (gradients) sums of D channels.
+constexpr int64_t share_floats(int64_t D, int sums) { return kGroupTokens / 32 * (4 * 64 + sums * D * 32); }
 
 // Runs and items made on the device, in the workspace.
 struct VisitCounts {
@@ -112,7 +112,7 @@ struct ScoredArgs : GridArgs {
   // workspace
   float* line;                 // [batch][n][kLineRows][B]: position, document (as an integer), limit; null where no array is given
   TileLine* tiles;             // [batch][n]
-  float* rows;                 // backward: [batch * heads][n][2][B]: log-sum-exp in powers of two, delta
+  float* rows;                 // backward: [batch * heads][n][2][B]: log-sum-exp in powers of two, delta (put right by dQ)
 };
 
 // bytes of the parts of the workspace, each a multiple of 256
