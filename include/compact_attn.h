@@ -460,7 +460,7 @@ int compact_attn_norm_rotate_backward(const ca_norm* norm, const void* dq_out, c
  *   s = scale * q.k;  s = cap * tanh(s / cap);  s = s - slope[head] * |position_q - position_k|
  *   a query sees a key of its kept tiles iff their documents are equal and not negative, and position_k <= limit_q.
  * With cap 0 and no arrays it is compact_attn_forward with a log-sum-exp and gradients.
- *   cap        0 (none) or positive.
+ *   cap        0 (none) or 2^-16 to 4096; scores are off by up to 2^-21 of it.
  *   slopes     device pointer to num_heads floats, or NULL (no bias).  Needs positions.
  *   positions  device pointers to int32[batch][N_real] in natural order, 4-byte aligned, or NULL.  A token's place on the line along which distances and
  *   limits     limits are counted (a frame number, say); limits: the last position that the token sees, so limit = position is a causal

@@ -105,10 +105,12 @@ int64_t extent(const ca_layout* L, const ca::RowStrides& s, int64_t tokens) {
 
 int check_strides(const ca_layout* L, const ca_strides* s, const char* name) {
   if (!s) return CA_OK;
-  const int64_t unit = 16 / elem_size(L->prob.dtype);
-  for (int64_t v : {s->batch, s->head, s->token})
-    if (v < 0 || v >= ((int64_t)1 << 40) || v % unit != 0) {
-      set_error("strides of %s must be multiples of 16 bytes, not negative and below 2^40", name);
+  const ca_problem& p = L->prob;
+  const int64_t unit = 16 / elem_size(p.dtype);
+  const std::pair<int64_t, int64_t> steps[] = {{s->batch, p.batch}, {s->head, p.num_heads}, {s->token, L->N_real}};
+  for (const auto& [stride, count] : steps)
+    if (stride < 0 || stride > ((int64_t)1 << 40) / std::max<int64_t>(1, count - 1) || stride % unit != 0) {
+      set_error("strides of %s must be multiples of 16 bytes, not negative, and lead over fewer than 2^40 elements", name);
       return CA_ERR_INVALID_ARG;
     }
   return CA_OK;
@@ -195,6 +197,14 @@ int check_norm(const ca_norm* m, const ca_layout* L) {
   return st;
 }
 
+// What is read besides the tensors: weights and positions.  (Positions are not, without a rotation.)
+bool overlaps_small_inputs(const ca_layout* L, const void* at, int64_t bytes, const ca_norm* m, const ca_rotary* rotary, const ca_where* where) {
+  const ca_problem& p = L->prob;
+  const int64_t weight_bytes = (int64_t)p.head_dim * elem_size(p.dtype);
+  if (m && ((m->q_weight && ranges_overlap(at, bytes, m->q_weight, weight_bytes)) || (m->k_weight && ranges_overlap(at, bytes, m->k_weight, weight_bytes)))) return true;
+  return rotary && where && where->positions && ranges_overlap(at, bytes, where->positions, (int64_t)p.batch * L->N_real * 3 * (int64_t)sizeof(int32_t));
+}
+
 int64_t plane_elements(const ca_layout* L) { return (int64_t)L->prob.batch * L->prob.num_heads * L->prob.head_dim; }
 
 }  // namespace
@@ -274,6 +284,7 @@ int compact_attn_rotate(const void* src, const ca_strides* src_strides, void* ds
   a.dst_strides = strides_of(L, dst_strides, dst_tokens);
   if (ranges_overlap(src, extent(L, a.src_strides, src_tokens), dst, extent(L, a.dst_strides, dst_tokens)))
     return fail(CA_ERR_INVALID_ARG, "src and dst must not overlap");
+  if (overlaps_small_inputs(L, dst, extent(L, a.dst_strides, dst_tokens), nullptr, rotary, where)) return fail(CA_ERR_INVALID_ARG, "dst must not overlap the positions");
   st = fill_rows(a, L, rotary, where, tiled, (hipStream_t)stream);
   if (st != CA_OK) return st;
   a.src[0] = src;
@@ -297,7 +308,7 @@ int compact_attn_norm_rotate(const ca_norm* m, void* q_out, void* k_out, const c
   a.dst_strides = a.dst_strides1 = strides_of(L, nullptr, tokens);
   const int64_t q_bytes = extent(L, a.src_strides, L->N_real), k_bytes = extent(L, a.src_strides1, L->N_real);
   for (const void* out : {q_out, k_out})
-    if (ranges_overlap(out, out_bytes, m->q, q_bytes) || ranges_overlap(out, out_bytes, m->k, k_bytes))
+    if (ranges_overlap(out, out_bytes, m->q, q_bytes) || ranges_overlap(out, out_bytes, m->k, k_bytes) || overlaps_small_inputs(L, out, out_bytes, m, m->rotary, m->where))
       return fail(CA_ERR_INVALID_ARG, "results must not overlap the inputs");
   if (ranges_overlap(q_out, out_bytes, k_out, out_bytes)) return fail(CA_ERR_INVALID_ARG, "results must not overlap each other");
   st = fill_rows(a, L, m->rotary, m->where, m->tiled, (hipStream_t)stream);
@@ -355,9 +366,12 @@ int compact_attn_norm_rotate_backward(const ca_norm* m, const void* dq_out, cons
   const Range inputs[] = {{dq_out, dy_bytes}, {dk_out, dy_bytes}, {m->q, extent(L, a.x_strides, L->N_real)}, {m->k, extent(L, a.x_strides1, L->N_real)}};
   const Range results[] = {{dq, extent(L, a.dst_strides, L->N_real)}, {dk, extent(L, a.dst_strides1, L->N_real)},
                            {dq_weight, need ? weight_bytes : 0}, {dk_weight, need ? weight_bytes : 0}, {need ? workspace : nullptr, need}};
-  for (const Range& out : results)
-    for (const Range& in : inputs)
-      if (out.bytes && ranges_overlap(out.at, out.bytes, in.at, in.bytes)) return fail(CA_ERR_INVALID_ARG, "results and workspace must not overlap the inputs");
+  for (const Range& out : results) {
+    if (!out.bytes) continue;
+    bool apart = !overlaps_small_inputs(L, out.at, out.bytes, m, m->rotary, m->where);
+    for (const Range& in : inputs) apart = apart && !ranges_overlap(out.at, out.bytes, in.at, in.bytes);
+    if (!apart) return fail(CA_ERR_INVALID_ARG, "results and workspace must not overlap the inputs");
+  }
   // dq and dk may be interleaved in one tensor (strides), so only what surely is the same is refused
   if (dq == dk) return fail(CA_ERR_INVALID_ARG, "dq and dk must not be the same tensor");
   for (int i = 0; i < 5; ++i)

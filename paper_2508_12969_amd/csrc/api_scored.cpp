@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <climits>
-#include <cmath>
 #include <functional>
 #include <new>
 #include <queue>
@@ -32,7 +31,9 @@ int check_scores(const ca_layout* L, const ca_scores* s) {
     return CA_ERR_UNSUPPORTED;
   }
   if (p.batch > 65535 || (int64_t)p.batch * p.num_heads * L->n > 0x7fffffff) return fail(CA_ERR_UNSUPPORTED, "more than 65535 batch entries or 2^31 - 1 rows");
-  if (!(s->cap >= 0.f) || std::isinf(s->cap)) return fail(CA_ERR_INVALID_ARG, "cap must be finite and not negative");
+  if (L->n > 0xffffff) return fail(CA_ERR_UNSUPPORTED, "more than 2^24 - 1 tiles");  // (a step's word has 24 bits for one)
+  // capped scores are held as (tanh - 1) / 2 and off by a few 2^-24 of the cap
+  if (s->cap != 0.f && !(s->cap >= ca::kLeastCap && s->cap <= ca::kMostCap)) return fail(CA_ERR_INVALID_ARG, "cap must be 0 or between 2^-16 and 4096");
   if (s->slopes && !s->positions) return fail(CA_ERR_INVALID_ARG, "slopes need positions");
   if (s->limits && !s->positions) return fail(CA_ERR_INVALID_ARG, "limits need positions");
   if (!aligned4(s->slopes) || !aligned4(s->positions) || !aligned4(s->limits) || !aligned4(s->documents))

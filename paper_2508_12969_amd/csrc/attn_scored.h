@@ -672,7 +672,7 @@ __global__ __launch_bounds__(S::kDBlocks * 64) void scored_merge_kernel(ScoredAr
 template <class S, bool kLine, ScoredKernel K>
 hipError_t launch_items(const ScoredArgs& a, hipStream_t stream) {
   const int64_t entries = a.header ? 1 : a.batch, items = entries * a.num_items, merges = entries * a.num_merges;
-  if (items < 1 || items > 0x7fffffff) return hipErrorInvalidValue;
+  if (items < 1 || items > 0xffffff || merges * S::kWaves > 0xffffff) return hipErrorInvalidValue;  // (2^32 threads)
   if (K != kScoredForward && a.cap > 0.f) scored_kernel<S, kLine, K, K != kScoredForward><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
   else scored_kernel<S, kLine, K, false><<<(unsigned)items, S::kThreads, 0, stream>>>(a);
   if (merges > 0) scored_merge_kernel<S, kLine, K><<<(unsigned)(merges * S::kWaves), S::kDBlocks * 64, 0, stream>>>(a);

@@ -234,7 +234,7 @@ hipError_t launch_visits(const ScoredArgs& a, const Visits* visits, int count, h
 
 hipError_t launch_row_stats(const ScoredArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.batch * a.num_heads * a.N_pad, per = 256 / (a.D / 8), workgroups = (rows + per - 1) / per;
-  if (workgroups > 0x7fffffff) return hipErrorInvalidValue;
+  if (workgroups > 0xffffff) return hipErrorInvalidValue;  // (2^32 threads)
   if (a.D == 64) row_stats_kernel<64><<<(unsigned)workgroups, 256, 0, stream>>>(a, rows);
   else row_stats_kernel<128><<<(unsigned)workgroups, 256, 0, stream>>>(a, rows);
   return hipGetLastError();

@@ -411,7 +411,7 @@ hipError_t launch_rows(const RowArgs& a, bool bf16, hipStream_t stream) {
   const int64_t count = !kBack && a.tiled ? a.N_pad : a.N_real, blocks = (count + rows - 1) / rows;
   int per = (a.heads + head_blocks(blocks * a.batch, a.heads) - 1) / head_blocks(blocks * a.batch, a.heads);
   const dim3 grid((unsigned)blocks, (unsigned)((a.heads + per - 1) / per), (unsigned)a.batch);
-  if (grid.y > 65535 || grid.z > 65535) return hipErrorInvalidValue;
+  if (blocks > 0xffffff || grid.y > 65535 || grid.z > 65535) return hipErrorInvalidValue;  // (2^32 threads in x)
   with_pairing(a, bf16, [&](auto type, auto pairing) {
     rows_kernel<decltype(type), decltype(pairing)::value, kNorm, kBack><<<grid, kRowThreads, 0, stream>>>(a, per);
   });

@@ -33,6 +33,7 @@ enum LineRow { kLinePosition = 0, kLineDocument = 1, kLineLimit = 2, kLineRows =
 // A workgroup takes an item, a group's run or a part of it; where a group has several, each leaves its sums as a share, which a second kernel adds up in
 // their order.
 constexpr int kGroupTokens = 128;
+constexpr float kLeastCap = 1.f / 65536, kMostCap = 4096.f;
 struct ScoredItem {
   int64_t first;               // of its steps
   int32_t count, group, share; // share: -1 for a group that is one item

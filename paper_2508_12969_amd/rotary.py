@@ -111,9 +111,17 @@ def _check_rows(t, layout, padded, name):
     return ca_strides(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
 
 
+def _table(rotary):
+    if rotary is not None and rotary.handle is None:
+        raise ValueError("rotary has been freed")
+    return None if rotary is None else rotary.handle
+
+
 def _where(layout, origin, positions):
+    if len(origin) != 3:
+        raise ValueError("origin has a value for each of three axes")
     if positions is None:
-        return None if origin == (0, 0, 0) else ca_where((ctypes.c_int32 * 3)(*origin), None)
+        return None if tuple(origin) == (0, 0, 0) else ca_where((ctypes.c_int32 * 3)(*origin), None)
     import torch
     _on_current_device(positions, "positions")
     expected = (layout.problem.batch, layout.n_tokens_real, 3)
@@ -144,7 +152,7 @@ def compact_attn_rotate(src, layout, rotary, origin=(0, 0, 0), positions=None, t
         with _on(stream, src.device):
             out = src.new_empty(layout.shape(padded_out))
     where = _where(layout, origin, positions)
-    _check(load_library().compact_attn_rotate(src.data_ptr(), src_strides, out.data_ptr(), dst_strides, layout.handle, rotary.handle, where, int(tiled),
+    _check(load_library().compact_attn_rotate(src.data_ptr(), src_strides, out.data_ptr(), dst_strides, layout.handle, _table(rotary), where, int(tiled),
                                               int(transpose), _stream_ptr(stream)))
     return out
 
@@ -159,7 +167,7 @@ def _norm(q, k, q_weight, k_weight, layout, rotary, eps, origin, positions, tile
     pointers = [None if s is None else ctypes.pointer(s) for s in strides]
     weights = [None if w is None else w.data_ptr() for w in (q_weight, k_weight)]
     where = _where(layout, origin, positions)
-    return ca_norm(q.data_ptr(), k.data_ptr(), *pointers, *weights, None if rotary is None else rotary.handle, None if where is None else ctypes.pointer(where), eps,
+    return ca_norm(q.data_ptr(), k.data_ptr(), *pointers, *weights, _table(rotary), None if where is None else ctypes.pointer(where), eps,
                    int(bool(tiled)))
 
 

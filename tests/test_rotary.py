@@ -142,6 +142,37 @@ def test_norm_refusals():
         assert st == -1 and message, (bad, st, message)
 
 
+def test_strides_and_overlaps_beyond_the_tensors_are_refused():
+    lay = _layout(4, 8, 8, (1, 4, 4), 16, 1, 2, 64, "f32")
+    tokens = lay.n_tokens_real
+    rotary = ca.compact_attn_build_rotary((8, 28, 28), (4, 8, 8))
+    rotate = lambda ss=None, where=None: _status(lambda lib: lib.compact_attn_rotate(P[0], ss, P[1], None, lay.handle, rotary.handle, where, 1, 0, None))
+    st, message = rotate(R.ca_strides(0, 64, (1 << 40) // (tokens - 1) // 4 * 4 + 4))
+    assert st == -1 and "2^40" in message
+    st, message = rotate(R.ca_strides(0, (1 << 62), 64))
+    assert st == -1 and "2^40" in message
+    st, message = rotate(where=R.ca_where((ctypes.c_int32 * 3)(0, 0, 0), P[1] + 64))
+    assert st == -1 and "positions" in message
+    norm = R.ca_norm(P[0], P[1], None, None, P[2], P[3], rotary.handle, ctypes.pointer(R.ca_where((ctypes.c_int32 * 3)(0, 0, 0), P[4])), 1e-6, 1)
+    for outs in ((P[2], P[5]), (P[5], P[3] + 16), (P[4], P[5])):
+        st, message = _status(lambda lib: lib.compact_attn_norm_rotate(norm, *outs, lay.handle, None))
+        assert st == -1 and "overlap" in message, outs
+    for dq, dwq in ((P[2], P[9]), (P[7], P[3]), (P[7], P[4] + 64)):
+        st, message = _status(lambda lib: lib.compact_attn_norm_rotate_backward(norm, P[5], P[6], dq, None, P[8], None, dwq, P[10], lay.handle, P[11], 1 << 30, None))
+        assert st == -1 and "overlap" in message, (dq, dwq)
+
+
+def test_freed_tables_and_short_origins_are_refused():
+    lay = _layout(4, 8, 8, (1, 4, 4), 16, 1, 2, 64, "f32")
+    rotary = ca.compact_attn_build_rotary((8, 28, 28), (4, 8, 8))
+    with pytest.raises(ValueError):
+        R._where(lay, (1, 2), None)
+    assert R._where(lay, [0, 0, 0], None) is None and R._table(None) is None and R._table(rotary) is rotary.handle
+    rotary.free()
+    with pytest.raises(ValueError):   # not a call without a rotation
+        R._table(rotary)
+
+
 # ---------------------------------------------------------------- the oracle's gradient, from differences
 
 @pytest.mark.parametrize("pairing", ["half", "interleaved"])
@@ -422,6 +453,19 @@ def test_binding_refusals():
     for bad in (lambda: rot(origin=(9, 0, 0)), lambda: rot(origin=(-1, 0, 0))):
         with pytest.raises(ca.CompactAttnError):
             bad()
+
+
+@pytest.mark.gpu
+def test_a_head_that_is_shared_is_read_in_place():
+    """Expanded keys (stride 0 over the heads): results and gradients are those of a copy, a gradient for every head."""
+    pb = Problem(CASES[2], 11)
+    q, wq, wk = pb.tensor(), pb.weight(), pb.weight()
+    k = pb.tensor()[:, :1].expand(q.shape)
+    dyq, dyk = (ca.compact_attn_permute(pb.tensor(False), pb.layout) for _ in range(2))
+    step = lambda k: (*ca.compact_attn_norm_rotate(q, k, wq, wk, pb.layout, pb.rotary),
+                      *ca.compact_attn_norm_rotate_backward(dyq, dyk, q, k, wq, wk, pb.layout, pb.rotary))
+    for a, b in zip(step(k), step(k.contiguous())):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.gpu

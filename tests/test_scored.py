@@ -61,7 +61,7 @@ def test_refusals():
         return _call("compact_attn_backward_scored", do, q, k, v, o, lse, lay.handle, s, dq, dk, dv, ws, size, None)
 
     S = SC.ca_scores
-    bad_scores = [S(-1.0, None, None, None, None), S(math.nan, None, None, None, None), S(math.inf, None, None, None, None), S(0.0, P[8], None, None, None),
+    bad_scores = [S(-1.0, None, None, None, None), S(math.nan, None, None, None, None), S(math.inf, None, None, None, None), S(1e-6, None, None, None, None), S(5000.0, None, None, None, None), S(0.0, P[8], None, None, None),
                   S(0.0, None, None, P[10], None), S(0.0, P[8] + 2, P[9], None, None), S(0.0, None, P[9] + 1, None, None), S(0.0, None, P[9], P[10] + 2, None),
                   S(0.0, None, None, None, P[11] + 3)]
     for bad in [dict(q=None), dict(out=None), dict(lse=None), dict(s=None), dict(q=P[0] + 8), dict(out=P[3] + 8), dict(lse=P[4] + 2), dict(ws=None), dict(ws=P[5] + 8),
@@ -263,7 +263,7 @@ def test_few_tokens(grid, tile, n_text, D, rule):
 @pytest.mark.gpu
 def test_peaked_and_flat_rows():
     """Scores that a cap bends hard, and rows whose weight lies on one key."""
-    for kw in (dict(cap=1.0, gain=30.0), dict(cap=50.0, gain=20.0), dict(gain=20.0), dict(cap=0.5, gain=0.0)):
+    for kw in (dict(cap=1.0, gain=30.0), dict(cap=50.0, gain=20.0), dict(gain=20.0), dict(cap=0.5, gain=0.0), dict(cap=2.0 ** -16, gain=1.0), dict(cap=4096.0, gain=2.0)):
         print("scored", kw, flush=True)
         pb = Problem((2, 9, 17), (1, 8, 8), 0, 64, seed=7, **kw)
         pb.check(*pb.run())
