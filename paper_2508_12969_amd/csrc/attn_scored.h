@@ -337,6 +337,32 @@ struct OwnToken {
   }
 };
 
+// What the tokens of a wave that are there have in common, in scalar registers: a streamed token outside of it has no pair with the wave.  Where pairs are compared, a
+// wave leaves out what it has no pair with (two lanes' worth of reads and a ballot a step; 9K tokens, three clips in a causal order, forward and backward: 1420 / 1360 us
+// without / with, 8K tokens causal at head dim 64, few steps compared: 139 / 141).
+template <bool kKeys>
+struct WaveLine {
+  int doc_min = 0x7fffffff, doc_max = -1;
+  float reach = kKeys ? __builtin_inff() : kMinusInf;  // lowest position of the keys, highest limit of the queries
+  template <class Token>
+  __device__ __forceinline__ explicit WaveLine(const Token& own) {
+    if (own.there) doc_min = doc_max = own.doc, reach = kKeys ? own.pos : own.limit;
+#pragma unroll
+    for (int step = 1; step < 32; step *= 2) {  // (both halves of a wave hold the same tokens)
+      doc_min = min(doc_min, __shfl_xor(doc_min, step));
+      doc_max = max(doc_max, __shfl_xor(doc_max, step));
+      reach = kKeys ? fminf(reach, __shfl_xor(reach, step)) : fmaxf(reach, __shfl_xor(reach, step));
+    }
+    doc_min = __builtin_amdgcn_readfirstlane(doc_min);
+    doc_max = __builtin_amdgcn_readfirstlane(doc_max);
+    reach = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, reach)));
+  }
+  // With which of the lanes' streamed tokens may the wave have a pair?
+  __device__ __forceinline__ uint64_t meets(int doc, float x) const {
+    return __builtin_amdgcn_ballot_w64((int)(doc >= doc_min) & (int)(doc <= doc_max) & (int)(kKeys ? reach <= x : x <= reach));
+  }
+};
+
 template <class S, ScoredKernel K>
 constexpr int sums_of() {
   return K == kScoredForward ? 1 : 2;
@@ -442,6 +468,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     asm volatile("" : "+v"(own_lse), "+v"(own_delta));
   }
   asm volatile("" : "+v"(own.pos), "+v"(own.limit), "+v"(own.doc));
+  const WaveLine<kKeys> wave_line(own);
   const uint32_t member = 1u << (30 + wave / (S::B / 32));  // the wave's tile in a step's word
 
   floatx16 sum1[kForward ? 1 : S::kDBlocks], sum2[S::kDBlocks];
@@ -482,10 +509,17 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
       WAIT_LGKMCNT0();
       BARRIER();  // the step's X and Y are there, and nobody reads the other buffer any more
       if (step + 1 < steps) issue(next, S::kSubs == 1 ? 0 : sub ^ 1, buffer ^ 1);
-      if (own.active && (word & member) != 0) {
+      const float(&info)[S::kInfoRows][64] = lds.info[buffer];
+      const bool compare = kLine && (word & kStepCompares) != 0;
+      bool visit = own.active && (word & member) != 0;
+      if constexpr (kLine) {
+        if (visit && compare) {
+          const uint64_t met = wave_line.meets(__builtin_bit_cast(int, info[kLineDocument][lane]), info[kKeys ? kLineLimit : kLinePosition][lane]);
+          visit = S::kStep == 64 ? met != 0 : (uint32_t)(met >> (first_block * 32)) != 0;
+        }
+      }
+      if (visit) {
         const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
-        const float(&info)[S::kInfoRows][64] = lds.info[buffer];
-        const bool compare = kLine && (word & kStepCompares) != 0;
         const int cls = compare ? 0 : step_class(word);  // (padding slots have a document of their own)
         const auto valid = CONST_PTR(uint32_t, a.class_mask) + (cls * 4 + step_half(word) * 2 + first_block);
         if constexpr (kForward) {
@@ -538,9 +572,9 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
 #pragma unroll
           for (int b = 0; b < S::kBlocks; ++b) {
             floatx16 s = block_product<S>(frag, x, b, own1), dp = block_product<S>(frag, y, b, own2);
-            // Both products end here.  Without it the compiler begins the weights while registers still hold the products' operands, and up to 36 values go to memory at
-            // head dim 128 (20K tokens, forward and backward 4176 / 3998 us); at head dim 64 there is room.
-            if constexpr (S::D == 128) __builtin_amdgcn_sched_barrier(0);
+            // Both products end here.  Without it the compiler begins the weights while registers still hold the products' operands, and up to 36 values go to memory
+            // at head dim 128 (forward and backward at 20K tokens, 6 heads: 4176 / 3998 us; at head dim 64, 8K tokens: 1315 / 1301).
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (kCapped) cap_scores(rule, s);
             if (kLine && compare) hide_scores<S, K>(s, info, first_block + b, g, own.pos, own.doc, own.limit);
             if (!kKeys && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
