@@ -303,10 +303,11 @@ struct Softmax {
 // What the lane's query of dQ adds up besides, over its share of the keys.  delta comes from the rounded result, and dS is rounded as an operand; both shift all of
 // a row's dS the same way, and such a shift meets the weighted mean of the keys, which is not small.  In exact arithmetic P (dP - delta) sums to zero over a row, and so the
 // row's sums say what the shift is: `lean` is by how much delta is off, `excess` what rounding added.  dQ is put right at the end by as much of
-// sum2 = sum of (P steep) K, and delta by lean, for dK.  (Relative error of dQ / dK at scores of a spread of 3: 3.6e-3 / 2.7e-3 without, 2.2e-3 / 2.2e-3 with, of which 1.7e-3 is the
-// rounding of the result.  It is one product more, of seven: 36K tokens, dense, forwards not counted, 17.0 / 18.4 ms at head dim 128 and 9.0 / 10.3 at 64.)
+// sum2 = sum of (P steep) K, and delta by lean, for dK.  Without a cap excess is the sum of the rounded dS, both in one, and delta is put right by that: what rounding adds to
+// it is small beside the roundings of dK's own dS.  (Relative error of dQ / dK at scores of a spread of 3: 3.6e-3 / 2.7e-3 without, 2.2e-3 / 2.2e-3 with, of which
+// 1.7e-3 is the rounding of the result.  It is one product more, of seven: 36K tokens, dense, forwards not counted, 17.0 / 18.0 ms at head dim 128 and 9.1 / 10.1 at 64.)
 struct RowSums {
-  float lean = 0.f, excess = 0.f, weight = 0.f;  // sums of P (dP - delta), of dS rounded less dS, of P steep; without a cap dS sums to lean, which is not taken off, and the weight is 1
+  float lean = 0.f, excess = 0.f, weight = 0.f;  // sums of P (dP - delta), of dS rounded less dS, of P steep; without a cap of dS rounded alone
 };
 
 // The lane's token, and what becomes of its sums.
@@ -386,7 +387,7 @@ __device__ __forceinline__ void store_columns(char* row, int g, int first_block,
 // Writes channel blocks first_block .. + kBlocks - 1 of a token's results.  state: Softmax (forward) or RowSums (dQ).
 template <class S, ScoredKernel K, int kBlocks, class Token, class State>
 __device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const State& state, int first_block,
-                                              floatx16* sum1, const floatx16* sum2) {
+                                              const floatx16* sum1, const floatx16* sum2) {
   if (!own.writes) return;
   const int64_t at = (plane * a.n * S::B + own.row) * S::kRowBytes;
   if constexpr (K == kScoredForward) {
@@ -395,17 +396,19 @@ __device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRu
     if (g == 0 && first_block == 0) a.lse[plane * a.n * S::B + own.row] = real ? log_sum_exp(rule, state, sum) : kMinusInf;
     store_columns<kBlocks>(static_cast<char*>(a.out) + at, g, first_block, sum2, 1.f / sum, real);
   } else if constexpr (K == kScoredDQ) {
-    const float lean = sum_with_partner(state.lean), excess = sum_with_partner(state.excess);
-    float shift = excess;
+    const float excess = sum_with_partner(state.excess);
+    float lean = excess, shift = excess;
     if (rule.capped) {
       const float weight = sum_with_partner(state.weight);
+      lean = sum_with_partner(state.lean);
       shift = lean + (weight > 0.f ? excess / weight : 0.f);
     }
+    floatx16 sum[kBlocks];
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum1[db][r] = __builtin_fmaf(-shift, sum2[db][r], sum1[db][r]);
-    store_columns<kBlocks>(static_cast<char*>(a.dq) + at, g, first_block, sum1, a.scale, own.there);
+      for (int r = 0; r < 16; ++r) sum[db][r] = __builtin_fmaf(-shift, sum2[db][r], sum1[db][r]);
+    store_columns<kBlocks>(static_cast<char*>(a.dq) + at, g, first_block, sum, a.scale, own.there);
     if (g == 0 && first_block == 0) a.rows[(plane * a.n * 2 + own.tile + 1) * S::B + own.row] += lean;  // (tile * 2 * B + B + slot)
   } else {
     store_columns<kBlocks>(static_cast<char*>(a.dk) + at, g, first_block, sum1, a.scale, own.there);
@@ -592,11 +595,11 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
                   float shift = kKeys ? -lse[e] : -own_lse;
                   if constexpr (biased) shift = __builtin_fmaf(__builtin_fabsf(own.pos - pos[e]), rule.slope2, shift);
                   float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, rule.c2, shift)), t = p * (dp[4 * j + e] - (kKeys ? delta[e] : own_delta));
-                  if constexpr (!kKeys) row.lean += t;
+                  if constexpr (!kKeys && kCapped) row.lean += t;
                   if constexpr (kCapped) {
                     const float bent = fmaxf(v, -1.f), steep = -4.f * __builtin_fmaf(bent, bent, bent);  // (a hidden score is minus infinity)
                     t *= steep;
-                    if constexpr (!kKeys) row.excess -= t, row.weight += p *= steep;
+                    if constexpr (!kKeys) row.excess -= t, p *= steep;
                   }
                   s[4 * j + e] = p;
                   dp[4 * j + e] = t;
@@ -613,6 +616,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
               block_sums<S>(frag, x, b, ds, sum1);
             } else {
               row.excess = sum_of_rounded(ds, row.excess);
+              if constexpr (kCapped) row.weight = sum_of_rounded(p, row.weight);
               block_sums<S>(frag, x, b, ds, sum1, p, sum2);
             }
           }
