@@ -461,7 +461,7 @@ int compact_attn_norm_rotate_backward(const ca_norm* norm, const void* dq_out, c
  *   a query sees a key of its kept tiles iff their documents are equal and not negative, and position_k <= limit_q.
  * With cap 0 and no arrays it is compact_attn_forward with a log-sum-exp and gradients.
  *   cap        0 (none) or 2^-16 to 4096; scores are off by up to 2^-21 of it.
- *   slopes     device pointer to num_heads floats, or NULL (no bias).  Needs positions.
+ *   slopes     device pointer to num_heads floats, or NULL (no bias).  Needs positions.  Slope times distance must stay below 10^12.
  *   positions  device pointers to int32[batch][N_real] in natural order, 4-byte aligned, or NULL.  A token's place on the line along which distances and
  *   limits     limits are counted (a frame number, say); limits: the last position that the token sees, so limit = position is a causal
  *   documents  order and limit = max(position, P - 1) one whose first P positions are seen by all (limits needs positions).  documents: tokens see tokens

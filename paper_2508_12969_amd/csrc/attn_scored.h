@@ -177,14 +177,14 @@ __device__ __forceinline__ void cap_scores(const ScoreRule& rule, floatx16& s) {
 }
 
 // Masks the padding slots of a block of 32 streamed keys (no arrays given), as QueryWave::mask_padding_keys does.
-__device__ __forceinline__ void mask_slots(floatx16& s, uint32_t bits) {
+__device__ __forceinline__ void mask_slots(floatx16& s, uint32_t bits, float hidden) {
   if (bits == 0xffffffffu) return;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int bit = 8 * (r / 4) + (r % 4);
     const uint32_t lo = 0u - ((bits >> bit) & 1u), hi = 0u - ((bits >> (bit + 4)) & 1u);
     const uint64_t keep = (uint64_t)lo | ((uint64_t)hi << 32);
-    asm("v_cndmask_b32 %0, %1, %0, %2" : "+v"(s[r]) : "v"(kMinusInf), "s"(keep));
+    asm("v_cndmask_b32 %0, %1, %0, %2" : "+v"(s[r]) : "v"(hidden), "s"(keep));
   }
 }
 
@@ -205,9 +205,9 @@ __device__ __forceinline__ void bias_scores(const ScoreRule& rule, floatx16& s, 
   }
 }
 
-// Documents and limits of a block: hidden pairs get minus infinity.  own_limit is the lane's where it is a query; else the streamed tokens' limits are read.
+// Documents and limits of a block: hidden pairs get the score `hidden`.  own_limit is the lane's where it is a query; else the streamed tokens' limits are read.
 template <class S, ScoredKernel K>
-__device__ __forceinline__ void hide_scores(floatx16& s, const float (&info)[S::kInfoRows][64], int block, int g, float own_pos, int own_doc, float own_limit) {
+__device__ __forceinline__ void hide_scores(floatx16& s, const float (&info)[S::kInfoRows][64], int block, int g, float own_pos, int own_doc, float own_limit, float hidden) {
   constexpr bool kKeys = K == kScoredDKV;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -216,7 +216,7 @@ __device__ __forceinline__ void hide_scores(floatx16& s, const float (&info)[S::
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const bool seen = (int)(kKeys ? own_pos <= reach[e] : reach[e] <= own_limit) & (int)(doc[e] == own_doc);
-      s[4 * i + e] = seen ? s[4 * i + e] : kMinusInf;
+      s[4 * i + e] = seen ? s[4 * i + e] : hidden;
     }
   }
 }
@@ -247,12 +247,16 @@ struct OwnOperand {
   __device__ __forceinline__ bf16x8 at(int s) const { return s < kInRegisters ? held[s < kInRegisters ? s : 0] : rest[(s - kInRegisters) * 64]; }
 };
 
-// S^T of a block: 32 streamed tokens x the lane's token
-template <class S, class Own>
-__device__ __forceinline__ floatx16 block_product(const Fragments<S>& f, LdsTile lds, int block, const Own& own) {
-  floatx16 acc;
+__device__ __forceinline__ floatx16 splat(float x) {
+  floatx16 v;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  for (int r = 0; r < 16; ++r) v[r] = x;
+  return v;
+}
+
+// S^T of a block, 32 streamed tokens x the lane's token, added to acc
+template <class S, class Own>
+__device__ __forceinline__ floatx16 block_product(const Fragments<S>& f, LdsTile lds, int block, const Own& own, floatx16 acc) {
 #pragma unroll
   for (int s = 0; s < S::kContraction; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.by_rows(lds, block, s), own.at(s), acc, 0, 0, 0);
   return acc;
@@ -384,6 +388,8 @@ __device__ __forceinline__ void store_columns(char* row, int g, int first_block,
       *reinterpret_cast<bf16x4*>(row + ((first_block + db) * 32 + 8 * r4 + 4 * g) * 2) = v;
     }
 }
+// Of sums of dS: with a cap they are made without the -4 of 1 - tanh^2 = -4 x (1 + x).
+__device__ __forceinline__ float gradient_factor(const ScoredArgs& a, const ScoreRule& rule) { return rule.capped ? -4.f * a.scale : a.scale; }
 // Writes channel blocks first_block .. + kBlocks - 1 of a token's results.  state: Softmax (forward) or RowSums (dQ).
 template <class S, ScoredKernel K, int kBlocks, class Token, class State>
 __device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRule& rule, int64_t plane, const Token& own, int g, const State& state, int first_block,
@@ -401,17 +407,17 @@ __device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRu
     if (rule.capped) {
       const float weight = sum_with_partner(state.weight);
       lean = sum_with_partner(state.lean);
-      shift = lean + (weight > 0.f ? excess / weight : 0.f);
+      shift = lean + (weight != 0.f ? excess / weight : 0.f);
     }
     floatx16 sum[kBlocks];
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum[db][r] = __builtin_fmaf(-shift, sum2[db][r], sum1[db][r]);
-    store_columns<kBlocks>(static_cast<char*>(a.dq) + at, g, first_block, sum, a.scale, own.there);
-    if (g == 0 && first_block == 0) a.rows[(plane * a.n * 2 + own.tile + 1) * S::B + own.row] += lean;  // (tile * 2 * B + B + slot)
+    store_columns<kBlocks>(static_cast<char*>(a.dq) + at, g, first_block, sum, gradient_factor(a, rule), own.there);
+    if (g == 0 && first_block == 0) a.rows[(plane * a.n * 2 + own.tile + 1) * S::B + own.row] -= lean;  // (tile * 2 * B + B + slot)
   } else {
-    store_columns<kBlocks>(static_cast<char*>(a.dk) + at, g, first_block, sum1, a.scale, own.there);
+    store_columns<kBlocks>(static_cast<char*>(a.dk) + at, g, first_block, sum1, gradient_factor(a, rule), own.there);
     store_columns<kBlocks>(static_cast<char*>(a.dv) + at, g, first_block, sum2, 1.f, own.there);
   }
 }
@@ -485,6 +491,11 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
     for (int r = 0; r < 16; ++r) t[r] = 0.f;
   Softmax soft;
   RowSums row;
+  // dP - delta: the product of dP begins at minus delta, which saves a subtraction a value.  For queries it takes 16 registers more: head dim 128 has none left, and 64 with
+  // token arrays would spill 25
+  constexpr bool kDeltaFirst = kKeys || (S::D == 64 && !kLine);
+  floatx16 minus_delta = splat(!kKeys && kDeltaFirst ? own_delta : 0.f);
+  if constexpr (!kForward && !kKeys && kDeltaFirst) asm volatile("" : "+v"(minus_delta));
 
   const StepCopy<S> copy(wave, lane);
   const Fragments<S> frag(lane);
@@ -528,7 +539,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
         if constexpr (kForward) {
           floatx16 s[S::kBlocks];
 #pragma unroll
-          for (int b = 0; b < S::kBlocks; ++b) s[b] = block_product<S>(frag, x, b, own1);
+          for (int b = 0; b < S::kBlocks; ++b) s[b] = block_product<S>(frag, x, b, own1, splat(0.f));
           if (rule.capped)
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) cap_scores(rule, s[b]);
@@ -537,10 +548,10 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
             for (int b = 0; b < S::kBlocks; ++b) bias_scores<S>(rule, s[b], info, first_block + b, g, own.pos);
           if (kLine && compare)
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) hide_scores<S, K>(s[b], info, first_block + b, g, own.pos, own.doc, own.limit);
+            for (int b = 0; b < S::kBlocks; ++b) hide_scores<S, K>(s[b], info, first_block + b, g, own.pos, own.doc, own.limit, kMinusInf);
           if (cls != 0) {
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) mask_slots(s[b], __builtin_amdgcn_readfirstlane(valid[b]));
+            for (int b = 0; b < S::kBlocks; ++b) mask_slots(s[b], __builtin_amdgcn_readfirstlane(valid[b]), kMinusInf);
           }
           float mx = s[0][0];
 #pragma unroll
@@ -574,30 +585,38 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
         } else {
 #pragma unroll
           for (int b = 0; b < S::kBlocks; ++b) {
-            floatx16 s = block_product<S>(frag, x, b, own1), dp = block_product<S>(frag, y, b, own2);
+            floatx16 less = minus_delta;
+            if constexpr (kKeys)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const floatx4 d = read4(info[5], first_block + b, j, g);
+                less[4 * j] = d[0], less[4 * j + 1] = d[1], less[4 * j + 2] = d[2], less[4 * j + 3] = d[3];
+              }
+            floatx16 s = block_product<S>(frag, x, b, own1, splat(0.f)), dp = block_product<S>(frag, y, b, own2, less);
             // Both products end here.  Without it the compiler begins the weights while registers still hold the products' operands, and up to 36 values go to memory
             // at head dim 128 (forward and backward at 20K tokens, 6 heads: 4176 / 3998 us; at head dim 64, 8K tokens: 1315 / 1301).
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (kCapped) cap_scores(rule, s);
-            if (kLine && compare) hide_scores<S, K>(s, info, first_block + b, g, own.pos, own.doc, own.limit);
-            if (!kKeys && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]));
-            // s -> P (dQ: P steep), dp -> dS.  One value at a time, so that nothing else is held: steep = 1 - tanh^2 = -4 x (1 + x) is made from x when it is used, the bias goes into
-            // the exponent.
+            constexpr float kHidden = kCapped ? -1e18f : kMinusInf;  // (no weight either way; its square is finite, for steep)
+            if (kLine && compare) hide_scores<S, K>(s, info, first_block + b, g, own.pos, own.doc, own.limit, kHidden);
+            if (!kKeys && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]), kHidden);
+            // s -> P (dQ: P steep), dp -> dS.  One value at a time, so that nothing else is held: steep = 1 - tanh^2 = -4 x (1 + x) is made from x when it is used, its -4 is left to the
+            // results (gradient_factor), the bias goes into the exponent.
             auto weigh = [&](auto biased) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                floatx4 lse, delta, pos;
-                if constexpr (kKeys) lse = read4(info[4], first_block + b, j, g), delta = read4(info[5], first_block + b, j, g);
+                floatx4 lse, pos;
+                if constexpr (kKeys) lse = read4(info[4], first_block + b, j, g);
                 if constexpr (biased) pos = read4(info[kLinePosition], first_block + b, j, g);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const float v = s[4 * j + e];
                   float shift = kKeys ? -lse[e] : -own_lse;
                   if constexpr (biased) shift = __builtin_fmaf(__builtin_fabsf(own.pos - pos[e]), rule.slope2, shift);
-                  float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, rule.c2, shift)), t = p * (dp[4 * j + e] - (kKeys ? delta[e] : own_delta));
+                  float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, rule.c2, shift)), t = p * (kDeltaFirst ? dp[4 * j + e] : dp[4 * j + e] + own_delta);
                   if constexpr (!kKeys && kCapped) row.lean += t;
                   if constexpr (kCapped) {
-                    const float bent = fmaxf(v, -1.f), steep = -4.f * __builtin_fmaf(bent, bent, bent);  // (a hidden score is minus infinity)
+                    const float steep = __builtin_fmaf(v, v, v);
                     t *= steep;
                     if constexpr (!kKeys) row.excess -= t, p *= steep;
                   }

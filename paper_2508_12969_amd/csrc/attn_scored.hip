@@ -53,7 +53,7 @@ __global__ void line_kernel(ScoredArgs a) {
 }
 
 // Per query: the log-sum-exp in powers of two, less the offset of a cap (ScoreRule) (plus infinity where it has none, so that all weights are zero backwards), and
-// delta = sum of dO O, which is what dP of every key is reduced by.  Bound: HBM, dO and O once.
+// minus delta, delta = sum of dO O, which is what dP of every key is reduced by.  Bound: HBM, dO and O once.
 template <int D>
 __global__ __launch_bounds__(256) void row_stats_kernel(ScoredArgs a, int64_t rows) {
   constexpr int kLanes = D / 8, kRows = 256 / kLanes;
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void row_stats_kernel(ScoredArgs a, int64_t ro
   const int64_t tile = row / a.B, slot = row - tile * a.B;
   float* const out = a.rows + tile * 2 * a.B + slot;
   out[0] = empty ? __builtin_inff() : (a.cap > 0.f ? lse - a.cap : lse) * kLog2e;
-  out[a.B] = empty ? 0.f : delta;
+  out[a.B] = empty ? 0.f : -delta;
 }
 
 // May any query of q see a key of k?  Does every query that is there see every slot of k?

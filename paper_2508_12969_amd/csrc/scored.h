@@ -113,7 +113,7 @@ struct ScoredArgs : GridArgs {
   // workspace
   float* line;                 // [batch][n][kLineRows][B]: position, document (as an integer), limit; null where no array is given
   TileLine* tiles;             // [batch][n]
-  float* rows;                 // backward: [batch * heads][n][2][B]: log-sum-exp in powers of two, delta (put right by dQ)
+  float* rows;                 // backward: [batch * heads][n][2][B]: log-sum-exp in powers of two, minus delta (put right by dQ)
 };
 
 // bytes of the parts of the workspace, each a multiple of 256
