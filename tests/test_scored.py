@@ -270,6 +270,17 @@ def test_peaked_and_flat_rows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cap", [34.0, 60.0])
+@pytest.mark.parametrize("D", [64, 128])
+def test_all_scores_at_an_end_of_the_cap(cap, D):
+    """Rows whose scores are all near minus the cap, all near the cap, and half each: weights as small as exp(-2 cap)."""
+    pb = Problem((2, 9, 17), (1, 8, 8), 64, D, seed=13, cap=cap, docs="frames")
+    pb.q[:, :, 0::3], pb.q[:, :, 1::3] = 8.0, -8.0
+    pb.k[:], pb.k[:, :, 5::7] = -8.0, 8.0
+    pb.check(*pb.run())
+
+
+@pytest.mark.gpu
 def test_lowest_and_highest_limits_and_far_positions():
     pb = Problem((3, 9, 17), (1, 8, 8), 64, 64, seed=8, prefix="random", bias=True)
     pb.positions[:] = pb.rng.integers(-2 ** 24, 2 ** 24, pb.positions.shape)
