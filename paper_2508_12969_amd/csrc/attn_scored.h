@@ -90,9 +90,9 @@ struct StepCopy {
           "global_load_lds_dwordx4 %[v0], %[sb] offset:0\n\t"
           "global_load_lds_dwordx4 %[v1], %[sb] offset:1024\n\t"
           "global_load_lds_dwordx4 %[v2], %[sb] offset:2048\n\t"
-          "global_load_lds_dwordx4 %[v3], %[sb] offset:3072\n\t"
+          "global_load_lds_dwordx4 %[v3], %[sb] offset:%[o3]\n\t"
           :
-          : [m0] "s"(m0), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [v2] "v"(voff[2]), [v3] "v"(voff[3]), [sb] "s"(sb)
+          : [o3] "n"(3 * 1024), [m0] "s"(m0), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [v2] "v"(voff[2]), [v3] "v"(voff[3]), [sb] "s"(sb)
           : "memory");
     } else if constexpr (S::kLoads == 2) {
       asm volatile(
@@ -309,7 +309,7 @@ struct Softmax {
 // row's sums say what the shift is: `lean` is by how much delta is off, `excess` what rounding added.  dQ is put right at the end by as much of
 // sum2 = sum of (P steep) K, and delta by lean, for dK.  Without a cap excess is the sum of the rounded dS, both in one, and delta is put right by that: what rounding adds to
 // it is small beside the roundings of dK's own dS.  (Relative error of dQ / dK at scores of a spread of 3: 3.6e-3 / 2.7e-3 without, 2.2e-3 / 2.2e-3 with, of which
-// 1.7e-3 is the rounding of the result.  It is one product more, of seven: 36K tokens, dense, forwards not counted, 17.0 / 18.0 ms at head dim 128 and 9.1 / 10.1 at 64.)
+// 1.7e-3 is the rounding of the result.  It is one product more, of seven: 36K tokens, dense, forwards not counted, 17.0 / 17.8 ms at head dim 128 and 9.1 / 9.3 at 64, the latter as it is now.)
 struct RowSums {
   float lean = 0.f, excess = 0.f, weight = 0.f;  // sums of P (dP - delta), of dS rounded less dS, of P steep; without a cap of dS rounded alone
 };
@@ -499,6 +499,10 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   floatx16 minus_delta = splat(!kKeys && kDeltaFirst ? own_delta : 0.f);
   if constexpr (!kForward && !kKeys && kDeltaFirst) asm volatile("" : "+v"(minus_delta));
 
+  // Gradients: a wave that has its weights ready goes before one that still makes them, so that matrix pipe and vector ALU are in use together (without / with: 8K tokens at head
+  // dim 64 1188 / 1127 us, 9K tokens with arrays 1263 / 1224, 20K 3820 / 3800).  Plain calls at head dim 128 are bound by power, and lose 3 % by it; around the products of scores
+  // it gave 0.98 to 1.01, in the forward kernel 0.96 to 1.01.
+  constexpr bool kSumsFirst = S::D == 64 || kLine;
   const StepCopy<S> copy(wave, lane);
   const Fragments<S> frag(lane);
   const uint32_t lds_x = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.x[0], lds_y = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.y[0];
@@ -632,6 +636,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
             bf16x8 p[2], ds[2];
             rounded(s, p);
             rounded(dp, ds);
+            if constexpr (kSumsFirst) __builtin_amdgcn_s_setprio(1);
             if constexpr (kKeys) {
               block_sums<S>(frag, y, b, p, sum2);
               block_sums<S>(frag, x, b, ds, sum1);
@@ -640,6 +645,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
               if constexpr (kCapped) row.weight = sum_of_rounded(p, row.weight);
               block_sums<S>(frag, x, b, ds, sum1, p, sum2);
             }
+            if constexpr (kSumsFirst) __builtin_amdgcn_s_setprio(0);
           }
         }
       }
