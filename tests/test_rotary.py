@@ -469,6 +469,26 @@ def test_a_head_that_is_shared_is_read_in_place():
 
 
 @pytest.mark.gpu
+def test_rows_past_4_gib():
+    """Token strides that lead past 32 bits, of the tensor that is read and of the one that is written."""
+    pb = Problem(((4, 8, 8), (1, 4, 4), 0, 1, 2, 64, "bf16", (16, 24, 24), "half"), 12)
+    gap = 1 << 24   # elements from token to token: 255 * 2^25 bytes
+    source, target = (torch.empty(pb.geom.N_real * gap, dtype=torch.bfloat16, device=DEV).view(1, pb.geom.N_real, gap) for _ in range(2))
+    rows = lambda t: t[:, :, :2 * pb.D].view(1, pb.geom.N_real, 2, pb.D).transpose(1, 2)
+    x, wq, wk = pb.tensor(False), pb.weight(), pb.weight()
+    far = rows(source)
+    far.copy_(x)
+    assert (pb.geom.N_real - 1) * gap * 2 > 2 ** 32
+    assert torch.equal(ca.compact_attn_rotate(far, pb.layout, pb.rotary), ca.compact_attn_rotate(x, pb.layout, pb.rotary))
+    dy = ca.compact_attn_permute(pb.tensor(False), pb.layout)
+    ca.compact_attn_rotate(dy, pb.layout, pb.rotary, transpose=True, out=rows(target))
+    assert torch.equal(rows(target), ca.compact_attn_rotate(dy, pb.layout, pb.rotary, transpose=True))
+    near = ca.compact_attn_norm_rotate_backward(dy, dy, x, x, wq, wk, pb.layout, pb.rotary)
+    got = ca.compact_attn_norm_rotate_backward(dy, dy, far, far, wq, wk, pb.layout, pb.rotary, out=(rows(target), torch.empty_like(x)))
+    assert all(torch.equal(a, b) for a, b in zip(near, got))
+
+
+@pytest.mark.gpu
 def test_long_table_and_far_positions():
     """Positions of 10^6: the angle is as exact as at 0."""
     n, far = 8, 1_000_000

@@ -338,6 +338,33 @@ def test_lists_longer_than_a_cut():
 
 
 @pytest.mark.gpu
+def test_planes_past_4_gib():
+    """Offsets past 32 bits: the last of 40 heads, 5 GiB into every tensor, gives what it gives alone."""
+    grid, tile, heads, D = (64, 64, 128), (1, 8, 8), 40, 128
+    group = [(0, (0, 0), ABSENT)]
+    many, one = (_layout(*grid, tile, 0, 1, [group] * n, D) for n in (heads, 1))
+    N = many.shape(True)[2]
+    assert (heads - 1) * N * D * 2 > 2 ** 32
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(4)
+    last = [torch.randn(1, 1, N, D, generator=gen, device=DEV).to(torch.bfloat16) for _ in range(4)]
+    wide = []
+    for x in last:
+        t = torch.zeros(1, heads, N, D, dtype=torch.bfloat16, device=DEV)
+        t[:, -1:] = x
+        wide.append(t)
+    documents = (torch.arange(N, device=DEV) // 96 % 5).to(torch.int32)[None]
+    for how in (dict(), dict(cap=20.0, documents=documents)):
+        results = []
+        for lay, (q, k, v, do) in ((many, wide), (one, last)):
+            out, lse = ca.compact_attn_forward_scored(q, k, v, lay, **how)
+            results.append((out, lse, *ca.compact_attn_backward_scored(do, q, k, v, out, lse, lay, **how)))
+        for a, b in zip(*results):
+            assert torch.equal(a[:, -1:], b) and bool(torch.isfinite(a[:, -1]).any())
+        del results
+
+
+@pytest.mark.gpu
 def test_side_stream_and_graph():
     """A stream of its own and a captured training step; replays read the arrays that lie there then."""
     pb = Problem(*SHAPES[2], seed=10, **RULES["all"])
