@@ -409,7 +409,7 @@ __device__ __forceinline__ void store_results(const ScoredArgs& a, const ScoreRu
       lean = sum_with_partner(state.lean);
       shift = lean + (weight != 0.f ? excess / weight : 0.f);
     }
-    floatx16 sum[kBlocks];
+    floatx16 sum[kBlocks];  // (changed in place, sum1 would be copied in every step: 20K tokens, forward and backward, 4120 / 3975 us)
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
