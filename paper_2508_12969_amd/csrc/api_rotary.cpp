@@ -134,6 +134,46 @@ int check_apart(const ca_layout* L, const ca_strides* s, const char* name) {
   return CA_OK;
 }
 
+// Do rows of two natural-order tensors that are written share memory?  Both are sums of steps, so the distance of a row of b from one of a is
+// b - a + sum of m * stride over the terms, and a term's m lies in a known range (steps that both have are one term: their difference).  Each term narrows down
+// what the later, shorter ones can still bring to less than a row; where one tensor's rows are nested as the other's, that leaves a few m a term, whatever their number.
+struct Term {
+  int64_t stride, least, most;  // of m
+};
+bool reaches_row(const Term* term, const Term* end, int64_t distance, int64_t row) {
+  if (term == end) return distance > -row && distance < row;
+  int64_t below = 0, above = 0;  // what the terms after this one add
+  for (const Term* t = term + 1; t != end; ++t) below += t->least * t->stride, above += t->most * t->stride;
+  // -row < distance + m stride + above  and  distance + m stride + below < row
+  auto floor_div = [](int64_t x, int64_t by) { return x / by - (x % by < 0); };
+  const int64_t first = std::max(term->least, floor_div(-row - distance - above, term->stride) + 1);
+  const int64_t last = std::min(term->most, floor_div(row - distance - below - 1, term->stride));
+  for (int64_t m = first; m <= last; ++m)
+    if (reaches_row(term + 1, end, distance + m * term->stride, row)) return true;
+  return false;
+}
+bool rows_share_memory(const ca_layout* L, const void* a, const ca::RowStrides& sa, const void* b, const ca::RowStrides& sb) {
+  const ca_problem& p = L->prob;
+  if (!ranges_overlap(a, extent(L, sa, L->N_real), b, extent(L, sb, L->N_real))) return false;
+  const struct {
+    int64_t a, b, count;
+  } steps[] = {{sa.batch, sb.batch, p.batch}, {sa.head, sb.head, p.num_heads}, {sa.token, sb.token, L->N_real}};
+  Term terms[6];
+  int n = 0;
+  for (const auto& s : steps) {
+    if (s.count <= 1) continue;
+    if (s.a == s.b) {
+      terms[n++] = {s.a, 1 - s.count, s.count - 1};
+    } else {
+      terms[n++] = {s.a, 1 - s.count, 0};
+      terms[n++] = {s.b, 0, s.count - 1};
+    }
+  }
+  std::sort(terms, terms + n, [](const Term& x, const Term& y) { return x.stride > y.stride; });
+  const int64_t bytes = static_cast<const char*>(b) - static_cast<const char*>(a);  // (both are 16-byte aligned)
+  return reaches_row(terms, terms + n, bytes / elem_size(p.dtype), p.head_dim);
+}
+
 int check_rows_support(const ca_layout* L) {
   const ca_problem& p = L->prob;
   const int most = p.dtype == CA_BF16 ? 512 : 256;
@@ -372,8 +412,8 @@ int compact_attn_norm_rotate_backward(const ca_norm* m, const void* dq_out, cons
     for (const Range& in : inputs) apart = apart && !ranges_overlap(out.at, out.bytes, in.at, in.bytes);
     if (!apart) return fail(CA_ERR_INVALID_ARG, "results and workspace must not overlap the inputs");
   }
-  // dq and dk may be interleaved in one tensor (strides), so only what surely is the same is refused
-  if (dq == dk) return fail(CA_ERR_INVALID_ARG, "dq and dk must not be the same tensor");
+  // dq and dk may be interleaved in one tensor (strides): their rows count, not what lies between them
+  if (rows_share_memory(L, dq, a.dst_strides, dk, a.dst_strides1)) return fail(CA_ERR_INVALID_ARG, "rows of dq and dk share memory");
   for (int i = 0; i < 5; ++i)
     for (int j = std::max(2, i + 1); j < 5; ++j)
       if (results[i].bytes && results[j].bytes && ranges_overlap(results[i].at, results[i].bytes, results[j].at, results[j].bytes))
