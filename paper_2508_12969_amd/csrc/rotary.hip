@@ -71,6 +71,10 @@ struct Turn {
   float c[kVec], s[kVec];
 };
 
+// What the partner adds.  Nothing where its factor is zero, as it is for channels that nothing turns (in no pair, or of an axis without a position): zero times an
+// infinity would be NaN there, and a zero that is added would lose the sign of another; minus zero does not.
+__device__ __forceinline__ float from_partner(float factor, float partner) { return factor == 0.f ? -0.f : factor * partner; }
+
 template <class T, bool kHalf>
 __device__ __forceinline__ void make_turn(const RowArgs& a, const Part& p, const Token& k, int64_t batch, Turn<Row<T>::kVec>& turn) {
   constexpr int kVec = Row<T>::kVec;
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
       float w[kVec], wp[kVec];
       load_weights<T, kPairing>(a, p, tensor ? a.weight[1] : a.weight[0], w, wp);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) own_c[e] *= w[e], other_c[e] *= wp[e];
+      for (int e = 0; e < kVec; ++e) own_c[e] *= w[e], other_c[e] = from_partner(other_c[e], wp[e]);
     }
     for (int h = h0; h < h1; h += kHeads) {
       Chunk own[kHeads], other[kHeads];
@@ -252,7 +256,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           const float x = (float)own[i][e], xp = kPairing == kNeighbours ? (float)own[i][e ^ 1] : (float)other[i][e];
-          y[e] = (T)(r * (own_c[e] * x + other_c[e] * xp));
+          y[e] = (T)(r * (own_c[e] * x + from_partner(other_c[e], xp)));
         }
         if (!real)
 #pragma unroll
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_backward_kernel(RowArgs a, i
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
             const float xe = live ? (float)x[i][e] : 0.f, dyp = kPairing == kNeighbours ? (float)own[i][e ^ 1] : (float)other[i][e];
-            u[e] = turn.c[e] * (float)own[i][e] + turn.s[e] * dyp;
+            u[e] = turn.c[e] * (float)own[i][e] + from_partner(turn.s[e], dyp);
             squares += xe * xe;
             dot += live ? w[e] * u[e] * xe : 0.f;
           }

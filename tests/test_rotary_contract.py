@@ -1,15 +1,17 @@
 """What the header promises of rotation and norms at the edges of a call: results of the norm's gradients that share memory are refused and those that are only interleaved
-are not."""
+are not; channels that nothing turns are left as they are, bit for bit, whatever their neighbours hold."""
 import ctypes
 import itertools
 import time
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2508_12969_amd as ca
 from paper_2508_12969_amd import rotary as R
 
+DEV = "cuda:0"
 ABSENT = (-1, -1)
 P = [0x100000000 * (i + 1) for i in range(8)]   # addresses that are never read
 
@@ -83,3 +85,105 @@ def test_long_interleaved_gradients_are_told_apart_quickly():
         assert "more rotated channels" in _backward(lay, P[4], strides, P[4] + 2 * apart, strides, table)[1]
     assert "share memory" in _backward(lay, P[4], strides, P[4] + 2 * 128, strides, table)[1]
     assert time.perf_counter() - begin < 0.1   # (rows against rows would be 10^13 comparisons)
+
+
+# ---------------------------------------------------------------- channels that nothing turns
+
+# element type, head dim, rotated channels per axis, pairing: within a lane, between lanes, and halves of an odd number of channels
+ROWS = [("bf16", 64, (8, 20, 20), "interleaved"), ("bf16", 64, (8, 20, 20), "half"), ("bf16", 24, (2, 6, 10), "half"), ("f32", 32, (4, 8, 8), "interleaved"),
+        ("f32", 40, (6, 12, 12), "half")]
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+LENGTHS = (5, 7, 8)
+
+
+class Rows:
+    """Tokens of a grid with text; `still` [batch, 1, tokens, D]: what their positions turn by no angle, of channels in no pair or of an axis without a position."""
+
+    def __init__(self, dtype, D, channels, pairing, explicit):
+        self.gen = torch.Generator().manual_seed(1)
+        self.batch, self.heads, self.D, self.dtype = 2, 3, D, TORCH[dtype]
+        self.layout = _layout(3, 5, 6, (1, 4, 4), 16, self.batch, self.heads, D, dtype)
+        self.rotary = ca.compact_attn_build_rotary(channels, LENGTHS, pairing=pairing, magnitude=1.5)
+        N, n_video = self.layout.n_tokens_real, 3 * 5 * 6
+        if explicit:
+            at = torch.stack([torch.randint(-1, n, (self.batch, N), generator=self.gen) for n in LENGTHS], dim=-1).to(torch.int32)
+            self.how = dict(positions=at.to(DEV))
+        else:
+            at = torch.cat([torch.zeros(n_video, 3), torch.full((16, 3), -1)]).to(torch.int32).expand(self.batch, N, 3)
+            self.how = dict(origin=(1, 2, 0))
+        axis = torch.repeat_interleave(torch.arange(3), torch.tensor(channels) // 2)   # of every pair
+        channel = torch.arange(D)
+        rotated = 2 * len(axis)
+        pair = channel % len(axis) if pairing == "half" else channel // 2
+        axis = torch.where(channel < rotated, axis[pair.clamp(max=len(axis) - 1)], 3)
+        at = torch.cat([at, torch.full_like(at[..., :1], -1)], dim=-1)
+        self.still = (at[..., axis] < 0)[:, None].expand(self.batch, self.heads, N, D).to(DEV)
+        self.shape = (self.batch, self.heads, N, D)
+
+    def tensor(self):
+        return torch.randn(self.shape, generator=self.gen).to(self.dtype).to(DEV)
+
+    def spoil(self, x, values):
+        """Puts `values` at a third of what is left as it is."""
+        hit = (torch.rand(self.shape, generator=self.gen) < 0.33).to(DEV) & self.still
+        which = torch.randint(len(values), self.shape, generator=self.gen).to(DEV)
+        return torch.where(hit, torch.tensor(values, dtype=self.dtype, device=DEV)[which], x)
+
+
+def _bits(x):
+    x = torch.where(torch.isnan(x), torch.full_like(x, float("nan")), x)   # (a NaN is a NaN)
+    return x.view(torch.int16 if x.dtype == torch.bfloat16 else torch.int32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("explicit", [False, True], ids=["grid", "positions"])
+@pytest.mark.parametrize("case", ROWS, ids=lambda c: f"{c[0]}-D{c[1]}-{c[3]}")
+def test_channels_that_are_not_turned_keep_their_bits(case, explicit):
+    """Rotation and its transpose: infinities, NaN and both zeros pass through, and reach no other channel."""
+    print("still channels", case, explicit, flush=True)
+    rows = Rows(*case, explicit)
+    assert rows.still.any() and not rows.still.all()
+    x = rows.tensor()
+    spoilt = rows.spoil(x, [float("inf"), float("-inf"), float("nan"), 0.0, -0.0])
+    for tiled in (False, True):
+        for transpose in (False, True):
+            def run(x):
+                if transpose:
+                    return ca.compact_attn_rotate(ca.compact_attn_permute(x, rows.layout) if tiled else x, rows.layout, rows.rotary, tiled=tiled, transpose=True, **rows.how)
+                y = ca.compact_attn_rotate(x, rows.layout, rows.rotary, tiled=tiled, **rows.how)
+                return ca.compact_attn_permute(y, rows.layout, inverse=True) if tiled else y
+            want, got = run(x), run(spoilt)
+            torch.cuda.synchronize()
+            assert torch.equal(_bits(got)[rows.still], _bits(spoilt)[rows.still]), (tiled, transpose)
+            assert torch.equal(_bits(got)[~rows.still], _bits(want)[~rows.still]), (tiled, transpose)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", ROWS, ids=lambda c: f"{c[0]}-D{c[1]}-{c[3]}")
+def test_norms_of_channels_that_are_not_turned(case):
+    """A weight or a gradient that is not finite reaches its own channel of what is not turned, and no neighbour; zeros keep their signs."""
+    print("still channels, norm", case, flush=True)
+    rows = Rows(*case, False)
+    x, dy = rows.spoil(rows.tensor(), [0.0, -0.0]), rows.tensor()
+    weight = torch.ones(rows.D, dtype=rows.dtype, device=DEV)
+    weight[1::4] = -1.0
+    run = lambda w: ca.compact_attn_norm_rotate(x, x, w, None, rows.layout, rows.rotary, tiled=False, **rows.how)[0]
+    plain = run(weight)
+    zero = rows.still & (x == 0)
+    assert zero.any() and torch.equal(torch.signbit(plain[zero]), torch.signbit((x * weight)[zero]))
+    for bad in (0, rows.D - 1):
+        spoilt = weight.clone()
+        spoilt[bad] = float("nan")
+        got = run(spoilt)
+        own = torch.zeros_like(rows.still)
+        own[..., bad] = True
+        assert torch.isnan(got[own]).all()
+        keep = rows.still & ~own
+        assert torch.equal(_bits(got)[keep], _bits(plain)[keep])
+        # a text token's gradient: nothing of it is turned
+        spoilt = dy.clone()
+        spoilt[0, 0, -1, bad] = float("nan")
+        back = lambda dy: ca.compact_attn_norm_rotate_backward(dy, dy, x, x, weight, None, rows.layout, rows.rotary, tiled=False, **rows.how)[2]
+        want, got = back(dy), back(spoilt)
+        channel = torch.arange(rows.D, device=DEV)
+        assert torch.isnan(got[bad]) and torch.equal(got[channel != bad], want[channel != bad])
