@@ -176,7 +176,7 @@ __device__ __forceinline__ void cap_scores(const ScoreRule& rule, floatx16& s) {
   for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
 }
 
-// Masks the padding slots of a block of 32 streamed keys (no arrays given), as QueryWave::mask_padding_keys does.
+// Masks the padding slots of a block of 32 streamed tokens where pairs are not compared, as QueryWave::mask_padding_keys does.
 __device__ __forceinline__ void mask_slots(floatx16& s, uint32_t bits, float hidden) {
   if (bits == 0xffffffffu) return;
 #pragma unroll
@@ -605,7 +605,8 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
             if constexpr (kCapped) cap_scores(rule, s);
             constexpr float kHidden = kCapped ? -1e18f : kMinusInf;  // (no weight either way; its square is finite, for steep)
             if (kLine && compare) hide_scores<S, K>(s, info, first_block + b, g, own.pos, own.doc, own.limit, kHidden);
-            if (!kKeys && cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]), kHidden);
+            // (padding queries too, whose weights are zero with any score but NaN: their zeros times an infinite key)
+            if (cls != 0) mask_slots(s, __builtin_amdgcn_readfirstlane(valid[b]), kHidden);
             // s -> P (dQ: P steep), dp -> dS.  One value at a time, so that nothing else is held: steep = 1 - tanh^2 = -4 x (1 + x) is made from x when it is used, its -4 is left to the
             // results (gradient_factor), the bias goes into the exponent.
             auto weigh = [&](auto biased) {
