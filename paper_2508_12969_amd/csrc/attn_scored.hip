@@ -137,8 +137,8 @@ __global__ __launch_bounds__(kVisitThreads) void visit_kernel(ScoredArgs a, Visi
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         if (!(v.keys ? any_visible(other, own[t]) : any_visible(own[t], other))) members &= ~(1u << t);
-        // (queries that are not there have no weights, whatever they are compared with)
-        const bool all = v.keys ? all_visible(other, own[t]) : other.whole && all_visible(own[t], other);
+        // (streamed tokens that are not there are compared, so that an infinite token of the group's meets none of their values; the group's own write zeros)
+        const bool all = other.whole && (v.keys ? all_visible(other, own[t]) : all_visible(own[t], other));
         compare = compare || ((members >> t & 1) != 0 && !all);
       }
       word = (word & 0x1fffffffu) | (compare ? 1u << 29 : 0u) | members << 30;

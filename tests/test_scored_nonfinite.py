@@ -184,3 +184,25 @@ def test_hidden_tokens_may_hold_the_largest_finite_values(kernel):
             assert all(torch.equal(a, b) for a, b in zip(results[0], other)), cap
         assert (results[0][0][:, hidden] == 0).all() and (results[0][1][:, hidden] == -INF).all()
         assert all((g[:, hidden] == 0).all() for g in results[0][2:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS, ids=ids)
+def test_an_infinite_key_beside_queries_that_are_not_there(kernel):
+    """Queries of no document are zero where a key is infinite: they have no part in its gradients, whether or not pairs of their tile are hidden for another reason."""
+    print("infinite key, hidden queries", kernel, flush=True)
+    pb = Step(*kernel)
+    token = pb.N // 2
+    hidden = torch.arange(pb.N, device=DEV) % 5 == (token + 3) % 5
+    documents = torch.where(hidden, -4, 0).to(torch.int32)[None]
+    q = pb.q.clone()
+    q[..., 0] = -1                                 # the key's scores are minus infinity
+    q[:, :, hidden] = 0
+    frames = (torch.arange(pb.N, device=DEV) // 260).to(torch.int32)[None]
+    for how in (dict(documents=documents), dict(documents=documents, positions=frames, limits=frames), dict(documents=documents, cap=6.0)):
+        pb.how = how
+        out, lse, _, _, dv = pb.run(q=q, k=pb.changed("k", token, INF, 0))
+        there = ~hidden
+        assert torch.isfinite(out).all() and torch.isfinite(lse[:, there]).all() and torch.isfinite(dv).all()
+        if not how.get("cap"):
+            assert (dv[:, token] == 0).all()
