@@ -468,16 +468,18 @@ int compact_attn_norm_rotate_backward(const ca_norm* norm, const void* dq_out, c
  *              of their own number; one below 0 is not there (a padded prompt): it sees and is seen by none.  Positions and limits of magnitude up
  *              to 2^24 are exact, others are rounded to float.
  * A query that sees no key has a zero result, log-sum-exp minus infinity, and no part in any gradient.  Values of tokens that are not seen must still be
- * finite, and padding slots zero, as compact_attn_permute leaves them.  The arrays are read on the device at every call. */
+ * finite, and padding slots zero, as compact_attn_permute leaves them; those of tokens that are seen may be infinite or NaN, and reach what depends on them.  The arrays are read on the device at every call. */
 typedef struct {
   float cap;
   const float* slopes;
   const int32_t *positions, *limits, *documents;
 } ca_scores;
 
-/* Bytes of device memory that a forward (backward = 0) or a backward call needs; 0 where it has no use for any: the token arrays in tile order, two floats
- * for a query (backward), and at most 140 MB for partial sums where long lists are shared by several workgroups.  The first call for a layout makes the
- * lists that scored attention walks over, on the host. */
+/* Bytes of device memory that a forward (backward = 0) or a backward call needs; 0 where it has no use for any: the token arrays in tile order (arrays but positions alone),
+ * two floats for a query (backward), at most 140 MB for partial sums where long lists are shared by several workgroups, and with limits or documents the lists that the call walks
+ * over: for every batch entry 4 bytes for each 64 keys that a group of 128 queries has in its lists, backward also for each 64 queries of a group of 128 keys (130K tokens,
+ * 24 heads: 143 MB forward and 304 backward in all at 35 % kept tiles, 269 and 556 with all kept).  The first call for a layout makes the lists that scored attention walks over,
+ * on the host, where the layout keeps them. */
 int compact_attn_scored_workspace(ca_layout* layout, const ca_scores* scores, int32_t backward, int64_t* workspace_bytes);
 
 /* Copies these lists to the current device, those of backward calls too if backward is 1.  Synchronous; idempotent.  The calls do it on first use
@@ -496,7 +498,9 @@ int compact_attn_forward_scored(const void* q, const void* k, const void* v, ca_
 
 /* Gradients dq, dk, dv (tile order, bf16, padding rows zero) for the gradient dout of out, from the forward call's inputs and results and the same scores.
  * dout: tile order, padding slots zero.  Weights and score gradients are rounded to bf16 as operands of the products, sums are fp32 in a fixed order.
- * Slopes and positions get no gradient. */
+ * out and lse must be what compact_attn_forward_scored gave for these very inputs: a row's gradients are put right by the knowledge that its weights add up to one over the keys of this
+ * call.  Results that were merged from calls on several sets of keys do not satisfy that, and give wrong dq and dk without an error.  lse takes no gradient of its own;
+ * slopes and positions get none. */
 int compact_attn_backward_scored(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, ca_layout* layout,
                                  const ca_scores* scores, void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes, void* stream);
 

@@ -500,7 +500,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(S::kThreads, S::kThreads),
   if constexpr (!kForward && !kKeys && kDeltaFirst) asm volatile("" : "+v"(minus_delta));
 
   // Gradients: a wave that has its weights ready goes before one that still makes them, so that matrix pipe and vector ALU are in use together (without / with: 8K tokens at head
-  // dim 64 1188 / 1127 us, 9K tokens with arrays 1263 / 1224, 20K 3820 / 3800).  Plain calls at head dim 128 are bound by power, and lose 3 % by it; around the products of scores
+  // dim 64 1241 / 1183 us, 9K tokens with arrays 1273 / 1243, 20K 3944 / 3878).  Plain calls at head dim 128 are bound by power, and lose 3 % by it; around the products of scores
   // it gave 0.98 to 1.01, in the forward kernel 0.96 to 1.01.
   constexpr bool kSumsFirst = S::D == 64 || kLine;
   const StepCopy<S> copy(wave, lane);

@@ -195,7 +195,8 @@ __device__ __forceinline__ void load_weights(const RowArgs& a, const Part& p, co
 // kHeads: rows that are loaded before the first of them is computed (2 / 4 / 8: 20K tokens x 24 rows of 64 channels, forward and gradients 157 / 151 / 149 us; fp32, 7K
 // tokens x 16 rows 30 / 28 / 30 us).  Results are stored past the caches, inputs loaded through them; inputs that lie in no cache, stores through / past / both past the caches:
 // 33K tokens x 16 heads of 128 64.6 / 61.3 / 59.7 us, 2 x 20K x 12 of 80 42.1 / 36.9 / 44.0, fp32 7K x 16 of 128 33.7 / 27.7 / 34.8 (4.9, 4.6 and 4.7 TB/s as they are); q and k of 75.6K
-// tokens x 40 heads, tokens first, 640 us = 5.0 TB/s (a plain copy of 1 GiB: 4.8 to 5.05 TB/s).
+// tokens x 40 heads, tokens first, 640 us = 5.0 TB/s (a plain copy of 1 GiB: 4.8 to 5.1 TB/s; permute_kernel on such a tensor 6.0 TB/s).  All of these are times of the operator alone: what
+// attention, which reads the results next, has of them in the caches either way was not measured.
 template <class T, Pairing kPairing, bool kNorm, bool kBack>
 __global__ __launch_bounds__(kRowThreads) void rows_kernel(RowArgs a, int heads_per_block) {
   constexpr int kVec = Row<T>::kVec, kHeads = 4;

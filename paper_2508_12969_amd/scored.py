@@ -74,7 +74,7 @@ def compact_attn_forward_scored(q, k, v, layout, cap=0.0, slopes=None, positions
 
 def compact_attn_backward_scored(dout, q, k, v, out, lse, layout, cap=0.0, slopes=None, positions=None, limits=None, documents=None, grads=None, stream=None):
     """Gradients (dq, dk, dv) of compact_attn_forward_scored for the gradient dout of its first result, from its inputs and results and the same scores; all in tile
-    order.  grads: three tensors to write to."""
+    order.  out and lse as that call left them, not merged from several (compact_attn.h); lse has no gradient.  grads: three tensors to write to."""
     for name, t in (("dout", dout), ("q", q), ("k", k), ("v", v), ("out", out)):
         _check_tiles(t, layout, name)
     _check_lse(lse, layout, "lse")

@@ -84,7 +84,7 @@ def test_long_interleaved_gradients_are_told_apart_quickly():
     for apart in (24 * 128, 2 * 24 * 128):
         assert "more rotated channels" in _backward(lay, P[4], strides, P[4] + 2 * apart, strides, table)[1]
     assert "share memory" in _backward(lay, P[4], strides, P[4] + 2 * 128, strides, table)[1]
-    assert time.perf_counter() - begin < 0.1   # (rows against rows would be 10^13 comparisons)
+    assert time.perf_counter() - begin < 1   # (rows against rows would be 10^13 comparisons)
 
 
 # ---------------------------------------------------------------- channels that nothing turns
