@@ -210,18 +210,10 @@ int fill_rows(ca::RowArgs& a, const ca_layout* L, ca_rotary* r, const ca_where* 
       }
     }
   }
-  const int st = ensure_rotary_uploaded(r, stream);
+  const int st = ca::fill_rotation(a, r, stream);
   if (st != CA_OK) return st;
-  a.angles = r->dev;
-  a.half = r->pairing == CA_PAIRS_HALF;
-  a.rotated = r->channels;
   a.where = where ? where->positions : nullptr;
-  for (int i = 0; i < 3; ++i) {
-    a.first[i] = r->first[i];
-    a.pairs[i] = r->axes[i].channels / 2;
-    a.positions[i] = r->axes[i].positions;
-    a.origin[i] = where && r->axes[i].channels ? where->origin[i] : 0;
-  }
+  for (int i = 0; i < 3; ++i) a.origin[i] = where && r->axes[i].channels ? where->origin[i] : 0;
   return CA_OK;
 }
 
@@ -248,6 +240,20 @@ bool overlaps_small_inputs(const ca_layout* L, const void* at, int64_t bytes, co
 int64_t plane_elements(const ca_layout* L) { return (int64_t)L->prob.batch * L->prob.num_heads * L->prob.head_dim; }
 
 }  // namespace
+
+int ca::fill_rotation(RowRule& a, ca_rotary* r, hipStream_t stream) {
+  const int st = ensure_rotary_uploaded(r, stream);
+  if (st != CA_OK) return st;
+  a.angles = r->dev;
+  a.half = r->pairing == CA_PAIRS_HALF;
+  a.rotated = r->channels;
+  for (int i = 0; i < 3; ++i) {
+    a.first[i] = r->first[i];
+    a.pairs[i] = r->axes[i].channels / 2;
+    a.positions[i] = r->axes[i].positions;
+  }
+  return CA_OK;
+}
 
 extern "C" {
 

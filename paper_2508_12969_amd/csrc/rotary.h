@@ -31,8 +31,21 @@ struct RowStrides {
   int64_t batch, head, token;  // elements
 };
 
+// What is done with a row of D channels.
+struct RowRule {
+  int32_t D;
+  float eps;
+  // rotation
+  const float* angles;         // (cos, sin) pairs; null: no rotation
+  int64_t first[3];
+  int32_t pairs[3], positions[3];
+  int32_t half;                // pairing: channels i and i + rotated/2
+  int32_t rotated;
+  float sign;                  // of the sine: -1 turns back
+};
+
 // One launch over the rows (token, head) of one or two tensors.
-struct RowArgs : GridArgs {  // rows are walked in the order of dst, which is in tile order (tiled forward) or in natural order
+struct RowArgs : GridArgs, RowRule {  // rows are walked in the order of dst, which is in tile order (tiled forward) or in natural order
   const void* src[2];
   void* dst[2];
   const void* x[2];            // norm, backward: the forward call's inputs
@@ -40,19 +53,14 @@ struct RowArgs : GridArgs {  // rows are walked in the order of dst, which is in
   const void* weight[2];       // null: ones
   float* partial;              // norm, backward: [workgroups][tensors][D], or null
   float* dweight[2];
-  float eps;
-  int32_t tensors, batch, heads, D;
+  int32_t tensors, batch, heads;
   int32_t tiled;               // the tensor that is not the model's own is in tile order: dst of forward, src of backward calls
-  // rotation
-  const float* angles;         // (cos, sin) pairs; null: no rotation
-  int64_t first[3];
-  int32_t pairs[3], positions[3];
-  int32_t half;                // pairing: channels i and i + rotated/2
-  int32_t rotated;
   int32_t origin[3];
   const int32_t* where;        // [batch][N_real][3] or null
-  float sign;                  // of the sine: -1 turns back
 };
+
+// The rotation part of a rule; puts the table on the current device at its first use (api_rotary.cpp).
+int fill_rotation(RowRule& a, ca_rotary* r, hipStream_t stream);
 
 hipError_t launch_rotate(const RowArgs& a, bool bf16, bool backward, hipStream_t stream);
 hipError_t launch_norm_rotate(const RowArgs& a, bool bf16, hipStream_t stream);
