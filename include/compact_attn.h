@@ -504,6 +504,90 @@ int compact_attn_forward_scored(const void* q, const void* k, const void* v, ca_
 int compact_attn_backward_scored(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, ca_layout* layout,
                                  const ca_scores* scores, void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- A paged cache of keys and values -------------------------------------------------------------------------
+ *
+ * For models that are causal over their frames (or tokens) and make them one after another: keys and values of what came before are kept in pages, those of new tokens
+ * are appended, and queries of the new tokens attend to all of it.  No layout is involved; tokens are in the order in which they came.
+ *
+ * A cache holds several sequences.  Token j of sequence s lies in slot j % page_tokens of page table[s][j / page_tokens].  A table entry that is no page's number (below 0, or num_pages and
+ * more) stands for tokens that are not there: nothing is read or written for them, and they are seen by none.  So entries past a sequence's end may be -1, and pages
+ * of a far past may be given up.
+ *
+ * Frames: the first origins[s] tokens of a sequence are its prompt, the tokens behind it stand in frames of frame_height x frame_width tokens, row by row (1 x 1: every token is a frame).
+ *
+ * A call brings new tokens, the last ones of their sequences: rows starts[s] .. starts[s + 1] - 1 of the call's packed tensors are the last tokens of sequence s, of which there are
+ * lengths[s] with them.  starts ascends from 0 to at most `tokens`; rows behind the last sequence belong to none, and results there are left as they were.  A sequence may have no new
+ * token.  A row whose token would have a number below 0 (more new tokens than the sequence has) or past the table is neither stored nor does it see anything.
+ *
+ * table, lengths, starts and origins are device memory, 4-byte aligned, and are read on the device at every call: a captured call goes by what lies there when it is replayed.  Numbers
+ * out of range are cut off on the device; nothing is read or written outside of the tensors. */
+typedef struct {
+  void *k, *v;                                  /* pages: [num_pages][kv_heads][page_tokens][head_dim], 16-byte aligned */
+  int64_t num_pages;                            /* up to 2^31 - 1 */
+  int32_t page_tokens;                          /* a multiple of 16, up to 65536 */
+  int32_t kv_heads, head_dim, dtype;            /* ca_dtype */
+  int32_t sequences, table_width;               /* table_width * page_tokens up to 2^30 */
+  const int32_t* table;                         /* [sequences][table_width] */
+  const int32_t* lengths;                       /* [sequences] */
+  const int32_t* starts;                        /* [sequences + 1] */
+  const int32_t* origins;                       /* [sequences], or NULL: no prompts */
+  int32_t tokens;                               /* rows of the packed tensors */
+  int32_t frame_height, frame_width;            /* their product up to 2^30 */
+} ca_cache;
+
+/* What is appended.  q, k, v: [tokens, heads or kv_heads, head_dim]; strides in elements, channels contiguous, every row 16-byte aligned (batch is not read; NULL: contiguous). */
+typedef struct {
+  const void *q, *k, *v;                               /* q may be NULL, with q_out */
+  const ca_strides *q_strides, *k_strides, *v_strides;
+  void* q_out;                                         /* [tokens, heads, head_dim], contiguous */
+  int32_t heads;                                       /* of q */
+  int32_t normed;                                      /* 1: norm of every query and key head, as compact_attn_norm_rotate */
+  const void *q_weight, *k_weight;                     /* [head_dim] of the cache's type, 16-byte aligned; NULL: ones */
+  float eps;                                           /* >= 0 */
+  ca_rotary* rotary;                                   /* NULL: no rotation */
+  const ca_where* where;                               /* NULL: origin 0, no positions */
+} ca_append;
+
+/* Stores keys and values of new tokens in their pages, keys with norm and rotation, and writes the queries with theirs to q_out, in one pass:
+ *   k' = R(p) (w * k * (mean(k^2) + eps)^-1/2),  q' likewise,  v as it is.
+ * Positions: where->positions (int32[tokens][3], as compact_attn_rotate), or else where->origin + (frame, row, column) of the token; prompts are not rotated then.  A position past the
+ * rotary table gives NaN.  Sums are fp32, results rounded once.  A page that is written must be in one place of the table only.  bf16 and f32; head_dim up to 512 (bf16) or 256
+ * (f32), CA_ERR_UNSUPPORTED beyond.  q_out and the pages must not overlap the inputs or each other. */
+int compact_attn_cache_append(const ca_append* append, const ca_cache* cache, void* stream);
+
+/* How scores are bent and what is seen, as in ca_scores.
+ *   s = scale * q.k;  s = cap * tanh(s / cap);  s = s - slope[head] * |frame_q - frame_k|        (a prompt's frame is -1; frames up to 2^24 are exact)
+ * A query sees the tokens of its sequence that are in the prompt, and of the others
+ *   causal = 1   those of its own and earlier frames (all of its own frame; a prompt's query: the prompt);  causal = 0: all
+ *   window > 0   only those with frame_k > frame_q - window
+ * tree: the new tokens are drafts in a tree, of which bit j of tree[row] says that the row sees its sequence's new token j (j < 64, its own bit included; a 65th new token is seen by
+ * none; bits past the sequence's new tokens are not read).  These bits alone decide among the new tokens.  A draft stands as many tokens behind the last one that is not new as bits are set, whatever its row: its frame, for distances and
+ * windows, is the one of that place.  tree is device memory, uint64[tokens], 8-byte aligned, or NULL. */
+typedef struct {
+  float scale;          /* <= 0: head_dim^-1/2 */
+  float cap;            /* 0 (none) or 2^-16 to 4096 */
+  const float* slopes;  /* device, [heads], or NULL */
+  int32_t causal, window;
+  const uint64_t* tree;
+} ca_reach;
+
+/* Bytes of device memory that compact_attn_cache_attend needs for a call of these sizes. */
+int compact_attn_cache_workspace(const ca_cache* cache, int32_t heads, int64_t* workspace_bytes);
+
+/* out, lse = softmax(scores) v and log of the sum of exp(scores), of the new tokens' queries over the cache.
+ *   q          [tokens, heads, head_dim], strides as in ca_append; heads is a multiple of kv_heads, and query heads h * heads / kv_heads .. of a key head h are neighbours.
+ *   out, lse   [tokens, heads, head_dim] of the cache's type and float [tokens, heads], contiguous.  A row that sees nothing has a zero result and minus infinity.
+ *   workspace  16-byte aligned, not overlapping the tensors; must not be used by anything else until the call's work on `stream` has run.
+ * Tokens below a sequence's length must have finite values unless all rows of their sequence see them; slots that hold no token may hold anything.  Weights are rounded to
+ * bf16 before the product with v, sums are fp32 in an order that depends on the sizes and lengths alone.  bf16 with head_dim 64 and 128, otherwise CA_ERR_UNSUPPORTED. */
+int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_t heads, const ca_cache* cache, const ca_reach* reach, void* out, float* lse, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
+/* Keeps some of the new tokens, the accepted path of a tree of drafts: new token kept[s][j] of sequence s becomes new token j, for j below counts[s], in the pages.  The program then goes
+ * on with lengths[s] less the others.  kept: int32 [sequences][width], width up to 64; counts: int32 [sequences]; device memory.  Everything is read before it is written, so any order of
+ * kept is right; an entry that is no new token's number leaves its target as it was.  f32 and bf16, head_dim as compact_attn_cache_append. */
+int compact_attn_cache_keep(const ca_cache* cache, const int32_t* kept, int32_t width, const int32_t* counts, void* stream);
+
 /* Message of the last failure on the calling thread ("" if none); valid until the next call. */
 const char* compact_attn_last_error(void);
 

@@ -46,3 +46,9 @@ from .scored import (  # noqa: F401
     compact_attn_forward_scored,
     compact_attn_layout_upload_scored,
 )
+from .cache import (  # noqa: F401
+    Cache,
+    compact_attn_cache_append,
+    compact_attn_cache_attend,
+    compact_attn_cache_keep,
+)

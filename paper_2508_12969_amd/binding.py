@@ -61,6 +61,10 @@ EXPORTED = (
     "compact_attn_forward_scored",
     "compact_attn_layout_upload_scored",
     "compact_attn_backward_scored",
+    "compact_attn_cache_append",
+    "compact_attn_cache_workspace",
+    "compact_attn_cache_attend",
+    "compact_attn_cache_keep",
     "compact_attn_last_error",
 )
 

@@ -1,0 +1,246 @@
+// Attention of new tokens over a paged cache, on the bf16 matrix instructions.
+//
+//   s = scale q.k;  s = cap tanh(s / cap);  s -= slope |frame_q - frame_k|;  O = softmax(s) V,  L = log sum exp s
+//
+// The rows of a sequence and a key head are its new tokens times the query heads that share the key head, token by token.  A wave owns 32 of them, one a lane: they are the columns of
+// S^T = K Q^T and O^T += V^T P^T (as in attn_scored.h, whose fragments and products these are), so that a row's maximum and sum stay in its lane and the rounded weights are, register for
+// register, the second product's operand.  Keys and values stream through LDS in steps of 32 tokens a wave or 64 a workgroup, copied straight from the pages: 16 rows of a page, a
+// "slice", are one contiguous piece whatever the page length.
+//
+// What a row sees of its sequence is the prompt and a range lo <= token < hi that follows from its frame, and among drafts the bits of its word.  So the steps that a tile of rows walks are two runs in closed form
+// (Walk), without a list, and only steps at the ends of a range compare anything.
+#pragma once
+
+#include "attn_scored.h"
+#include "cache_tokens.h"
+
+namespace ca {
+namespace {
+
+constexpr int kSlice = 16;  // tokens
+
+template <int D_>
+struct CacheShape {
+  static constexpr int D = D_;
+  static constexpr int kRowBytes = D * 2, kChunksPerRow = D / 8, kRowsPerLoad = 1024 / kRowBytes;
+  static constexpr int kSliceLoads = kSlice / kRowsPerLoad;  // wave-wide copies of a slice
+  static constexpr int kSliceBytes = kSlice * kRowBytes;
+  static constexpr int kContraction = D / 16, kDBlocks = D / 32;
+};
+
+// Bits of a draft, of the new tokens that there are; and where it stands.
+__device__ __forceinline__ uint64_t draft_bits(const AttendArgs& a, const Sequence& q, int32_t row) {
+  const uint64_t bits = a.tree[row];
+  return q.count < kMostDrafts ? bits & (((uint64_t)1 << q.count) - 1) : bits;
+}
+__device__ __forceinline__ int32_t draft_place(const Sequence& q, uint64_t bits) { return max(q.base + max((int)__popcll(bits), 1) - 1, 0); }
+
+// What rows at a place of their sequence see.
+struct View {
+  int32_t lo, hi;  // behind the prompt
+  int32_t frame;
+};
+__device__ __forceinline__ int32_t frame_at(const CacheArgs& a, const Sequence& q, int32_t place) { return place < q.origin ? -1 : (place - q.origin) / a.span; }
+__device__ __forceinline__ View view_at(const AttendArgs& a, const Sequence& q, int32_t place) {
+  View v;
+  v.frame = frame_at(a, q, place);
+  const int64_t end = a.causal ? q.origin + (v.frame + (int64_t)1) * a.span : q.length;
+  const int64_t begin = a.window && v.frame >= a.window ? q.origin + ((int64_t)v.frame - a.window + 1) * a.span : q.origin;
+  v.hi = (int32_t)min(end, (int64_t)q.length);
+  v.lo = (int32_t)min(begin, (int64_t)q.length);
+  return v;
+}
+
+// Tokens of a prompt that are seen as such (a draft is not, wherever it lies).
+__device__ __forceinline__ int32_t prompt_end(const AttendArgs& a, const Sequence& q) { return a.tree ? max(0, min(q.origin, q.base)) : q.origin; }
+
+// Steps of kStep tokens that a tile of rows walks over: those of the prompt, then those of all its rows' ranges.
+template <int kStep>
+struct Walk {
+  int32_t prompt, jump, count;  // steps of the prompt; what is added to the number of a later one; all
+  __device__ __forceinline__ int32_t token(int32_t step) const { return (step + (step < prompt ? 0 : jump)) * kStep; }
+};
+template <int kStep>
+__device__ __forceinline__ Walk<kStep> walk_of(const AttendArgs& a, const Sequence& q, int32_t first_token, int32_t last_token) {
+  const int32_t least = max(q.base + (a.tree ? 0 : first_token), 0), most = a.tree ? q.length - 1 : q.base + last_token;
+  const View low = view_at(a, q, least), high = view_at(a, q, most);
+  const int32_t hi = a.tree ? q.length : high.hi;
+  Walk<kStep> w;
+  w.prompt = (prompt_end(a, q) + kStep - 1) / kStep;
+  const int32_t from = max(w.prompt, min(low.lo, a.tree ? max(q.base, 0) : low.lo) / kStep), to = (hi + kStep - 1) / kStep;
+  w.jump = from - w.prompt;
+  w.count = most < 0 ? 0 : w.prompt + max(0, to - from);
+  return w;
+}
+
+// Finds the sequence in which `target` lies when every sequence takes up weight(sequence) places, and how far behind its first place.  All threads call it; false: there are fewer places.
+struct LocateLds {
+  int64_t waves[16], rest, all;
+  int32_t sequence;
+};
+template <int kThreads, class Weight>
+__device__ __forceinline__ bool locate(const CacheArgs& a, int64_t target, LocateLds& lds, int32_t& sequence, int64_t& rest, int64_t& all, Weight&& weight) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t per = ((int64_t)a.sequences + kThreads - 1) / kThreads;
+  const int32_t from = (int32_t)min(tid * per, (int64_t)a.sequences), to = (int32_t)min(from + per, (int64_t)a.sequences);
+  int64_t own = 0;
+  for (int32_t s = from; s < to; ++s) own += weight(sequence_at(a, s));
+  int64_t up = own;
+#pragma unroll
+  for (int step = 1; step < 64; step *= 2) {
+    const int64_t other = __shfl_up(up, step);
+    if (lane >= step) up += other;
+  }
+  if (lane == 63) lds.waves[wave] = up;
+  if (tid == 0) lds.sequence = -1;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) before += lds.waves[w];
+    total += lds.waves[w];
+  }
+  int64_t at = before + up - own;
+  if (target >= at && target < at + own) {
+    for (int32_t s = from; s < to; ++s) {
+      const int64_t w = weight(sequence_at(a, s));
+      if (target < at + w) {
+        lds.sequence = s;
+        lds.rest = target - at;
+        break;
+      }
+      at += w;
+    }
+  }
+  __syncthreads();
+  sequence = __builtin_amdgcn_readfirstlane(lds.sequence);
+  const int64_t r = lds.rest;
+  rest = (int64_t)((uint64_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)r >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)r));
+  all = total;
+  return sequence >= 0;
+}
+
+__device__ __forceinline__ int32_t row_tiles(const AttendArgs& a, const Sequence& q, int rows) { return (int32_t)(((int64_t)q.count * a.group + rows - 1) / rows); }
+
+// The unit of scores, see ScoreRule; a lane's query head has its own slope.
+struct CacheRule {
+  float bend, c2, offset;
+  bool capped;
+  __device__ __forceinline__ explicit CacheRule(const AttendArgs& a) {
+    capped = a.cap > 0.f;
+    bend = capped ? 2.f * a.scale * kLog2e / a.cap : 0.f;
+    c2 = (capped ? 2.f * a.cap : a.scale) * kLog2e;
+    offset = capped ? a.cap * kLog2e : 0.f;
+  }
+};
+
+// A lane's row.
+struct CacheRow {
+  int32_t row;        // of the packed tensors; -1: there is none
+  int32_t head;       // of the query
+  View view;          // nothing where it has no place
+  int32_t prompt;     // what it sees of it
+  uint64_t drafts;
+  float slope;        // in units of the scores, negative
+  __device__ __forceinline__ CacheRow(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int64_t index) {
+    const int32_t i = (int32_t)(index / a.group);
+    head = key_head * a.group + (int32_t)(index - (int64_t)i * a.group);
+    row = i < q.count ? q.first + i : -1;
+    const bool there = row >= 0 && q.base + i >= 0;
+    drafts = there && a.tree ? draft_bits(a, q, row) : 0;
+    view = view_at(a, q, !there ? 0 : a.tree ? draft_place(q, drafts) : q.base + i);
+    prompt = prompt_end(a, q);
+    if (a.tree) view.hi = min(view.hi, max(q.base, 0));
+    if (!there) view.lo = view.hi = prompt = 0;
+    slope = a.slopes ? -a.slopes[head] / (rule.capped ? 2.f * a.cap : a.scale) : 0.f;
+  }
+};
+
+// Copies a slice (16 rows of a page) into LDS, asynchronously; logical chunks lie where swizzle() puts them.
+template <class S>
+struct SliceCopy {
+  uint32_t voff[S::kSliceLoads];
+  __device__ __forceinline__ explicit SliceCopy(int lane) {
+#pragma unroll
+    for (int i = 0; i < S::kSliceLoads; ++i) {
+      const int within = lane / S::kChunksPerRow, phys = lane % S::kChunksPerRow;
+      voff[i] = (uint32_t)(within * S::kRowBytes + ((phys ^ swizzle<S::D>(i * S::kRowsPerLoad + within)) << 4));
+    }
+  }
+  __device__ __forceinline__ void operator()(const char* slice, uint32_t lds) const {
+    const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
+    if constexpr (S::kSliceLoads == 4) {
+      asm volatile(
+          "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
+          "global_load_lds_dwordx4 %[v0], %[sb] offset:0\n\t"
+          "global_load_lds_dwordx4 %[v1], %[sb] offset:1024\n\t"
+          "global_load_lds_dwordx4 %[v2], %[sb] offset:2048\n\t"
+          "global_load_lds_dwordx4 %[v3], %[sb] offset:%[o3]\n\t"
+          :
+          : [o3] "n"(3 * 1024), [m0] "s"(m0), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [v2] "v"(voff[2]), [v3] "v"(voff[3]), [sb] "s"(slice)
+          : "memory");
+    } else {
+      static_assert(S::kSliceLoads == 2, "copies are written for two or four loads");
+      asm volatile(
+          "s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
+          "global_load_lds_dwordx4 %[v0], %[sb] offset:0\n\t"
+          "global_load_lds_dwordx4 %[v1], %[sb] offset:1024\n\t"
+          :
+          : [m0] "s"(m0), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [sb] "s"(slice)
+          : "memory");
+    }
+  }
+};
+
+// Where the slices of the next 64 / kSlices steps lie, one a lane; fetched by all lanes at once.
+template <int kSlices, int kStep>
+struct SlicePlaces {
+  int32_t first = 0;      // step of lane 0
+  int64_t offset = 0;     // bytes; of a slice that is not there: 0, a place that can be read
+  uint64_t there = 0;     // a bit a lane
+  static constexpr int kSteps = 64 / kSlices;
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const Sequence& q, int32_t s, int32_t head, const Walk<kStep>& w, int32_t step, int32_t end, int lane, int row_bytes) {
+    first = step;
+    const int32_t mine = step + lane / kSlices;
+    const int64_t token = mine < end ? (int64_t)w.token(mine) + lane % kSlices * kSlice : q.length;
+    const int32_t page = token < q.length ? page_at(a, s, (int32_t)token) : -1;
+    offset = page >= 0 ? cache_row(a, page, head, (int32_t)token % a.page_tokens) * row_bytes : 0;
+    there = __builtin_amdgcn_ballot_w64(page >= 0);
+  }
+  __device__ __forceinline__ int64_t at(int32_t step, int slice) const {
+    const int from = (step - first) * kSlices + slice;
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(offset >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)offset, from));
+  }
+  __device__ __forceinline__ uint32_t mask(int32_t step) const { return (uint32_t)(there >> ((step - first) * kSlices)) & ((1u << kSlices) - 1); }
+};
+
+// Rows of a step that hold no token become zero: what lies there is multiplied by a weight of zero, and may be anything.
+template <class S>
+__device__ __forceinline__ void clear_rows(char* y, int first_row, int rows, int lane) {
+  for (int r = first_row; r < rows; ++r)
+    if (lane < S::kChunksPerRow) *reinterpret_cast<intx4*>(y + r * S::kRowBytes + lane * 16) = intx4{0, 0, 0, 0};
+}
+
+// Hides what a row does not see in a block of 32 tokens from `token` on; slices: which of its two are there.
+__device__ __forceinline__ void hide_tokens(const AttendArgs& a, const Sequence& q, const CacheRow& own, floatx16& s, int32_t token, uint32_t slices, int g) {
+  const int32_t at = token + 4 * g, lo = own.view.lo - at, hi = own.view.hi - at, prompt = own.prompt - at;
+  uint32_t drafts = 0;
+  if (a.tree) {
+    const int32_t shift = at - q.base;  // bit of the lane's first token
+    if (shift > -32 && shift < kMostDrafts) drafts = (uint32_t)(shift >= 0 ? own.drafts >> shift : own.drafts << -shift);
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int c = 8 * (r / 4) + (r % 4);
+    const bool seen = (int)(c < prompt) | ((int)(c >= lo) & (int)(c < hi)) | (int)((drafts >> c) & 1u);
+    s[r] = seen && ((slices >> (r / 8)) & 1u) ? s[r] : kMinusInf;
+  }
+}
+
+// Frame of a token of the cache, for the bias: drafts stand where their words say.
+__device__ __forceinline__ float frame_of_token(const AttendArgs& a, const Sequence& q, int32_t token) {
+  const bool draft = a.tree && token >= q.base && token < q.length;
+  return (float)frame_at(a, q, draft ? draft_place(q, draft_bits(a, q, q.first + (token - q.base))) : token);
+}
+
+}  // namespace
+}  // namespace ca
