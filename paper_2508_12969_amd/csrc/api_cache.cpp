@@ -20,6 +20,7 @@ namespace {
 
 constexpr int64_t kMostTokens = (int64_t)1 << 30, kMostBytes = (int64_t)1 << 46;
 constexpr int32_t kMostSequences = 1 << 20;
+constexpr int64_t kWholeTokens = 512;  // sequences of at most so many are not cut
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -143,14 +144,28 @@ int check_attend(const ca_cache* c, const ca_reach* r, int32_t heads) {
   return CA_OK;
 }
 
+// Parts of a call's workspace, in their order.
+struct Workspace {
+  int64_t splits = 0, pieces = 0;
+  int64_t bytes() const { return splits + pieces; }
+};
+
+int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
 // Sizes of a call's launch.
-int fill_attend(ca::AttendArgs& a, const ca_cache* c, int32_t heads) {
+int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t heads) {
   fill_cache(a, c);
   a.heads = heads;
   a.group = heads / c->kv_heads;
   a.D = c->head_dim;
-  a.tiles = (int64_t)c->tokens * a.group / 32 + std::min(c->tokens, c->sequences);
+  a.tiles = (int64_t)c->tokens * a.group / ca::kFewRows + std::min(c->tokens, c->sequences);
   if (a.tiles * c->kv_heads > 0xffffff) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
+  // Items of a few steps are not worth a second launch, and tiles of one sequence share their keys if workgroups walk over them side by side.
+  const int64_t rows = (int64_t)((c->tokens + (int64_t)c->sequences - 1) / c->sequences) * a.group;
+  const bool split = (int64_t)c->table_width * c->page_tokens > kWholeTokens && rows <= ca::kFewRows;
+  a.workgroups = split ? ca::few_workgroups(c->head_dim) : 0;
+  w.splits = padded256(a.workgroups * (int64_t)sizeof(ca::CacheSplit));
+  w.pieces = (int64_t)a.workgroups * 2 * ca::kFewRows * ca::piece_row(c->head_dim) * 4;
   return CA_OK;
 }
 
@@ -203,7 +218,9 @@ int compact_attn_cache_workspace(const ca_cache* c, int32_t heads, int64_t* work
   int st = check_cache(c);
   if (st == CA_OK) st = check_attend(c, nullptr, heads);
   ca::AttendArgs a{};
-  if (st == CA_OK) st = fill_attend(a, c, heads);
+  Workspace w;
+  if (st == CA_OK) st = fill_attend(a, w, c, heads);
+  if (st == CA_OK) *workspace_bytes = w.bytes();
   return st;
 }
 
@@ -219,9 +236,10 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   ca::AttendArgs a{};
   int64_t q_bytes = 0;
   st = packed_strides(c, q_strides, heads, "q", a.q_strides, q_bytes);
-  if (st == CA_OK) st = fill_attend(a, c, heads);
+  Workspace w;
+  if (st == CA_OK) st = fill_attend(a, w, c, heads);
   if (st != CA_OK) return st;
-  const int64_t need = 0, rows = (int64_t)c->tokens * heads, pages = page_bytes(c);
+  const int64_t need = c->tokens > 0 ? w.bytes() : 0, rows = (int64_t)c->tokens * heads, pages = page_bytes(c);
   if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) {
     set_error("the call needs a 16-byte aligned workspace of %lld bytes; got %lld", (long long)need, (long long)(workspace ? workspace_bytes : 0));
     return CA_ERR_INVALID_ARG;
@@ -229,6 +247,8 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   st = check_apart(c, {{out, rows * c->head_dim * 2}, {lse, rows * 4}, {workspace, need}},
                    {{q, q_bytes}, {c->k, pages}, {c->v, pages}, {r->slopes, (int64_t)heads * 4}, {r->tree, (int64_t)c->tokens * 8}});
   if (st != CA_OK || c->tokens == 0) return st;
+  a.splits = static_cast<ca::CacheSplit*>(workspace);
+  a.pieces = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.splits);
   a.q = q;
   a.out = out;
   a.lse = lse;

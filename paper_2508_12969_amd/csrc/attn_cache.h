@@ -73,51 +73,64 @@ __device__ __forceinline__ Walk<kStep> walk_of(const AttendArgs& a, const Sequen
   return w;
 }
 
-// Finds the sequence in which `target` lies when every sequence takes up weight(sequence) places, and how far behind its first place.  All threads call it; false: there are fewer places.
-struct LocateLds {
-  int64_t waves[16], rest, all;
+// The sequences on a line on which each takes up weight(sequence) places, one after the other.  All threads of a workgroup make it and ask it together.
+struct LineLds {
+  int64_t waves[16], rest;
   int32_t sequence;
 };
-template <int kThreads, class Weight>
-__device__ __forceinline__ bool locate(const CacheArgs& a, int64_t target, LocateLds& lds, int32_t& sequence, int64_t& rest, int64_t& all, Weight&& weight) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t per = ((int64_t)a.sequences + kThreads - 1) / kThreads;
-  const int32_t from = (int32_t)min(tid * per, (int64_t)a.sequences), to = (int32_t)min(from + per, (int64_t)a.sequences);
-  int64_t own = 0;
-  for (int32_t s = from; s < to; ++s) own += weight(sequence_at(a, s));
-  int64_t up = own;
-#pragma unroll
-  for (int step = 1; step < 64; step *= 2) {
-    const int64_t other = __shfl_up(up, step);
-    if (lane >= step) up += other;
-  }
-  if (lane == 63) lds.waves[wave] = up;
-  if (tid == 0) lds.sequence = -1;
-  __syncthreads();
-  int64_t before = 0, total = 0;
-  for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) before += lds.waves[w];
-    total += lds.waves[w];
-  }
-  int64_t at = before + up - own;
-  if (target >= at && target < at + own) {
-    for (int32_t s = from; s < to; ++s) {
-      const int64_t w = weight(sequence_at(a, s));
-      if (target < at + w) {
-        lds.sequence = s;
-        lds.rest = target - at;
-        break;
-      }
-      at += w;
-    }
-  }
-  __syncthreads();
-  sequence = __builtin_amdgcn_readfirstlane(lds.sequence);
-  const int64_t r = lds.rest;
-  rest = (int64_t)((uint64_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)r >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)r));
-  all = total;
-  return sequence >= 0;
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
+template <int kThreads>
+struct SequenceLine {
+  int32_t from, to;   // the thread's sequences
+  int64_t at, own;    // where they begin, what they take up
+  int64_t all;        // places, in scalar registers
+  template <class Weight>
+  __device__ __forceinline__ SequenceLine(const CacheArgs& a, LineLds& lds, Weight&& weight) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int32_t per = (a.sequences + kThreads - 1) / kThreads;
+    from = min(tid * per, a.sequences), to = min(from + per, a.sequences);
+    own = 0;
+    for (int32_t s = from; s < to; ++s) own += weight(sequence_at(a, s));
+    int64_t up = own;
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) {
+      const int64_t other = __shfl_up(up, step);
+      if (lane >= step) up += other;
+    }
+    if (lane == 63) lds.waves[wave] = up;
+    if (tid == 0) lds.sequence = -1;
+    __syncthreads();
+    at = up - own;
+    int64_t total = 0;
+    for (int w = 0; w < kThreads / 64; ++w) {
+      if (w < wave) at += lds.waves[w];
+      total += lds.waves[w];
+    }
+    all = uniform64(total);
+  }
+  // The sequence that holds a place, and how far behind its first; false: there is no such place.
+  template <class Weight>
+  __device__ __forceinline__ bool find(const CacheArgs& a, LineLds& lds, int64_t place, int32_t& sequence, int64_t& rest, Weight&& weight) const {
+    if (place >= at && place < at + own) {
+      int64_t here = at;
+      for (int32_t s = from; s < to; ++s) {
+        const int64_t w = weight(sequence_at(a, s));
+        if (place < here + w) {
+          lds.sequence = s;
+          lds.rest = place - here;
+          break;
+        }
+        here += w;
+      }
+    }
+    __syncthreads();
+    sequence = __builtin_amdgcn_readfirstlane(lds.sequence);
+    rest = uniform64(lds.rest);
+    return sequence >= 0;
+  }
+};
 
 __device__ __forceinline__ int32_t row_tiles(const AttendArgs& a, const Sequence& q, int rows) { return (int32_t)(((int64_t)q.count * a.group + rows - 1) / rows); }
 

@@ -4,12 +4,13 @@
 namespace ca {
 namespace {
 
-constexpr int kFewRows = 32, kFewStep = 32, kFewWaves = 4, kFewThreads = kFewWaves * 64;
+constexpr int kFewWaves = 4, kFewThreads = kFewWaves * 64;
+constexpr int kLeastFewSteps = 8;  // of a workgroup's share: two a wave
 
 // A wave's own part of LDS: two buffers of a step; at the end its sums, row by row.
 template <class S>
 struct FewWave {
-  static constexpr int kStepBytes = kFewStep * S::kRowBytes, kSumRow = S::D + 4;  // (rows of sums begin in different banks)
+  static constexpr int kStepBytes = kFewStep * S::kRowBytes, kSumRow = piece_row(S::D);
   union {
     char steps[2][2][kStepBytes];          // [buffer][keys, values]
     float sums[kFewRows][kSumRow];         // D sums, then the reference and the sum of weights
@@ -17,155 +18,277 @@ struct FewWave {
   float frames[kFewStep];
 };
 
-// A workgroup takes a tile of 32 rows, its waves a quarter of the steps each; they join their sums at the end.
+// Steps of a tile of rows; a tile without any is still one, so that its results are written.
+__device__ __forceinline__ Walk<kFewStep> few_walk(const AttendArgs& a, const Sequence& q, int64_t tile) {
+  const int64_t first = tile * kFewRows, last = min(first + kFewRows, (int64_t)q.count * a.group) - 1;
+  return walk_of<kFewStep>(a, q, (int32_t)(first / a.group), (int32_t)(last / a.group));
+}
+__device__ __forceinline__ int64_t few_steps(const AttendArgs& a, const Sequence& q) {
+  int64_t all = 0;
+  for (int32_t t = 0, n = row_tiles(a, q, kFewRows); t < n; ++t) all += max(1, few_walk(a, q, t).count);
+  return all * a.kv_heads;
+}
+
+// Writes a row's four channels from the joined sums.
+template <int D>
+__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int64_t row, int channel, const floatx4& o, float ref, float total) {
+  const int32_t t = (int32_t)(row / a.group), head = key_head * a.group + (int32_t)(row - (int64_t)t * a.group);
+  const int64_t at = (int64_t)(q.first + t) * a.heads + head;
+  const bool real = total != 0.f;
+  bf16x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? o[e] / total : 0.f);
+  *reinterpret_cast<bf16x4*>(static_cast<char*>(a.out) + (at * D + channel) * 2) = v;
+  if (channel == 0) a.lse[at] = real ? (__builtin_fmaf(ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInf;
+}
+
+// Sums of a row of which parts were made with references of their own.
+struct Joined {
+  float ref = kMinusInf, total = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(const CacheRule& rule, float part_ref, float part_total, const floatx4& part) {
+    const float to = fmaxf(ref, part_ref), old = ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((ref - to) * rule.c2);
+    const float fresh = part_ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((part_ref - to) * rule.c2);
+    ref = to;
+    total = total * old + part_total * fresh;  // (NaN stays, whatever its weight)
+    o = o * old + part * fresh;
+  }
+};
+
+// Where an item's sums go: LDS holds those of the waves.
+template <int D>
+__device__ __forceinline__ Joined join_waves(const CacheRule& rule, const FewWave<CacheShape<D>>* lds, int row, int channel) {
+  Joined j;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) j.add(rule, lds[w].sums[row][D], lds[w].sums[row][D + 1], *reinterpret_cast<const floatx4*>(&lds[w].sums[row][channel]));
+  return j;
+}
+
+// The steps of all items lie on one line: sequences, their key heads, their tiles.  A workgroup takes an even share of the line, whatever items that cuts (a batch of sequences
+// of very different lengths is as even as one of equal ones), and of an item its waves a quarter of the steps each; they join their sums at the end.  An item that
+// lies in several shares is joined by few_rows_join_kernel.
 template <int D>
 __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2))) void few_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
   __shared__ FewWave<S> lds[kFewWaves];
-  __shared__ LocateLds found;
+  __shared__ LineLds found;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
-  const int32_t key_head = (int32_t)(blockIdx.x % (uint32_t)a.kv_heads);
-  int32_t s;
-  int64_t tile, all;
-  if (!locate<kFewThreads>(a, blockIdx.x / (uint32_t)a.kv_heads, found, s, tile, all, [&](const Sequence& q) { return (int64_t)row_tiles(a, q, kFewRows); })) return;
-  const Sequence q = sequence_at(a, s);
+  const bool split = a.workgroups > 0;
+  const auto weight = [&](const Sequence& q) { return split ? few_steps(a, q) : (int64_t)row_tiles(a, q, kFewRows) * a.kv_heads; };
+  const SequenceLine<kFewThreads> line(a, found, weight);
+  const int64_t share = split ? max((int64_t)kLeastFewSteps, (line.all + a.workgroups - 1) / a.workgroups) : 1, first = blockIdx.x * share;
+  int64_t left = min(share, line.all - first), done;
+  int32_t s, begun = 0;
+  if (left < 1 || !line.find(a, found, first, s, done, weight)) {
+    if (split && threadIdx.x == 0) a.splits[blockIdx.x] = CacheSplit{0, 0, 0, 0};
+    return;
+  }
   const CacheRule rule(a);
-  const int64_t first_row = tile * kFewRows;
-  const int rows = (int)min((int64_t)kFewRows, (int64_t)q.count * a.group - first_row);
-  const int32_t first_token = (int32_t)(first_row / a.group), last_token = (int32_t)((first_row + rows - 1) / a.group);
-  const Walk<kFewStep> walk = walk_of<kFewStep>(a, q, first_token, last_token);
-  CacheRow own(a, rule, q, key_head, first_row + i);
-  const int32_t own_row = own.row >= 0 ? own.row : q.first + first_token, own_head = own.row >= 0 ? own.head : key_head * a.group;
-  asm volatile("" : "+v"(own.slope), "+v"(own.drafts));  // (waited for here, not in the loop)
-  const OwnOperand<S, S::kContraction> query(static_cast<const char*>(a.q) + (own_row * a.q_strides.token + own_head * a.q_strides.head) * 2, g, nullptr);
-  // what all rows of the tile see, in scalar registers
-  const int32_t sure_prompt = prompt_end(a, q), sure_hi = q.base < 0 ? 0 : a.tree ? q.base : view_at(a, q, q.base + first_token).hi;
-  const int32_t sure_lo = view_at(a, q, a.tree ? max(q.length - 1, 0) : max(q.base + last_token, 0)).lo;
+  Sequence q = sequence_at(a, s);
+  // the first item, and how many of its steps lie in other shares
+  int32_t tiles = row_tiles(a, q, kFewRows), key_head, tile = 0;
+  if (split) {
+    const int64_t per_head = few_steps(a, q) / a.kv_heads;
+    key_head = (int32_t)(done / per_head);
+    done -= key_head * per_head;
+    for (int32_t c; (c = max(1, few_walk(a, q, tile).count)) <= done; ++tile) done -= c;
+  } else {
+    key_head = (int32_t)(done / tiles);
+    tile = (int32_t)(done - (int64_t)key_head * tiles);
+    done = 0;
+  }
 
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   FewWave<S>& mine = lds[wave];
   const uint32_t lds_steps = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine.steps[0][0];
-  floatx16 sum[S::kDBlocks];
-#pragma unroll
-  for (auto& t : sum) t = splat(0.f);
-  Softmax soft;
+  while (true) {
+    const int64_t first_row = (int64_t)tile * kFewRows;
+    const int rows = (int)min((int64_t)kFewRows, (int64_t)q.count * a.group - first_row);
+    const int32_t first_token = (int32_t)(first_row / a.group), last_token = (int32_t)((first_row + rows - 1) / a.group);
+    const Walk<kFewStep> walk = walk_of<kFewStep>(a, q, first_token, last_token);
+    const int32_t count = max(1, walk.count), steps = split ? (int32_t)min((int64_t)count - done, left) : count;
+    CacheRow own(a, rule, q, key_head, first_row + i);
+    const int32_t own_row = own.row >= 0 ? own.row : q.first + first_token, own_head = own.row >= 0 ? own.head : key_head * a.group;
+    asm volatile("" : "+v"(own.slope), "+v"(own.drafts));  // (waited for here, not in the loop)
+    const OwnOperand<S, S::kContraction> query(static_cast<const char*>(a.q) + (own_row * a.q_strides.token + own_head * a.q_strides.head) * 2, g, nullptr);
+    // what all rows of the tile see, in scalar registers
+    const int32_t sure_prompt = prompt_end(a, q), sure_hi = q.base < 0 ? 0 : a.tree ? q.base : view_at(a, q, q.base + first_token).hi;
+    const int32_t sure_lo = view_at(a, q, a.tree ? max(q.length - 1, 0) : max(q.base + last_token, 0)).lo;
 
-  const int32_t part = (walk.count + kFewWaves - 1) / kFewWaves, from = min(walk.count, wave * part), to = min(walk.count, from + part);
-  SlicePlaces<2, kFewStep> places;
-  auto issue = [&](int32_t step) {
-    if (step == from || step - places.first >= places.kSteps) places.fetch(a, q, s, key_head, walk, step, to, lane, S::kRowBytes);
-    WAIT_LGKMCNT0();  // nothing still reads the buffer
-    const uint32_t to_lds = lds_steps + (uint32_t)(step & 1) * 2 * FewWave<S>::kStepBytes;
+    floatx16 sum[S::kDBlocks];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int64_t at = places.at(step, c);
-      copy(static_cast<const char*>(a.k) + at, to_lds + c * S::kSliceBytes);
-      copy(static_cast<const char*>(a.v) + at, to_lds + FewWave<S>::kStepBytes + c * S::kSliceBytes);
+    for (auto& t : sum) t = splat(0.f);
+    Softmax soft;
+
+    const int32_t end = min((int32_t)done + steps, walk.count), part = (steps + kFewWaves - 1) / kFewWaves;
+    const int32_t from = min(end, (int32_t)done + wave * part), to = min(end, from + part);
+    SlicePlaces<2, kFewStep> places;
+    auto issue = [&](int32_t step) {
+      if (step == from || step - places.first >= places.kSteps) places.fetch(a, q, s, key_head, walk, step, to, lane, S::kRowBytes);
+      WAIT_LGKMCNT0();  // nothing still reads the buffer
+      const uint32_t to_lds = lds_steps + (uint32_t)(step & 1) * 2 * FewWave<S>::kStepBytes;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int64_t at = places.at(step, c);
+        copy(static_cast<const char*>(a.k) + at, to_lds + c * S::kSliceBytes);
+        copy(static_cast<const char*>(a.v) + at, to_lds + FewWave<S>::kStepBytes + c * S::kSliceBytes);
+      }
+    };
+    uint32_t there = 0, next_there = 0;
+    if (from < to) {
+      issue(from);
+      there = places.mask(from);
     }
-  };
-  uint32_t there = 0, next_there = 0;
-  if (from < to) {
-    issue(from);
-    there = places.mask(from);
-  }
-  for (int32_t step = from; step < to; ++step) {
-    if (step + 1 < to) {
-      issue(step + 1);
-      next_there = places.mask(step + 1);
-      WAIT_VMCNT(4 * S::kSliceLoads);
-    } else {
-      WAIT_VMCNT(0);
+    for (int32_t step = from; step < to; ++step) {
+      if (step + 1 < to) {
+        issue(step + 1);
+        next_there = places.mask(step + 1);
+        WAIT_VMCNT(4 * S::kSliceLoads);
+      } else {
+        WAIT_VMCNT(0);
+      }
+      const LdsTile x = (LdsTile)mine.steps[step & 1][0], y = (LdsTile)mine.steps[step & 1][1];
+      const int32_t token = walk.token(step);
+      if (there != 3) clear_rows<S>(mine.steps[step & 1][1], there & 1 ? kSlice : 0, there & 2 ? kSlice : kFewStep, lane);
+      if (token + kFewStep > q.length) clear_rows<S>(mine.steps[step & 1][1], q.length - token, kFewStep, lane);
+      floatx16 p = block_product<S>(frag, x, 0, query, splat(0.f));
+      if (rule.capped) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(p[r] * rule.bend));
+      }
+      if (a.slopes) {
+        if (lane < kFewStep) mine.frames[lane] = frame_of_token(a, q, token + lane);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const floatx4 f = read4(mine.frames, 0, j, g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[4 * j + e] = __builtin_fmaf(__builtin_fabsf((float)own.view.frame - f[e]), own.slope, p[4 * j + e]);
+        }
+      }
+      const bool sure = token + kFewStep <= sure_hi && (token >= sure_lo || token + kFewStep <= sure_prompt) && there == 3;
+      if (!sure) hide_tokens(a, q, own, p, token, there, g);
+      float mx = p[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, p[r]);
+      mx = max_with_partner(mx);
+      const bool moves = mx > soft.ref + kLazyLog2 / rule.c2;
+      if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+        const float ref = moves ? mx : soft.ref;
+        const float alpha = moves && soft.ref != kMinusInf ? __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2) : 1.f;
+        soft.ref = ref;
+        soft.sum *= alpha;
+#pragma unroll
+        for (int db = 0; db < S::kDBlocks; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[db][r] *= alpha;
+      }
+      const float shift = soft.ref == kMinusInf ? 0.f : -soft.ref * rule.c2;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], rule.c2, shift));
+        soft.sum += p[r];
+      }
+      bf16x8 weights[2];
+      rounded(p, weights);
+      block_sums<S>(frag, y, 0, weights, sum);
+      there = next_there;
     }
-    const LdsTile x = (LdsTile)mine.steps[step & 1][0], y = (LdsTile)mine.steps[step & 1][1];
-    const int32_t token = walk.token(step);
-    if (there != 3) clear_rows<S>(mine.steps[step & 1][1], there & 1 ? kSlice : 0, there & 2 ? kSlice : kFewStep, lane);
-    if (token + kFewStep > q.length) clear_rows<S>(mine.steps[step & 1][1], q.length - token, kFewStep, lane);
-    floatx16 p = block_product<S>(frag, x, 0, query, splat(0.f));
-    if (rule.capped) {
+
+    // the wave's sums, row by row
+    const float total = sum_with_partner(soft.sum);
+    WAIT_LGKMCNT0();
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(p[r] * rule.bend));
-    }
-    if (a.slopes) {
-      if (lane < kFewStep) mine.frames[lane] = frame_of_token(a, q, token + lane);
-      __builtin_amdgcn_wave_barrier();
+    for (int db = 0; db < S::kDBlocks; ++db)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const floatx4 f = read4(mine.frames, 0, j, g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[4 * j + e] = __builtin_fmaf(__builtin_fabsf((float)own.view.frame - f[e]), own.slope, p[4 * j + e]);
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<floatx4*>(&mine.sums[i][db * 32 + 8 * j + 4 * g]) = floatx4{sum[db][4 * j], sum[db][4 * j + 1], sum[db][4 * j + 2], sum[db][4 * j + 3]};
+    if (g == 0) mine.sums[i][D] = soft.ref, mine.sums[i][D + 1] = total;
+    __syncthreads();
+    const bool whole = steps == count;
+    // sums of an item that is begun here go to the first place of the workgroup, of one that others have begun to the second
+    float* const piece = whole ? nullptr : a.pieces + ((int64_t)blockIdx.x * 2 + (done > 0)) * kFewRows * piece_row(D);
+    for (int item = threadIdx.x; item < rows * (D / 4); item += kFewThreads) {
+      const int r = item / (D / 4), c = item % (D / 4) * 4;
+      const Joined j = join_waves<D>(rule, lds, r, c);
+      if (whole) {
+        store_row<D>(a, rule, q, key_head, first_row + r, c, j.o, j.ref, j.total);
+      } else {
+        *reinterpret_cast<floatx4*>(piece + r * piece_row(D) + c) = j.o;
+        if (c == 0) *reinterpret_cast<float2*>(piece + r * piece_row(D) + D) = float2{j.ref, j.total};
       }
     }
-    const bool sure = token + kFewStep <= sure_hi && (token >= sure_lo || token + kFewStep <= sure_prompt) && there == 3;
-    if (!sure) hide_tokens(a, q, own, p, token, there, g);
-    float mx = p[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, p[r]);
-    mx = max_with_partner(mx);
-    const bool moves = mx > soft.ref + kLazyLog2 / rule.c2;
-    if (__builtin_amdgcn_ballot_w64(moves) != 0) {
-      const float ref = moves ? mx : soft.ref;
-      const float alpha = moves && soft.ref != kMinusInf ? __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2) : 1.f;
-      soft.ref = ref;
-      soft.sum *= alpha;
-#pragma unroll
-      for (int db = 0; db < S::kDBlocks; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum[db][r] *= alpha;
+    if (!whole && done == 0) {
+      begun = 1 + (int32_t)((count - steps + share - 1) / share);
+      break;
     }
-    const float shift = soft.ref == kMinusInf ? 0.f : -soft.ref * rule.c2;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], rule.c2, shift));
-      soft.sum += p[r];
+    left -= steps;
+    if (!split || left < 1) break;
+    // the next item
+    done = 0;
+    if (++tile == tiles) {
+      tile = 0;
+      if (++key_head == a.kv_heads) {
+        key_head = 0;
+        do q = sequence_at(a, ++s);
+        while (q.count == 0);
+        tiles = row_tiles(a, q, kFewRows);
+      }
     }
-    bf16x8 weights[2];
-    rounded(p, weights);
-    block_sums<S>(frag, y, 0, weights, sum);
-    there = next_there;
+    __syncthreads();  // (the sums lie where the next steps go)
   }
+  if (split && threadIdx.x == 0) a.splits[blockIdx.x] = CacheSplit{s, key_head, tile, begun};
+}
 
-  // the wave's sums, row by row
-  const float weight = sum_with_partner(soft.sum);
-  WAIT_LGKMCNT0();
-#pragma unroll
-  for (int db = 0; db < S::kDBlocks; ++db)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<floatx4*>(&mine.sums[i][db * 32 + 8 * j + 4 * g]) = floatx4{sum[db][4 * j], sum[db][4 * j + 1], sum[db][4 * j + 2], sum[db][4 * j + 3]};
-  if (g == 0) mine.sums[i][D] = soft.ref, mine.sums[i][D + 1] = weight;
-  __syncthreads();
-  for (int item = threadIdx.x; item < rows * (D / 4); item += kFewThreads) {
-    const int r = item / (D / 4), c = item % (D / 4) * 4;
-    float ref = kMinusInf, total = 0.f;
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) ref = fmaxf(ref, lds[w].sums[r][D]);
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-      const float there_ref = lds[w].sums[r][D], factor = there_ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((there_ref - ref) * rule.c2);
-      total += lds[w].sums[r][D + 1] * factor;
-      o += *reinterpret_cast<const floatx4*>(&lds[w].sums[r][c]) * factor;
+// Joins the pieces of an item, in their order.  A workgroup takes some rows of the item that one workgroup of few_rows_kernel has begun; its threads take four channels each, and so many of them
+// together a part of the pieces.  Bound: latency.
+template <int D>
+__global__ __launch_bounds__(kFewThreads) void few_rows_join_kernel(AttendArgs a) {
+  constexpr int kColumns = D / 4, kParts = kFewThreads / kColumns;
+  __shared__ floatx4 sums[kParts][kColumns];
+  __shared__ float2 stats[kParts];
+  const CacheSplit split = a.splits[blockIdx.x];
+  if (split.pieces == 0) return;
+  const Sequence q = sequence_at(a, split.sequence);
+  const CacheRule rule(a);
+  const int64_t first_row = (int64_t)split.tile * kFewRows;
+  const int rows = (int)min((int64_t)kFewRows, (int64_t)q.count * a.group - first_row);
+  const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns;
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+    Joined j;
+#pragma unroll 4
+    for (int k = part; k < split.pieces; k += kParts) {
+      const float* from = a.pieces + (((int64_t)blockIdx.x + k) * 2 + (k > 0)) * kFewRows * piece_row(D) + r * piece_row(D);
+      const float2 stat = *reinterpret_cast<const float2*>(from + D);
+      j.add(rule, stat.x, stat.y, *reinterpret_cast<const floatx4*>(from + column * 4));
     }
-    const int32_t t = (int32_t)((first_row + r) / a.group), head = key_head * a.group + (int32_t)(first_row + r - (int64_t)t * a.group);
-    const int64_t at = (int64_t)(q.first + t) * a.heads + head;
-    const bool real = total != 0.f;
-    bf16x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? o[e] / total : 0.f);
-    *reinterpret_cast<bf16x4*>(static_cast<char*>(a.out) + (at * D + c) * 2) = v;
-    if (c == 0) a.lse[at] = real ? (__builtin_fmaf(ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInf;
+    sums[part][column] = j.o;
+    if (column == 0) stats[part] = float2{j.ref, j.total};
+    __syncthreads();
+    if (part == 0) {
+      for (int k = 1; k < kParts; ++k) j.add(rule, stats[k].x, stats[k].y, sums[k][column]);
+      store_row<D>(a, rule, q, split.key_head, first_row + r, column * 4, j.o, j.ref, j.total);
+    }
+    __syncthreads();
   }
+}
+
+template <int D>
+hipError_t launch_few_rows(const AttendArgs& a, hipStream_t stream) {
+  const int64_t workgroups = a.workgroups > 0 ? a.workgroups : a.tiles * a.kv_heads;
+  if (workgroups < 1 || workgroups > 0xffffff) return hipErrorInvalidValue;  // (2^32 threads)
+  few_rows_kernel<D><<<(unsigned)workgroups, kFewThreads, 0, stream>>>(a);
+  if (a.workgroups > 0) {
+    // a workgroup for every row that a sequence has on average, as far as a tile has them
+    const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group;
+    few_rows_join_kernel<D><<<dim3((unsigned)workgroups, (unsigned)(rows < kFewRows ? rows : kFewRows)), kFewThreads, 0, stream>>>(a);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attend(const AttendArgs& a, hipStream_t stream) {
-  const int64_t workgroups = a.tiles * a.kv_heads;
-  if (workgroups < 1 || workgroups > 0xffffff) return hipErrorInvalidValue;  // (2^32 threads)
-  if (a.D == 64) few_rows_kernel<64><<<(unsigned)workgroups, kFewThreads, 0, stream>>>(a);
-  else few_rows_kernel<128><<<(unsigned)workgroups, kFewThreads, 0, stream>>>(a);
-  return hipGetLastError();
-}
+hipError_t launch_attend(const AttendArgs& a, hipStream_t stream) { return a.D == 64 ? launch_few_rows<64>(a, stream) : launch_few_rows<128>(a, stream); }
 
 }  // namespace ca

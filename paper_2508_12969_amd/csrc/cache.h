@@ -38,6 +38,12 @@ struct KeepArgs : CacheArgs {
   int32_t width, row_bytes;
 };
 
+// An item (a tile of rows and a key head) that a workgroup begins and others go on with.
+struct CacheSplit {
+  int32_t sequence, key_head, tile;
+  int32_t pieces;  // of one workgroup after the other; 0: this workgroup begins none such
+};
+
 struct AttendArgs : CacheArgs {
   const void* q;
   TokenStrides q_strides;
@@ -49,7 +55,17 @@ struct AttendArgs : CacheArgs {
   int32_t causal, window;
   const uint64_t* tree;        // [tokens] or null
   int64_t tiles;               // most row tiles that the sequences can have together
+  int32_t workgroups;          // that share all steps evenly; 0: a workgroup for every item
+  CacheSplit* splits;          // workspace: [workgroups]
+  float* pieces;               // workspace: [workgroups][2][rows of a tile][piece_row(D)]
 };
+
+// A few rows a sequence are taken in tiles of 32, which read their keys and values in steps of 32 tokens.
+constexpr int kFewRows = 32, kFewStep = 32;
+// Workgroups that the device holds at a time: one per compute unit at head dim 128 (its buffers fill the LDS), two at 64.
+constexpr int few_workgroups(int D) { return D == 128 ? 256 : 512; }
+// Sums of a row: D, then the reference of the exponent and the sum of weights; rows begin at 16 bytes, and in different banks of LDS.
+constexpr int piece_row(int D) { return D + 4; }
 
 hipError_t launch_append(const AppendArgs& a, bool bf16, bool normed, hipStream_t stream);
 hipError_t launch_keep(const KeepArgs& a, hipStream_t stream);
