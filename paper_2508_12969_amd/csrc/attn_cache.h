@@ -168,6 +168,51 @@ struct CacheRow {
   }
 };
 
+__device__ __forceinline__ void cap_scores(const CacheRule& rule, floatx16& s) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
+}
+
+// frames: of the step's tokens
+__device__ __forceinline__ void bias_scores(const CacheRow& own, floatx16& s, const float* frames, int block, int g) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const floatx4 f = read4(frames, block, j, g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[4 * j + e] = __builtin_fmaf(__builtin_fabsf((float)own.view.frame - f[e]), own.slope, s[4 * j + e]);
+  }
+}
+
+// Scores -> weights.  The reference lags behind the maximum (see QueryWave::softmax); sums are put in relation to a new one when it moves.
+template <int kBlocks, int kDBlocks>
+__device__ __forceinline__ void soften(const CacheRule& rule, Softmax& soft, floatx16 (&s)[kBlocks], floatx16 (&sum)[kDBlocks]) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+  mx = max_with_partner(mx);
+  const bool moves = mx > soft.ref + kLazyLog2 / rule.c2;
+  if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+    const float ref = moves ? mx : soft.ref;
+    const float alpha = moves && soft.ref != kMinusInf ? __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2) : 1.f;
+    soft.ref = ref;
+    soft.sum *= alpha;
+#pragma unroll
+    for (int db = 0; db < kDBlocks; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[db][r] *= alpha;
+  }
+  const float shift = soft.ref == kMinusInf ? 0.f : -soft.ref * rule.c2;
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], rule.c2, shift));
+      soft.sum += s[b][r];
+    }
+}
+
 // Copies a slice (16 rows of a page) into LDS, asynchronously; logical chunks lie where swizzle() puts them.
 template <class S>
 struct SliceCopy {
@@ -204,20 +249,35 @@ struct SliceCopy {
   }
 };
 
-// Where the slices of the next 64 / kSlices steps lie, one a lane; fetched by all lanes at once.
+// Where the slices of 64 / kSlices steps lie, one a lane, fetched by all lanes at once; the table is read some steps before the places are needed.
 template <int kSlices, int kStep>
 struct SlicePlaces {
+  static constexpr int kSteps = 64 / kSlices;
   int32_t first = 0;      // step of lane 0
   int64_t offset = 0;     // bytes; of a slice that is not there: 0, a place that can be read
   uint64_t there = 0;     // a bit a lane
-  static constexpr int kSteps = 64 / kSlices;
-  __device__ __forceinline__ void fetch(const AttendArgs& a, const Sequence& q, int32_t s, int32_t head, const Walk<kStep>& w, int32_t step, int32_t end, int lane, int row_bytes) {
-    first = step;
+  int32_t page = -1;      // of the steps asked for
+  __device__ __forceinline__ int64_t token_of(const Sequence& q, const Walk<kStep>& w, int32_t step, int32_t end, int lane) const {
     const int32_t mine = step + lane / kSlices;
-    const int64_t token = mine < end ? (int64_t)w.token(mine) + lane % kSlices * kSlice : q.length;
-    const int32_t page = token < q.length ? page_at(a, s, (int32_t)token) : -1;
-    offset = page >= 0 ? cache_row(a, page, head, (int32_t)token % a.page_tokens) * row_bytes : 0;
-    there = __builtin_amdgcn_ballot_w64(page >= 0);
+    return mine < end ? (int64_t)w.token(mine) + lane % kSlices * kSlice : q.length;
+  }
+  __device__ __forceinline__ void ask(const AttendArgs& a, const Sequence& q, int32_t s, const Walk<kStep>& w, int32_t step, int32_t end, int lane) {
+    const int64_t token = token_of(q, w, step, end, lane);
+    page = token < q.length ? a.table[(int64_t)s * a.table_width + (int32_t)token / a.page_tokens] : -1;
+  }
+  __device__ __forceinline__ void take(const AttendArgs& a, const Sequence& q, int32_t head, const Walk<kStep>& w, int32_t step, int32_t end, int lane, int row_bytes) {
+    first = step;
+    const int64_t token = token_of(q, w, step, end, lane);
+    const bool here = page >= 0 && page < a.num_pages;
+    offset = here ? cache_row(a, page, head, (int32_t)token % a.page_tokens) * row_bytes : 0;
+    there = __builtin_amdgcn_ballot_w64(here);
+  }
+  // Called for every step in turn, from `begin` on.
+  __device__ __forceinline__ void at_step(const AttendArgs& a, const Sequence& q, int32_t s, int32_t head, const Walk<kStep>& w, int32_t step, int32_t begin, int32_t end, int lane,
+                                          int row_bytes) {
+    if (step == begin) ask(a, q, s, w, step, end, lane);
+    if (step == begin || step - first == kSteps) take(a, q, head, w, step, end, lane, row_bytes);
+    if (step - first == kSteps / 2 && first + kSteps < end) ask(a, q, s, w, first + kSteps, end, lane);
   }
   __device__ __forceinline__ int64_t at(int32_t step, int slice) const {
     const int from = (step - first) * kSlices + slice;
@@ -253,6 +313,61 @@ __device__ __forceinline__ void hide_tokens(const AttendArgs& a, const Sequence&
 __device__ __forceinline__ float frame_of_token(const AttendArgs& a, const Sequence& q, int32_t token) {
   const bool draft = a.tree && token >= q.base && token < q.length;
   return (float)frame_at(a, q, draft ? draft_place(q, draft_bits(a, q, q.first + (token - q.base))) : token);
+}
+
+// Writes a row's four channels from the joined sums.
+template <int D>
+__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int64_t row, int channel, const floatx4& o, float ref, float total) {
+  const int32_t t = (int32_t)(row / a.group), head = key_head * a.group + (int32_t)(row - (int64_t)t * a.group);
+  const int64_t at = (int64_t)(q.first + t) * a.heads + head;
+  const bool real = total != 0.f;
+  bf16x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? o[e] / total : 0.f);
+  *reinterpret_cast<bf16x4*>(static_cast<char*>(a.out) + (at * D + channel) * 2) = v;
+  if (channel == 0) a.lse[at] = real ? (__builtin_fmaf(ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInf;
+}
+
+// Sums of a row of which parts were made with references of their own.
+struct Joined {
+  float ref = kMinusInf, total = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(const CacheRule& rule, float part_ref, float part_total, const floatx4& part) {
+    const float to = fmaxf(ref, part_ref), old = ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((ref - to) * rule.c2);
+    const float fresh = part_ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((part_ref - to) * rule.c2);
+    ref = to;
+    total = total * old + part_total * fresh;  // (NaN stays, whatever its weight)
+    o = o * old + part * fresh;
+  }
+};
+
+// Joins the pieces of a row, in their order; piece(k): where the k-th lies (D sums, reference, sum of weights).  Threads take four channels each, and so many of them together a part of the pieces.
+template <int D, int kThreads>
+struct JoinLds {
+  static constexpr int kColumns = D / 4, kParts = kThreads / kColumns;
+  floatx4 sums[kParts][kColumns];
+  float2 stats[kParts];
+};
+template <int D, int kThreads, class Piece>
+__device__ __forceinline__ void join_row(const AttendArgs& a, const Sequence& q, int32_t key_head, int64_t row, int pieces, JoinLds<D, kThreads>& lds, Piece&& piece) {
+  constexpr int kColumns = JoinLds<D, kThreads>::kColumns, kParts = JoinLds<D, kThreads>::kParts;
+  const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns;
+  const CacheRule rule(a);
+  Joined j;
+#pragma unroll 4
+  for (int k = part; k < pieces; k += kParts) {
+    const float* from = piece(k);
+    const float2 stat = *reinterpret_cast<const float2*>(from + D);
+    j.add(rule, stat.x, stat.y, *reinterpret_cast<const floatx4*>(from + column * 4));
+  }
+  lds.sums[part][column] = j.o;
+  if (column == 0) lds.stats[part] = float2{j.ref, j.total};
+  __syncthreads();
+  if (part == 0) {
+    for (int k = 1; k < kParts && k < pieces; ++k) j.add(rule, lds.stats[k].x, lds.stats[k].y, lds.sums[k][column]);
+    store_row<D>(a, rule, q, key_head, row, column * 4, j.o, j.ref, j.total);
+  }
+  __syncthreads();
 }
 
 }  // namespace

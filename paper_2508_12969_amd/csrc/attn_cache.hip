@@ -29,32 +29,6 @@ __device__ __forceinline__ int64_t few_steps(const AttendArgs& a, const Sequence
   return all * a.kv_heads;
 }
 
-// Writes a row's four channels from the joined sums.
-template <int D>
-__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int64_t row, int channel, const floatx4& o, float ref, float total) {
-  const int32_t t = (int32_t)(row / a.group), head = key_head * a.group + (int32_t)(row - (int64_t)t * a.group);
-  const int64_t at = (int64_t)(q.first + t) * a.heads + head;
-  const bool real = total != 0.f;
-  bf16x4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? o[e] / total : 0.f);
-  *reinterpret_cast<bf16x4*>(static_cast<char*>(a.out) + (at * D + channel) * 2) = v;
-  if (channel == 0) a.lse[at] = real ? (__builtin_fmaf(ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInf;
-}
-
-// Sums of a row of which parts were made with references of their own.
-struct Joined {
-  float ref = kMinusInf, total = 0.f;
-  floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  __device__ __forceinline__ void add(const CacheRule& rule, float part_ref, float part_total, const floatx4& part) {
-    const float to = fmaxf(ref, part_ref), old = ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((ref - to) * rule.c2);
-    const float fresh = part_ref == kMinusInf ? 0.f : __builtin_amdgcn_exp2f((part_ref - to) * rule.c2);
-    ref = to;
-    total = total * old + part_total * fresh;  // (NaN stays, whatever its weight)
-    o = o * old + part * fresh;
-  }
-};
-
 // Where an item's sums go: LDS holds those of the waves.
 template <int D>
 __device__ __forceinline__ Joined join_waves(const CacheRule& rule, const FewWave<CacheShape<D>>* lds, int row, int channel) {
@@ -125,7 +99,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
     const int32_t from = min(end, (int32_t)done + wave * part), to = min(end, from + part);
     SlicePlaces<2, kFewStep> places;
     auto issue = [&](int32_t step) {
-      if (step == from || step - places.first >= places.kSteps) places.fetch(a, q, s, key_head, walk, step, to, lane, S::kRowBytes);
+      places.at_step(a, q, s, key_head, walk, step, from, to, lane, S::kRowBytes);
       WAIT_LGKMCNT0();  // nothing still reads the buffer
       const uint32_t to_lds = lds_steps + (uint32_t)(step & 1) * 2 * FewWave<S>::kStepBytes;
 #pragma unroll
@@ -153,43 +127,15 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
       if (there != 3) clear_rows<S>(mine.steps[step & 1][1], there & 1 ? kSlice : 0, there & 2 ? kSlice : kFewStep, lane);
       if (token + kFewStep > q.length) clear_rows<S>(mine.steps[step & 1][1], q.length - token, kFewStep, lane);
       floatx16 p = block_product<S>(frag, x, 0, query, splat(0.f));
-      if (rule.capped) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(p[r] * rule.bend));
-      }
+      if (rule.capped) cap_scores(rule, p);
       if (a.slopes) {
         if (lane < kFewStep) mine.frames[lane] = frame_of_token(a, q, token + lane);
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const floatx4 f = read4(mine.frames, 0, j, g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[4 * j + e] = __builtin_fmaf(__builtin_fabsf((float)own.view.frame - f[e]), own.slope, p[4 * j + e]);
-        }
+        bias_scores(own, p, mine.frames, 0, g);
       }
       const bool sure = token + kFewStep <= sure_hi && (token >= sure_lo || token + kFewStep <= sure_prompt) && there == 3;
       if (!sure) hide_tokens(a, q, own, p, token, there, g);
-      float mx = p[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, p[r]);
-      mx = max_with_partner(mx);
-      const bool moves = mx > soft.ref + kLazyLog2 / rule.c2;
-      if (__builtin_amdgcn_ballot_w64(moves) != 0) {
-        const float ref = moves ? mx : soft.ref;
-        const float alpha = moves && soft.ref != kMinusInf ? __builtin_amdgcn_exp2f((soft.ref - ref) * rule.c2) : 1.f;
-        soft.ref = ref;
-        soft.sum *= alpha;
-#pragma unroll
-        for (int db = 0; db < S::kDBlocks; ++db)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sum[db][r] *= alpha;
-      }
-      const float shift = soft.ref == kMinusInf ? 0.f : -soft.ref * rule.c2;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], rule.c2, shift));
-        soft.sum += p[r];
-      }
+      soften<1, S::kDBlocks>(rule, soft, reinterpret_cast<floatx16(&)[1]>(p), sum);
       bf16x8 weights[2];
       rounded(p, weights);
       block_sums<S>(frag, y, 0, weights, sum);
@@ -241,37 +187,18 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
   if (split && threadIdx.x == 0) a.splits[blockIdx.x] = CacheSplit{s, key_head, tile, begun};
 }
 
-// Joins the pieces of an item, in their order.  A workgroup takes some rows of the item that one workgroup of few_rows_kernel has begun; its threads take four channels each, and so many of them
-// together a part of the pieces.  Bound: latency.
+// Bound: latency.  A workgroup takes some rows of the item that one workgroup of few_rows_kernel has begun.
 template <int D>
 __global__ __launch_bounds__(kFewThreads) void few_rows_join_kernel(AttendArgs a) {
-  constexpr int kColumns = D / 4, kParts = kFewThreads / kColumns;
-  __shared__ floatx4 sums[kParts][kColumns];
-  __shared__ float2 stats[kParts];
+  __shared__ JoinLds<D, kFewThreads> lds;
   const CacheSplit split = a.splits[blockIdx.x];
   if (split.pieces == 0) return;
   const Sequence q = sequence_at(a, split.sequence);
-  const CacheRule rule(a);
   const int64_t first_row = (int64_t)split.tile * kFewRows;
   const int rows = (int)min((int64_t)kFewRows, (int64_t)q.count * a.group - first_row);
-  const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns;
-  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-    Joined j;
-#pragma unroll 4
-    for (int k = part; k < split.pieces; k += kParts) {
-      const float* from = a.pieces + (((int64_t)blockIdx.x + k) * 2 + (k > 0)) * kFewRows * piece_row(D) + r * piece_row(D);
-      const float2 stat = *reinterpret_cast<const float2*>(from + D);
-      j.add(rule, stat.x, stat.y, *reinterpret_cast<const floatx4*>(from + column * 4));
-    }
-    sums[part][column] = j.o;
-    if (column == 0) stats[part] = float2{j.ref, j.total};
-    __syncthreads();
-    if (part == 0) {
-      for (int k = 1; k < kParts; ++k) j.add(rule, stats[k].x, stats[k].y, sums[k][column]);
-      store_row<D>(a, rule, q, split.key_head, first_row + r, column * 4, j.o, j.ref, j.total);
-    }
-    __syncthreads();
-  }
+  for (int r = blockIdx.y; r < rows; r += gridDim.y)
+    join_row<D>(a, q, split.key_head, first_row + r, split.pieces, lds,
+                [&](int k) { return a.pieces + ((((int64_t)blockIdx.x + k) * 2 + (k > 0)) * kFewRows + r) * piece_row(D); });
 }
 
 template <int D>
@@ -289,6 +216,6 @@ hipError_t launch_few_rows(const AttendArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_attend(const AttendArgs& a, hipStream_t stream) { return a.D == 64 ? launch_few_rows<64>(a, stream) : launch_few_rows<128>(a, stream); }
+hipError_t launch_attend_few(const AttendArgs& a, hipStream_t stream) { return a.D == 64 ? launch_few_rows<64>(a, stream) : launch_few_rows<128>(a, stream); }
 
 }  // namespace ca

@@ -54,14 +54,21 @@ struct AttendArgs : CacheArgs {
   const float* slopes;         // [heads] or null
   int32_t causal, window;
   const uint64_t* tree;        // [tokens] or null
+  bool many;                   // rows a sequence: tiles of kManyRows, else of kFewRows
   int64_t tiles;               // most row tiles that the sequences can have together
+  // few rows
   int32_t workgroups;          // that share all steps evenly; 0: a workgroup for every item
   CacheSplit* splits;          // workspace: [workgroups]
-  float* pieces;               // workspace: [workgroups][2][rows of a tile][piece_row(D)]
+  // many rows
+  int32_t part_steps, most_parts;  // tiles of more steps are cut into parts
+  float* pieces;               // workspace: [workgroups][2], or [tiles * kv_heads][most_parts], of [rows of a tile][piece_row(D)]
 };
 
 // A few rows a sequence are taken in tiles of 32, which read their keys and values in steps of 32 tokens.
 constexpr int kFewRows = 32, kFewStep = 32;
+// Many rows are taken in tiles of 128, with steps of 64 tokens that the waves of a workgroup share.
+constexpr int kManyRows = 128, kManyStep = 64;
+constexpr int kManyPlaces = 512;  // workgroups that the device holds at a time
 // Workgroups that the device holds at a time: one per compute unit at head dim 128 (its buffers fill the LDS), two at 64.
 constexpr int few_workgroups(int D) { return D == 128 ? 256 : 512; }
 // Sums of a row: D, then the reference of the exponent and the sum of weights; rows begin at 16 bytes, and in different banks of LDS.
@@ -69,6 +76,7 @@ constexpr int piece_row(int D) { return D + 4; }
 
 hipError_t launch_append(const AppendArgs& a, bool bf16, bool normed, hipStream_t stream);
 hipError_t launch_keep(const KeepArgs& a, hipStream_t stream);
-hipError_t launch_attend(const AttendArgs& a, hipStream_t stream);
+hipError_t launch_attend_few(const AttendArgs& a, hipStream_t stream);
+hipError_t launch_attend_many(const AttendArgs& a, hipStream_t stream);
 
 }  // namespace ca

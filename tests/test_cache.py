@@ -254,6 +254,11 @@ ATTEND = {
     "tree-past-64": dict(sequences=[(100, 70), (80, 80)], kv=1, group=2, D=64, page=16, tree=True),
     "long": dict(sequences=[(20011, 1), (9, 1)], kv=1, group=2, D=128, page=128),
     "long-64": dict(sequences=[(30000, 2)], kv=1, group=1, D=64, page=256),
+    "rows-cut": dict(sequences=[(6000, 60), (1200, 200), (40, 40)], kv=1, group=2, D=128, page=48),
+    "rows-cut-64": dict(sequences=[(9000, 35), (2, 2)], kv=2, group=2, D=64, page=16, window=3000, cap=20.0),
+    "rows-cut-frames": dict(sequences=[(4000, 140), (70, 70)], kv=2, group=1, D=128, page=256, frame=(7, 10), origins=[333, 5], window=30, slopes=True),
+    "rows-cut-tree": dict(sequences=[(5000, 64), (300, 33)], kv=1, group=4, D=64, page=64, tree=True),
+    "few-cut-tree": dict(sequences=[(5000, 9), (300, 5), (0, 0), (777, 8)], kv=3, group=3, D=128, page=64, tree=True, slopes=True),
     "more-new-than-tokens": dict(sequences=[(20, 30), (40, 10)], kv=1, group=2, D=64, page=16),
     "many": dict(sequences=[((i * 37) % 90 + 1, (i * 37) % 90 % 2 + (i % 3 > 0)) if (i * 37) % 90 > 3 else (3, 0) for i in range(700)], kv=1, group=1, D=64, page=16),
 }
