@@ -21,6 +21,8 @@ namespace {
 constexpr int64_t kMostTokens = (int64_t)1 << 30, kMostBytes = (int64_t)1 << 46;
 constexpr int32_t kMostSequences = 1 << 20;
 constexpr int64_t kWholeTokens = 512;  // sequences of at most so many are not cut
+constexpr int64_t kLeastFewSteps = 8, kLeastManySteps = 8;  // of a workgroup's share: 256 and 512 tokens
+constexpr int64_t kSideBySide = 512;   // rows of a sequence from which on tiles walk side by side
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -152,18 +154,19 @@ struct Workspace {
 
 int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Parts that a tile of so many steps is cut into, at most: launches of few tiles would leave compute units without work, or end with a round that is not full.  A workgroup takes as long as
+// Equal parts of items of up to `steps` steps: launches of few items would leave compute units without work, or end with a round that is not full.  A workgroup takes as long as
 // kItemSteps steps besides its own, and kPieceSteps more where its sums are joined.
-void cut_tiles(ca::AttendArgs& a, int64_t items, int64_t steps) {
-  constexpr int64_t kItemSteps = 6, kPieceSteps = 4, kLeastSteps = 8, kMostParts = 64, kMostPieceBytes = (int64_t)256 << 20;
-  const int64_t piece_bytes = (int64_t)ca::kManyRows * ca::piece_row(a.D) * 4;
+void cut_items(ca::AttendArgs& a, int64_t steps) {
+  constexpr int64_t kItemSteps = 6, kPieceSteps = 4, kMostParts = 64, kMostPieceBytes = (int64_t)256 << 20;
+  const int64_t items = a.tiles * a.kv_heads, piece_bytes = (int64_t)a.tile_rows * ca::piece_row(a.D) * 4, places = ca::many_workgroups(a.tile_rows);
   int64_t best = 1, best_end = 0;
   for (int64_t parts = 1; parts <= kMostParts; ++parts) {
     const int64_t size = (steps + parts - 1) / parts;
-    if (parts > 1 && (size < kLeastSteps || items * parts * piece_bytes > kMostPieceBytes)) break;
-    const int64_t rounds = (items * parts + ca::kManyPlaces - 1) / ca::kManyPlaces, end = rounds * (size + kItemSteps + (parts > 1 ? kPieceSteps : 0));
+    if (parts > 1 && (size < kLeastManySteps || items * parts * piece_bytes > kMostPieceBytes)) break;
+    const int64_t rounds = (items * parts + places - 1) / places, end = rounds * (size + kItemSteps + (parts > 1 ? kPieceSteps : 0));
     if (parts == 1 || 50 * end < 49 * best_end) best = parts, best_end = end;  // (not for a per cent)
   }
+  a.way = best > 1 ? ca::kParts : ca::kItems;
   a.most_parts = (int32_t)best;
   a.part_steps = (int32_t)((steps + best - 1) / best);
 }
@@ -175,19 +178,25 @@ int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t head
   a.group = heads / c->kv_heads;
   a.D = c->head_dim;
   const int64_t most_tokens = (int64_t)c->table_width * c->page_tokens, rows = (int64_t)((c->tokens + (int64_t)c->sequences - 1) / c->sequences) * a.group;
-  const int64_t piece_bytes = ca::piece_row(a.D) * 4;
-  a.many = rows > ca::kFewRows;
-  const int tile = a.many ? ca::kManyRows : ca::kFewRows;
-  a.tiles = (int64_t)c->tokens * a.group / tile + std::min(c->tokens, c->sequences);
-  if (a.tiles * c->kv_heads > 0xffffff / 64) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
-  if (a.many) {
-    const int64_t items = a.tiles * c->kv_heads;
-    cut_tiles(a, items, (most_tokens + ca::kManyStep - 1) / ca::kManyStep);
-    w.pieces = a.most_parts > 1 ? items * a.most_parts * tile * piece_bytes : 0;
-  } else if (most_tokens > kWholeTokens) {  // (items of a few steps are not worth a second launch)
-    a.workgroups = ca::few_workgroups(a.D);
+  const bool many = rows > ca::kFewRows;
+  a.tile_rows = !many ? ca::kFewRows : rows > 128 && rows < kSideBySide ? 256 : 128;
+  const int64_t piece_bytes = (int64_t)a.tile_rows * ca::piece_row(a.D) * 4;
+  a.tiles = (int64_t)c->tokens * a.group / a.tile_rows + std::min(c->tokens, c->sequences);
+  if (a.tiles * c->kv_heads > 0xffffff / 64 || (int64_t)c->tokens * a.group > kMostTokens) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
+  const int64_t items = a.tiles * c->kv_heads;
+  a.way = ca::kItems;  // (items of a few steps are not worth a second launch)
+  if (rows >= kSideBySide) {
+    cut_items(a, (most_tokens + ca::kManyStep - 1) / ca::kManyStep);
+    if (a.way == ca::kParts) {
+      w.splits = padded256(items * (int64_t)sizeof(ca::CacheSplit));
+      w.pieces = items * a.most_parts * piece_bytes;
+    }
+  } else if (most_tokens > kWholeTokens) {
+    a.way = ca::kShares;
+    a.workgroups = many ? ca::many_workgroups(a.tile_rows) : ca::few_workgroups(a.D);
+    a.least_steps = many ? kLeastManySteps : kLeastFewSteps;
     w.splits = padded256(a.workgroups * (int64_t)sizeof(ca::CacheSplit));
-    w.pieces = (int64_t)a.workgroups * 2 * tile * piece_bytes;
+    w.pieces = (int64_t)a.workgroups * 2 * piece_bytes;
   }
   return CA_OK;
 }
@@ -281,7 +290,7 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   a.causal = r->causal;
   a.window = r->window;
   a.tree = r->tree;
-  const hipError_t e = a.many ? ca::launch_attend_many(a, (hipStream_t)stream) : ca::launch_attend_few(a, (hipStream_t)stream);
+  const hipError_t e = a.tile_rows > ca::kFewRows ? ca::launch_attend_many(a, (hipStream_t)stream) : ca::launch_attend_few(a, (hipStream_t)stream);
   return e == hipSuccess ? CA_OK : hip_fail(e, "cache attention launch");
 }
 

@@ -40,7 +40,7 @@ struct View {
   int32_t lo, hi;  // behind the prompt
   int32_t frame;
 };
-__device__ __forceinline__ int32_t frame_at(const CacheArgs& a, const Sequence& q, int32_t place) { return place < q.origin ? -1 : (place - q.origin) / a.span; }
+__device__ __forceinline__ int32_t frame_at(const CacheArgs& a, const Sequence& q, int32_t place) { return place < q.origin ? -1 : divided(place - q.origin, a.span); }
 __device__ __forceinline__ View view_at(const AttendArgs& a, const Sequence& q, int32_t place) {
   View v;
   v.frame = frame_at(a, q, place);
@@ -73,26 +73,34 @@ __device__ __forceinline__ Walk<kStep> walk_of(const AttendArgs& a, const Sequen
   return w;
 }
 
-// The sequences on a line on which each takes up weight(sequence) places, one after the other.  All threads of a workgroup make it and ask it together.
-struct LineLds {
-  int64_t waves[16], rest;
-  int32_t sequence;
-};
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
+
+// The sequences on a line on which each takes up weight(sequence) places, one after the other.  All threads of a workgroup make it and ask it together.
+struct LineLds {
+  int64_t waves[8], rest, weight;
+  int32_t sequence;
+  Sequence q;
+};
 template <int kThreads>
 struct SequenceLine {
   int32_t from, to;   // the thread's sequences
   int64_t at, own;    // where they begin, what they take up
+  Sequence last;      // of them
   int64_t all;        // places, in scalar registers
   template <class Weight>
   __device__ __forceinline__ SequenceLine(const CacheArgs& a, LineLds& lds, Weight&& weight) {
+    if (a.sequences == 1) {  // nothing to look for
+      last = sequence_at(a, 0);
+      all = own = weight(last);
+      return;
+    }
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t per = (a.sequences + kThreads - 1) / kThreads;
     from = min(tid * per, a.sequences), to = min(from + per, a.sequences);
     own = 0;
-    for (int32_t s = from; s < to; ++s) own += weight(sequence_at(a, s));
+    for (int32_t s = from; s < to; ++s) last = sequence_at(a, s), own += weight(last);
     int64_t up = own;
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) {
@@ -110,29 +118,145 @@ struct SequenceLine {
     }
     all = uniform64(total);
   }
-  // The sequence that holds a place, and how far behind its first; false: there is no such place.
+  // The sequence that holds a place, what it takes up and how far behind its first the place is; false: there is no such place.
   template <class Weight>
-  __device__ __forceinline__ bool find(const CacheArgs& a, LineLds& lds, int64_t place, int32_t& sequence, int64_t& rest, Weight&& weight) const {
+  __device__ __forceinline__ bool find(const CacheArgs& a, LineLds& lds, int64_t place, int32_t& sequence, Sequence& q, int64_t& takes, int64_t& rest, Weight&& weight) const {
+    if (a.sequences == 1) {
+      sequence = 0, q = last, takes = all, rest = place;
+      return place >= 0 && place < all;
+    }
     if (place >= at && place < at + own) {
-      int64_t here = at;
-      for (int32_t s = from; s < to; ++s) {
-        const int64_t w = weight(sequence_at(a, s));
-        if (place < here + w) {
-          lds.sequence = s;
-          lds.rest = place - here;
-          break;
+      int64_t here = at, w = own;
+      int32_t s = from;
+      Sequence mine = last;
+      if (to - from > 1)
+        for (;; ++s) {
+          mine = sequence_at(a, s);
+          w = weight(mine);
+          if (place < here + w) break;
+          here += w;
         }
-        here += w;
-      }
+      lds.sequence = s;
+      lds.q = mine;
+      lds.weight = w;
+      lds.rest = place - here;
     }
     __syncthreads();
     sequence = __builtin_amdgcn_readfirstlane(lds.sequence);
+    if (sequence < 0) return false;
+    q.first = __builtin_amdgcn_readfirstlane(lds.q.first), q.count = __builtin_amdgcn_readfirstlane(lds.q.count);
+    q.length = __builtin_amdgcn_readfirstlane(lds.q.length), q.origin = __builtin_amdgcn_readfirstlane(lds.q.origin), q.base = __builtin_amdgcn_readfirstlane(lds.q.base);
+    takes = uniform64(lds.weight);
     rest = uniform64(lds.rest);
-    return sequence >= 0;
+    return true;
   }
 };
 
-__device__ __forceinline__ int32_t row_tiles(const AttendArgs& a, const Sequence& q, int rows) { return (int32_t)(((int64_t)q.count * a.group + rows - 1) / rows); }
+__device__ __forceinline__ int32_t row_tiles(const AttendArgs& a, const Sequence& q, int rows) { return (q.count * a.group + rows - 1) / rows; }  // (rows of a call: at most 2^30)
+
+// Steps of a tile of rows.
+template <int kRows, int kStep>
+__device__ __forceinline__ Walk<kStep> tile_walk(const AttendArgs& a, const Sequence& q, int32_t tile) {
+  const int32_t first = tile * kRows, last = min(first + kRows, q.count * a.group) - 1;
+  return walk_of<kStep>(a, q, divided(first, a.group), divided(last, a.group));
+}
+
+// A workgroup's share of a launch of items (tiles of rows and key heads), in one of three ways.
+//   kItems   an item a workgroup.
+//   kShares  The steps of all items lie on one line: sequences, their key heads, their tiles.  A workgroup takes an even share of the line, whatever items that cuts: a batch of sequences of
+//            very different lengths is as even as one of equal ones.  An item takes up kItemCost places before its steps, for the time it takes to begin one.
+//   kParts   Items are cut into equal parts.  Tiles of one key head and part begin together, on one XCD, and walk over their keys side by side: its L2 serves all of them.
+// Sums of an item that is cut are left as pieces, which a second kernel joins.  An item without steps has one, with nothing to read: its results are written.
+template <int kRows, int kStep, int kThreads, int kItemCost>
+struct Share {
+  int32_t sequence, key_head, tile, tiles;
+  Sequence q;
+  Walk<kStep> walk;
+  int32_t count, done, steps;  // of the item: its steps, those before this workgroup's, this workgroup's
+  bool whole;                  // they are all
+  int64_t size, left, place;   // kShares: places of a share, those not taken yet, its number; kParts: place of the item
+  int32_t part, parts;         // kParts
+  int32_t begun = 0;           // pieces of an item that begins here
+
+  __device__ __forceinline__ static int64_t places_of(const AttendArgs& a, const Sequence& q) {
+    int64_t all = 0;
+    for (int32_t t = 0, n = row_tiles(a, q, kRows); t < n; ++t) all += kItemCost + max(1, tile_walk<kRows, kStep>(a, q, t).count);
+    return all * a.kv_heads;
+  }
+  // false: there is nothing to do
+  __device__ __forceinline__ bool begin(const AttendArgs& a, LineLds& lds, int64_t workgroup) {
+    place = workgroup;
+    const auto tiles_of = [&](const Sequence& s) { return (int64_t)row_tiles(a, s, kRows); };
+    const auto all_places = [&](const Sequence& s) { return places_of(a, s); };
+    int64_t rest, takes;
+    tile = done = 0;
+    if (a.way == kShares) {
+      const SequenceLine<kThreads> line(a, lds, all_places);
+      size = max((int64_t)a.least_steps, (line.all + a.workgroups - 1) / a.workgroups);
+      left = min(size, line.all - workgroup * size);
+      if (left < 1 || !line.find(a, lds, workgroup * size, sequence, q, takes, rest, all_places)) return false;
+      tiles = row_tiles(a, q, kRows);
+      const int64_t per_head = a.kv_heads == 1 ? takes : takes / a.kv_heads;
+      key_head = a.kv_heads == 1 ? 0 : (int32_t)(rest / per_head);
+      rest -= key_head * per_head;
+      for (int32_t c; (c = kItemCost + max(1, tile_walk<kRows, kStep>(a, q, tile).count)) <= rest; ++tile) rest -= c;
+      return take_share(a, (int32_t)rest);
+    }
+    const int64_t items = a.tiles * a.kv_heads;
+    part = (int32_t)((uint32_t)workgroup / (uint32_t)items);  // (launches have fewer than 2^24 workgroups)
+    place = workgroup - part * items;
+    key_head = (int32_t)((uint32_t)place / (uint32_t)a.tiles);
+    const SequenceLine<kThreads> line(a, lds, tiles_of);
+    // the last tiles come first: in a causal order they see most
+    if (!line.find(a, lds, a.tiles - 1 - (place - key_head * a.tiles), sequence, q, takes, rest, tiles_of)) return false;
+    tiles = (int32_t)takes;
+    tile = (int32_t)rest;
+    walk = tile_walk<kRows, kStep>(a, q, tile);
+    count = max(1, walk.count);
+    parts = a.way == kParts ? max(1, min((count + a.part_steps - 1) / a.part_steps, a.most_parts)) : 1;
+    const int32_t each = (count + parts - 1) / parts;
+    done = min(count, part * each);
+    steps = min(count - done, each);
+    whole = parts == 1;
+    if (part == 0 && parts > 1) begun = parts;
+    return part < parts;
+  }
+  // What is left of the share begins `from` places behind the first of the item.  false: it ends before the item's steps.
+  __device__ __forceinline__ bool take_share(const AttendArgs& a, int32_t from) {
+    walk = tile_walk<kRows, kStep>(a, q, tile);
+    count = max(1, walk.count);
+    const int32_t all = kItemCost + count, to = (int32_t)min((int64_t)all, from + left), rest = all - to;
+    left -= to - from;
+    done = max(0, from - kItemCost);
+    steps = max(0, to - kItemCost) - done;
+    whole = steps == count;
+    if (steps > 0 && done == 0 && rest > 0) begun = size >= rest ? 2 : 1 + (int32_t)((uint32_t)(rest + (int32_t)size - 1) / (uint32_t)size);
+    return steps > 0;
+  }
+  // Rows of sums of this piece.
+  __device__ __forceinline__ float* piece(const AttendArgs& a, int D) const {
+    return a.pieces + (a.way == kShares ? place * 2 + (done > 0) : place * a.most_parts + part) * kRows * piece_row(D);
+  }
+  // The next item; false: there is none.
+  __device__ __forceinline__ bool next(const AttendArgs& a) {
+    if (a.way != kShares || left < 1) return false;
+    if (++tile == tiles) {
+      tile = 0;
+      if (++key_head == a.kv_heads) {
+        key_head = 0;
+        do q = sequence_at(a, ++sequence);
+        while (q.count == 0);
+        tiles = row_tiles(a, q, kRows);
+      }
+    }
+    return take_share(a, 0);
+  }
+  // What the second kernel has to know: of an item that begins here, in how many pieces it lies.
+  __device__ __forceinline__ void leave(const AttendArgs& a, bool any) const {
+    if (a.way == kItems || (a.way == kParts && part > 0)) return;
+    if (threadIdx.x == 0) a.splits[place] = any && begun > 1 ? CacheSplit{sequence, key_head, tile, begun} : CacheSplit{0, 0, 0, 0};
+  }
+};
 
 // The unit of scores, see ScoreRule; a lane's query head has its own slope.
 struct CacheRule {
@@ -154,9 +278,9 @@ struct CacheRow {
   int32_t prompt;     // what it sees of it
   uint64_t drafts;
   float slope;        // in units of the scores, negative
-  __device__ __forceinline__ CacheRow(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int64_t index) {
-    const int32_t i = (int32_t)(index / a.group);
-    head = key_head * a.group + (int32_t)(index - (int64_t)i * a.group);
+  __device__ __forceinline__ CacheRow(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int32_t index) {
+    const int32_t i = divided(index, a.group);
+    head = key_head * a.group + (index - i * a.group);
     row = i < q.count ? q.first + i : -1;
     const bool there = row >= 0 && q.base + i >= 0;
     drafts = there && a.tree ? draft_bits(a, q, row) : 0;
@@ -263,13 +387,14 @@ struct SlicePlaces {
   }
   __device__ __forceinline__ void ask(const AttendArgs& a, const Sequence& q, int32_t s, const Walk<kStep>& w, int32_t step, int32_t end, int lane) {
     const int64_t token = token_of(q, w, step, end, lane);
-    page = token < q.length ? a.table[(int64_t)s * a.table_width + (int32_t)token / a.page_tokens] : -1;
+    page = token < q.length ? a.table[(int64_t)s * a.table_width + divided((int32_t)token, a.page_tokens)] : -1;
   }
   __device__ __forceinline__ void take(const AttendArgs& a, const Sequence& q, int32_t head, const Walk<kStep>& w, int32_t step, int32_t end, int lane, int row_bytes) {
     first = step;
     const int64_t token = token_of(q, w, step, end, lane);
     const bool here = page >= 0 && page < a.num_pages;
-    offset = here ? cache_row(a, page, head, (int32_t)token % a.page_tokens) * row_bytes : 0;
+    const int32_t slot = (int32_t)token - divided((int32_t)token, a.page_tokens) * a.page_tokens;
+    offset = here ? cache_row(a, page, head, slot) * row_bytes : 0;
     there = __builtin_amdgcn_ballot_w64(here);
   }
   // Called for every step in turn, from `begin` on.
@@ -317,8 +442,8 @@ __device__ __forceinline__ float frame_of_token(const AttendArgs& a, const Seque
 
 // Writes a row's four channels from the joined sums.
 template <int D>
-__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int64_t row, int channel, const floatx4& o, float ref, float total) {
-  const int32_t t = (int32_t)(row / a.group), head = key_head * a.group + (int32_t)(row - (int64_t)t * a.group);
+__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int32_t row, int channel, const floatx4& o, float ref, float total) {
+  const int32_t t = divided(row, a.group), head = key_head * a.group + (row - t * a.group);
   const int64_t at = (int64_t)(q.first + t) * a.heads + head;
   const bool real = total != 0.f;
   bf16x4 v;
@@ -341,33 +466,41 @@ struct Joined {
   }
 };
 
-// Joins the pieces of a row, in their order; piece(k): where the k-th lies (D sums, reference, sum of weights).  Threads take four channels each, and so many of them together a part of the pieces.
-template <int D, int kThreads>
-struct JoinLds {
-  static constexpr int kColumns = D / 4, kParts = kThreads / kColumns;
-  floatx4 sums[kParts][kColumns];
-  float2 stats[kParts];
-};
-template <int D, int kThreads, class Piece>
-__device__ __forceinline__ void join_row(const AttendArgs& a, const Sequence& q, int32_t key_head, int64_t row, int pieces, JoinLds<D, kThreads>& lds, Piece&& piece) {
-  constexpr int kColumns = JoinLds<D, kThreads>::kColumns, kParts = JoinLds<D, kThreads>::kParts;
-  const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns;
+// Joins the pieces of the item that begins at place blockIdx.x, in their order.  Threads take four channels of a row each, and kParts of them together a part of the
+// pieces.  Bound: latency, and the pieces once.
+template <int D, int kRows, int kThreads, int kParts>
+__device__ __forceinline__ void join_pieces(const AttendArgs& a) {
+  constexpr int kColumns = D / 4, kRowsAtOnce = kThreads / kColumns / kParts;
+  __shared__ floatx4 sums[kParts > 1 ? kRowsAtOnce : 1][kParts][kColumns];
+  __shared__ float2 stats[kParts > 1 ? kRowsAtOnce : 1][kParts];
+  const CacheSplit split = a.splits[blockIdx.x];
+  if (split.pieces == 0) return;
+  const Sequence q = sequence_at(a, split.sequence);
   const CacheRule rule(a);
-  Joined j;
+  const int32_t first_row = split.tile * kRows, rows = min(kRows, q.count * a.group - first_row);
+  const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns % kParts, within = threadIdx.x / kColumns / kParts;
+  for (int r0 = blockIdx.y * kRowsAtOnce; r0 < rows; r0 += gridDim.y * kRowsAtOnce) {
+    const int r = r0 + within;
+    Joined j;
+    if (r < rows) {
 #pragma unroll 4
-  for (int k = part; k < pieces; k += kParts) {
-    const float* from = piece(k);
-    const float2 stat = *reinterpret_cast<const float2*>(from + D);
-    j.add(rule, stat.x, stat.y, *reinterpret_cast<const floatx4*>(from + column * 4));
+      for (int k = part; k < split.pieces; k += kParts) {
+        const int64_t piece = a.way == kShares ? ((int64_t)blockIdx.x + k) * 2 + (k > 0) : (int64_t)blockIdx.x * a.most_parts + k;
+        const float* from = a.pieces + (piece * kRows + r) * piece_row(D);
+        const float2 stat = *reinterpret_cast<const float2*>(from + D);
+        j.add(rule, stat.x, stat.y, *reinterpret_cast<const floatx4*>(from + column * 4));
+      }
+    }
+    if constexpr (kParts > 1) {
+      sums[within][part][column] = j.o;
+      if (column == 0) stats[within][part] = float2{j.ref, j.total};
+      __syncthreads();
+      if (part == 0)
+        for (int k = 1; k < kParts && k < split.pieces; ++k) j.add(rule, stats[within][k].x, stats[within][k].y, sums[within][k][column]);
+    }
+    if (r < rows && part == 0) store_row<D>(a, rule, q, split.key_head, first_row + r, column * 4, j.o, j.ref, j.total);
+    if constexpr (kParts > 1) __syncthreads();
   }
-  lds.sums[part][column] = j.o;
-  if (column == 0) lds.stats[part] = float2{j.ref, j.total};
-  __syncthreads();
-  if (part == 0) {
-    for (int k = 1; k < kParts && k < pieces; ++k) j.add(rule, lds.stats[k].x, lds.stats[k].y, lds.sums[k][column]);
-    store_row<D>(a, rule, q, key_head, row, column * 4, j.o, j.ref, j.total);
-  }
-  __syncthreads();
 }
 
 }  // namespace

@@ -5,7 +5,7 @@ namespace ca {
 namespace {
 
 constexpr int kFewWaves = 4, kFewThreads = kFewWaves * 64;
-constexpr int kLeastFewSteps = 8;  // of a workgroup's share: two a wave
+constexpr int kFewItemCost = 8;  // steps that a workgroup's four waves do in the time that it takes to begin an item
 
 // A wave's own part of LDS: two buffers of a step; at the end its sums, row by row.
 template <class S>
@@ -18,17 +18,6 @@ struct FewWave {
   float frames[kFewStep];
 };
 
-// Steps of a tile of rows; a tile without any is still one, so that its results are written.
-__device__ __forceinline__ Walk<kFewStep> few_walk(const AttendArgs& a, const Sequence& q, int64_t tile) {
-  const int64_t first = tile * kFewRows, last = min(first + kFewRows, (int64_t)q.count * a.group) - 1;
-  return walk_of<kFewStep>(a, q, (int32_t)(first / a.group), (int32_t)(last / a.group));
-}
-__device__ __forceinline__ int64_t few_steps(const AttendArgs& a, const Sequence& q) {
-  int64_t all = 0;
-  for (int32_t t = 0, n = row_tiles(a, q, kFewRows); t < n; ++t) all += max(1, few_walk(a, q, t).count);
-  return all * a.kv_heads;
-}
-
 // Where an item's sums go: LDS holds those of the waves.
 template <int D>
 __device__ __forceinline__ Joined join_waves(const CacheRule& rule, const FewWave<CacheShape<D>>* lds, int row, int channel) {
@@ -38,54 +27,31 @@ __device__ __forceinline__ Joined join_waves(const CacheRule& rule, const FewWav
   return j;
 }
 
-// The steps of all items lie on one line: sequences, their key heads, their tiles.  A workgroup takes an even share of the line, whatever items that cuts (a batch of sequences
-// of very different lengths is as even as one of equal ones), and of an item its waves a quarter of the steps each; they join their sums at the end.  An item that
-// lies in several shares is joined by few_rows_join_kernel.
+// Of an item the waves of a workgroup take a quarter of the steps each; they join their sums at the end.
 template <int D>
 __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2))) void few_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
   __shared__ FewWave<S> lds[kFewWaves];
   __shared__ LineLds found;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
-  const bool split = a.workgroups > 0;
-  const auto weight = [&](const Sequence& q) { return split ? few_steps(a, q) : (int64_t)row_tiles(a, q, kFewRows) * a.kv_heads; };
-  const SequenceLine<kFewThreads> line(a, found, weight);
-  const int64_t share = split ? max((int64_t)kLeastFewSteps, (line.all + a.workgroups - 1) / a.workgroups) : 1, first = blockIdx.x * share;
-  int64_t left = min(share, line.all - first), done;
-  int32_t s, begun = 0;
-  if (left < 1 || !line.find(a, found, first, s, done, weight)) {
-    if (split && threadIdx.x == 0) a.splits[blockIdx.x] = CacheSplit{0, 0, 0, 0};
+  Share<kFewRows, kFewStep, kFewThreads, kFewItemCost> share;
+  if (!share.begin(a, found, blockIdx.x)) {
+    share.leave(a, false);
     return;
   }
   const CacheRule rule(a);
-  Sequence q = sequence_at(a, s);
-  // the first item, and how many of its steps lie in other shares
-  int32_t tiles = row_tiles(a, q, kFewRows), key_head, tile = 0;
-  if (split) {
-    const int64_t per_head = few_steps(a, q) / a.kv_heads;
-    key_head = (int32_t)(done / per_head);
-    done -= key_head * per_head;
-    for (int32_t c; (c = max(1, few_walk(a, q, tile).count)) <= done; ++tile) done -= c;
-  } else {
-    key_head = (int32_t)(done / tiles);
-    tile = (int32_t)(done - (int64_t)key_head * tiles);
-    done = 0;
-  }
-
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   FewWave<S>& mine = lds[wave];
   const uint32_t lds_steps = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine.steps[0][0];
   while (true) {
-    const int64_t first_row = (int64_t)tile * kFewRows;
-    const int rows = (int)min((int64_t)kFewRows, (int64_t)q.count * a.group - first_row);
-    const int32_t first_token = (int32_t)(first_row / a.group), last_token = (int32_t)((first_row + rows - 1) / a.group);
-    const Walk<kFewStep> walk = walk_of<kFewStep>(a, q, first_token, last_token);
-    const int32_t count = max(1, walk.count), steps = split ? (int32_t)min((int64_t)count - done, left) : count;
+    const Sequence& q = share.q;
+    const int32_t s = share.sequence, key_head = share.key_head;
+    const Walk<kFewStep> walk = share.walk;
+    const int32_t first_row = share.tile * kFewRows, rows = min(kFewRows, q.count * a.group - first_row);
+    const int32_t first_token = divided(first_row, a.group), last_token = divided(first_row + rows - 1, a.group);
     CacheRow own(a, rule, q, key_head, first_row + i);
     const int32_t own_row = own.row >= 0 ? own.row : q.first + first_token, own_head = own.row >= 0 ? own.head : key_head * a.group;
-    asm volatile("" : "+v"(own.slope), "+v"(own.drafts));  // (waited for here, not in the loop)
-    const OwnOperand<S, S::kContraction> query(static_cast<const char*>(a.q) + (own_row * a.q_strides.token + own_head * a.q_strides.head) * 2, g, nullptr);
     // what all rows of the tile see, in scalar registers
     const int32_t sure_prompt = prompt_end(a, q), sure_hi = q.base < 0 ? 0 : a.tree ? q.base : view_at(a, q, q.base + first_token).hi;
     const int32_t sure_lo = view_at(a, q, a.tree ? max(q.length - 1, 0) : max(q.base + last_token, 0)).lo;
@@ -95,8 +61,8 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
     for (auto& t : sum) t = splat(0.f);
     Softmax soft;
 
-    const int32_t end = min((int32_t)done + steps, walk.count), part = (steps + kFewWaves - 1) / kFewWaves;
-    const int32_t from = min(end, (int32_t)done + wave * part), to = min(end, from + part);
+    const int32_t end = min(share.done + share.steps, walk.count), part = (share.steps + kFewWaves - 1) / kFewWaves;
+    const int32_t from = min(end, share.done + wave * part), to = min(end, from + part);
     SlicePlaces<2, kFewStep> places;
     auto issue = [&](int32_t step) {
       places.at_step(a, q, s, key_head, walk, step, from, to, lane, S::kRowBytes);
@@ -114,6 +80,9 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
       issue(from);
       there = places.mask(from);
     }
+    // (loaded while the first copies are on their way)
+    const OwnOperand<S, S::kContraction> query(static_cast<const char*>(a.q) + (own_row * a.q_strides.token + own_head * a.q_strides.head) * 2, g, nullptr);
+    asm volatile("" : "+v"(own.slope), "+v"(own.drafts));  // (waited for here, not in the loop)
     for (int32_t step = from; step < to; ++step) {
       if (step + 1 < to) {
         issue(step + 1);
@@ -152,9 +121,8 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
         *reinterpret_cast<floatx4*>(&mine.sums[i][db * 32 + 8 * j + 4 * g]) = floatx4{sum[db][4 * j], sum[db][4 * j + 1], sum[db][4 * j + 2], sum[db][4 * j + 3]};
     if (g == 0) mine.sums[i][D] = soft.ref, mine.sums[i][D + 1] = total;
     __syncthreads();
-    const bool whole = steps == count;
-    // sums of an item that is begun here go to the first place of the workgroup, of one that others have begun to the second
-    float* const piece = whole ? nullptr : a.pieces + ((int64_t)blockIdx.x * 2 + (done > 0)) * kFewRows * piece_row(D);
+    const bool whole = share.whole;
+    float* const piece = whole ? nullptr : share.piece(a, D);
     for (int item = threadIdx.x; item < rows * (D / 4); item += kFewThreads) {
       const int r = item / (D / 4), c = item % (D / 4) * 4;
       const Joined j = join_waves<D>(rule, lds, r, c);
@@ -165,48 +133,23 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
         if (c == 0) *reinterpret_cast<float2*>(piece + r * piece_row(D) + D) = float2{j.ref, j.total};
       }
     }
-    if (!whole && done == 0) {
-      begun = 1 + (int32_t)((count - steps + share - 1) / share);
-      break;
-    }
-    left -= steps;
-    if (!split || left < 1) break;
-    // the next item
-    done = 0;
-    if (++tile == tiles) {
-      tile = 0;
-      if (++key_head == a.kv_heads) {
-        key_head = 0;
-        do q = sequence_at(a, ++s);
-        while (q.count == 0);
-        tiles = row_tiles(a, q, kFewRows);
-      }
-    }
+    if (!share.next(a)) break;
     __syncthreads();  // (the sums lie where the next steps go)
   }
-  if (split && threadIdx.x == 0) a.splits[blockIdx.x] = CacheSplit{s, key_head, tile, begun};
+  share.leave(a, true);
 }
 
-// Bound: latency.  A workgroup takes some rows of the item that one workgroup of few_rows_kernel has begun.
 template <int D>
 __global__ __launch_bounds__(kFewThreads) void few_rows_join_kernel(AttendArgs a) {
-  __shared__ JoinLds<D, kFewThreads> lds;
-  const CacheSplit split = a.splits[blockIdx.x];
-  if (split.pieces == 0) return;
-  const Sequence q = sequence_at(a, split.sequence);
-  const int64_t first_row = (int64_t)split.tile * kFewRows;
-  const int rows = (int)min((int64_t)kFewRows, (int64_t)q.count * a.group - first_row);
-  for (int r = blockIdx.y; r < rows; r += gridDim.y)
-    join_row<D>(a, q, split.key_head, first_row + r, split.pieces, lds,
-                [&](int k) { return a.pieces + ((((int64_t)blockIdx.x + k) * 2 + (k > 0)) * kFewRows + r) * piece_row(D); });
+  join_pieces<D, kFewRows, kFewThreads, kFewThreads / (D / 4)>(a);
 }
 
 template <int D>
 hipError_t launch_few_rows(const AttendArgs& a, hipStream_t stream) {
-  const int64_t workgroups = a.workgroups > 0 ? a.workgroups : a.tiles * a.kv_heads;
-  if (workgroups < 1 || workgroups > 0xffffff) return hipErrorInvalidValue;  // (2^32 threads)
+  const int64_t workgroups = a.way == kShares ? a.workgroups : a.tiles * a.kv_heads;
+  if (a.way == kParts || workgroups < 1 || workgroups > 0xffffff) return hipErrorInvalidValue;  // (2^32 threads)
   few_rows_kernel<D><<<(unsigned)workgroups, kFewThreads, 0, stream>>>(a);
-  if (a.workgroups > 0) {
+  if (a.way == kShares) {
     // a workgroup for every row that a sequence has on average, as far as a tile has them
     const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group;
     few_rows_join_kernel<D><<<dim3((unsigned)workgroups, (unsigned)(rows < kFewRows ? rows : kFewRows)), kFewThreads, 0, stream>>>(a);

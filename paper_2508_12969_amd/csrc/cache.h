@@ -38,10 +38,13 @@ struct KeepArgs : CacheArgs {
   int32_t width, row_bytes;
 };
 
-// An item (a tile of rows and a key head) that a workgroup begins and others go on with.
+// How a launch is shared out among workgroups, see Share.
+enum CacheWay { kItems, kShares, kParts };
+
+// An item (a tile of rows and a key head) that is cut.
 struct CacheSplit {
   int32_t sequence, key_head, tile;
-  int32_t pieces;  // of one workgroup after the other; 0: this workgroup begins none such
+  int32_t pieces;  // 0: there is none at this place
 };
 
 struct AttendArgs : CacheArgs {
@@ -54,21 +57,20 @@ struct AttendArgs : CacheArgs {
   const float* slopes;         // [heads] or null
   int32_t causal, window;
   const uint64_t* tree;        // [tokens] or null
-  bool many;                   // rows a sequence: tiles of kManyRows, else of kFewRows
+  int32_t tile_rows;           // kFewRows, or 128 or 256 of many rows
   int64_t tiles;               // most row tiles that the sequences can have together
-  // few rows
-  int32_t workgroups;          // that share all steps evenly; 0: a workgroup for every item
-  CacheSplit* splits;          // workspace: [workgroups]
-  // many rows
-  int32_t part_steps, most_parts;  // tiles of more steps are cut into parts
+  CacheWay way;
+  int32_t workgroups, least_steps;  // kShares: workgroups, least steps of a share
+  int32_t part_steps, most_parts;   // kParts: items of more steps are cut
+  CacheSplit* splits;          // workspace: [workgroups], or (kParts) [tiles * kv_heads]
   float* pieces;               // workspace: [workgroups][2], or [tiles * kv_heads][most_parts], of [rows of a tile][piece_row(D)]
 };
 
 // A few rows a sequence are taken in tiles of 32, which read their keys and values in steps of 32 tokens.
 constexpr int kFewRows = 32, kFewStep = 32;
-// Many rows are taken in tiles of 128, with steps of 64 tokens that the waves of a workgroup share.
-constexpr int kManyRows = 128, kManyStep = 64;
-constexpr int kManyPlaces = 512;  // workgroups that the device holds at a time
+// Many rows are taken in tiles of 128 or 256, with steps of 64 tokens that the waves of a workgroup share.
+constexpr int kManyStep = 64;
+constexpr int many_workgroups(int tile_rows) { return tile_rows == 128 ? 512 : 256; }  // that the device holds at a time
 // Workgroups that the device holds at a time: one per compute unit at head dim 128 (its buffers fill the LDS), two at 64.
 constexpr int few_workgroups(int D) { return D == 128 ? 256 : 512; }
 // Sums of a row: D, then the reference of the exponent and the sum of weights; rows begin at 16 bytes, and in different banks of LDS.

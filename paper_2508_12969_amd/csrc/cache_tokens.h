@@ -23,9 +23,12 @@ __device__ __forceinline__ Sequence sequence_at(const CacheArgs& a, int32_t s) {
   return q;
 }
 
+// x / by, in 32 bits; plain tokens and ungrouped heads divide by one.
+__device__ __forceinline__ int32_t divided(int32_t x, int32_t by) { return by == 1 ? x : (int32_t)((uint32_t)x / (uint32_t)by); }
+
 // Page of a token that the table has an entry for, -1 where it is not there.
 __device__ __forceinline__ int32_t page_at(const CacheArgs& a, int32_t s, int32_t token) {
-  const int32_t page = a.table[(int64_t)s * a.table_width + token / a.page_tokens];
+  const int32_t page = a.table[(int64_t)s * a.table_width + divided(token, a.page_tokens)];
   return page >= 0 && page < a.num_pages ? page : -1;
 }
 
