@@ -14,18 +14,32 @@ namespace {
 
 constexpr int kKeepThreads = 256;
 
-// The sequence that a row of the packed tensors belongs to: the last one that starts at or before it.
-__device__ __forceinline__ int32_t sequence_of_row(const CacheArgs& a, int32_t row) {
-  int32_t lo = 0, hi = a.sequences;  // starts[lo] <= row < starts[hi], where starts ascends
-  while (hi - lo > 1) {
-    const int32_t mid = (int32_t)(((uint32_t)lo + (uint32_t)hi) / 2);
-    if (a.starts[mid] <= row) lo = mid;
-    else hi = mid;
+// The sequence that a row of the packed tensors belongs to: the last one that starts at or before it.  A wave's rows, first to last, follow each other: its lanes look at 64 sequences at a time
+// for that of the first row, those of the others are among the next ones.
+__device__ __forceinline__ int32_t sequence_of_row(const CacheArgs& a, int32_t first, int32_t last, int32_t row, int lane) {
+  int32_t base = 0, count = a.sequences;  // starts[base] <= first, where starts ascends, and that of the sequence after these is past it
+  while (true) {
+    const int32_t stride = (count + 63) / 64, start = a.starts[base + min(lane * stride, count - 1)];
+    const int found = 63 - (int)__builtin_clzll(__builtin_amdgcn_ballot_w64(start <= first) | 1);
+    if (stride > 1) {
+      const int32_t from = min(found * stride, count - 1);
+      base += from;
+      count = min(stride, count - from);
+      continue;
+    }
+    int32_t s = base + min(found, count - 1), k = min(found, count - 1) + 1;
+    for (; k < min(count, 64); ++k) {
+      const int32_t next = __builtin_amdgcn_readlane(start, k);
+      if (next > last) return s;
+      if (next <= row) s = base + k;
+    }
+    for (k += base; k < a.sequences && a.starts[k] <= last; ++k)
+      if (a.starts[k] <= row) s = k;
+    return s;
   }
-  return lo;
 }
 
-// Heads are walked in the order q, k, v; blockIdx.y takes heads_per_block of them.
+// Heads are walked in the order q, k, v; blockIdx.y takes heads_per_block of them.  kHeads of them are loaded while those before are computed, the first ones while the wave looks for its sequences.
 template <class T, Pairing kPairing, bool kNorm>
 __global__ __launch_bounds__(kRowThreads) void append_kernel(AppendArgs a, int heads_per_block) {
   constexpr int kVec = Row<T>::kVec, kHeads = 4;
@@ -33,96 +47,108 @@ __global__ __launch_bounds__(kRowThreads) void append_kernel(AppendArgs a, int h
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Part p = part_of<T>(a, lane);
   const int64_t at = (((int64_t)blockIdx.x * kRowWaves + wave) << (6 - p.lanes_log2)) + p.row;
-  const int32_t row = (int32_t)min(at, (int64_t)a.tokens - 1);
-  const int32_t s = sequence_of_row(a, row);
+  const int32_t row = (int32_t)min(at, (int64_t)a.tokens - 1), first_row = (int32_t)min(at - p.row, (int64_t)a.tokens - 1);  // (first_row: of the wave)
+  const int32_t last_row = (int32_t)min(at - p.row + ((1 << (6 - p.lanes_log2)) - 1), (int64_t)a.tokens - 1);
+  const int h0 = blockIdx.y * heads_per_block, h1 = min(a.heads + 2 * a.kv_heads, h0 + heads_per_block);
+  const int keys = a.heads, values = a.heads + a.kv_heads;  // where they begin
+  const int64_t q_at = row * a.q_strides.token, k_at = row * a.k_strides.token, v_at = row * a.v_strides.token;
+  auto source = [&](int h) {
+    return h < keys     ? static_cast<const T*>(a.q) + q_at + h * a.q_strides.head
+           : h < values ? static_cast<const T*>(a.k_new) + k_at + (h - keys) * a.k_strides.head
+                        : static_cast<const T*>(a.v_new) + v_at + (h - values) * a.v_strides.head;
+  };
+  Chunk next[kHeads];
+  auto load = [&](int h) {
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i)
+      if (h + i < h1) next[i] = *reinterpret_cast<const Chunk*>(source(h + i) + p.first);
+  };
+  load(h0);
+  Chunk q_weight, k_weight;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) q_weight[e] = k_weight[e] = (T)1.f;
+  if (kNorm && a.q_weight && h0 < keys) q_weight = *reinterpret_cast<const Chunk*>(static_cast<const T*>(a.q_weight) + p.first);
+  if (kNorm && a.k_weight && h0 < values && h1 > keys) k_weight = *reinterpret_cast<const Chunk*>(static_cast<const T*>(a.k_weight) + p.first);
+
+  const int32_t s = sequence_of_row(a, __builtin_amdgcn_readfirstlane(first_row), __builtin_amdgcn_readfirstlane(last_row), row, lane);
   const Sequence seq = sequence_at(a, s);
   const bool live = p.live && at < a.tokens && row >= seq.first && row < seq.first + seq.count;
   const int32_t token = seq.base + (row - seq.first);
   const bool exists = live && token >= 0 && token < seq.length;
-  const int32_t page = exists ? page_at(a, s, token) : -1, slot = exists ? token % a.page_tokens : 0;
+  const int32_t entry = exists ? divided(token, a.page_tokens) : 0, slot = exists ? token - entry * a.page_tokens : 0;
+  const int32_t in_table = a.table[(int64_t)s * a.table_width + entry];  // (looked at when it is there)
 
   Turn<kVec> turn;
   no_turn(turn);
-  if (a.angles && exists) {
+  if (a.angles && exists && h0 < values) {
     int where[3];
     if (a.where) {
 #pragma unroll
       for (int i = 0; i < 3; ++i) where[i] = a.where[(int64_t)row * 3 + i];
     } else {
-      const int32_t behind = token - seq.origin, line = behind / a.frame_w;
-      const int32_t of[3] = {line / a.frame_h, line % a.frame_h, behind % a.frame_w};
+      const int32_t behind = token - seq.origin, line = behind < 0 ? 0 : divided(behind, a.frame_w), frame = divided(line, a.frame_h);
+      const int32_t of[3] = {frame, line - frame * a.frame_h, behind - line * a.frame_w};
 #pragma unroll
       for (int i = 0; i < 3; ++i) where[i] = behind < 0 ? -1 : (int)min((int64_t)a.origin[i] + of[i], (int64_t)0x7fffffff);
     }
-    make_turn<T, kPairing != kNeighbours>(a, p, where, turn);
+    make_turn<T, kPairing != kNeighbours>(a, p, where[0], where[1], where[2], turn);
   }
   const Exchange<T> exchange(a, p, lane);
-  const int h0 = blockIdx.y * heads_per_block, h1 = min(a.heads + 2 * a.kv_heads, h0 + heads_per_block);
-
+  // y = own_c x + other_c partner (times r), of queries and of keys
+  float q_own[kVec], q_other[kVec], k_own[kVec], k_other[kVec];
+  auto weigh = [&](const void* weight, const Chunk& w, float (&own_c)[kVec], float (&other_c)[kVec]) {
+    Chunk wp;
+    if constexpr (kPairing == kHalves) wp = exchange(w);
+    if constexpr (kPairing == kApart) {
 #pragma unroll
-  for (int tensor = 0; tensor < 2; ++tensor) {
-    const int first = tensor ? a.heads : 0, count = tensor ? a.kv_heads : a.heads, from = max(h0 - first, 0), to = min(h1 - first, count);
-    if (from >= to) continue;
-    const TokenStrides ss = tensor ? a.k_strides : a.q_strides;
-    const T* __restrict__ src = static_cast<const T*>(tensor ? a.k_new : a.q) + row * ss.token;
-    const bool store = tensor ? page >= 0 : live;
-    const int64_t dst_head = tensor ? (int64_t)a.page_tokens * a.D : a.D;
-    T* __restrict__ dst = static_cast<T*>(tensor ? a.k : a.q_out) + (tensor ? cache_row(a, max(page, 0), 0, slot) * a.D : (int64_t)row * a.heads * a.D) + p.first;
-    float own_c[kVec], other_c[kVec];  // y = own_c x + other_c partner (times r)
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) own_c[e] = turn.c[e], other_c[e] = turn.s[e];
-    if constexpr (kNorm) {
-      float w[kVec], wp[kVec];
-      load_weights<T, kPairing>(a, p, tensor ? a.k_weight : a.q_weight, w, wp);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) own_c[e] *= w[e], other_c[e] = from_partner(other_c[e], wp[e]);
+      for (int e = 0; e < kVec; ++e) wp[e] = (T)1.f;
+      if (kNorm && weight) wp = load_partner<T>(a, p, static_cast<const T*>(weight));
     }
-    for (int h = from; h < to; h += kHeads) {
-      Chunk own[kHeads], other[kHeads];
 #pragma unroll
-      for (int i = 0; i < kHeads; ++i) {
-        if (h + i < to && live) {
-          const T* r = src + (h + i) * ss.head;
-          own[i] = *reinterpret_cast<const Chunk*>(r + p.first);
-          if constexpr (kPairing == kApart) other[i] = load_partner<T>(a, p, r);
-        } else {
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) own[i][e] = other[i][e] = (T)0.f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kHeads; ++i) {
-        if (h + i >= to) break;
-        if constexpr (kPairing == kHalves) other[i] = exchange(own[i]);
-        float r = 1.f;
-        if constexpr (kNorm) {
-          float sum = 0.f;
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) sum += live ? (float)own[i][e] * (float)own[i][e] : 0.f;
-          r = rsqrtf(row_sum(sum, p.lanes_log2) / a.D + a.eps);
-        }
-        Chunk y;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float x = (float)own[i][e], xp = kPairing == kNeighbours ? (float)own[i][e ^ 1] : (float)other[i][e];
-          y[e] = (T)(r * (own_c[e] * x + from_partner(other_c[e], xp)));
-        }
-        if (store) *reinterpret_cast<Chunk*>(dst + (h + i) * dst_head) = y;
-      }
+    for (int e = 0; e < kVec; ++e) {
+      own_c[e] = turn.c[e], other_c[e] = turn.s[e];
+      if (kNorm) own_c[e] *= (float)w[e], other_c[e] = from_partner(other_c[e], kPairing == kNeighbours ? (float)w[e ^ 1] : (float)wp[e]);
     }
-  }
+  };
+  weigh(a.q_weight, q_weight, q_own, q_other);
+  weigh(a.k_weight, k_weight, k_own, k_other);
+  const int32_t page = exists && in_table >= 0 && in_table < a.num_pages ? in_table : -1;
+  T* const q_out = static_cast<T*>(a.q_out) + (int64_t)row * a.heads * a.D + p.first;
+  const int64_t in_page = cache_row(a, max(page, 0), 0, slot) * a.D + p.first, page_head = (int64_t)a.page_tokens * a.D;
 
-  const int first = a.heads + a.kv_heads, from = max(h0 - first, 0), to = min(h1 - first, a.kv_heads);
-  const T* __restrict__ src = static_cast<const T*>(a.v_new) + row * a.v_strides.token + p.first;
-  T* __restrict__ dst = static_cast<T*>(a.v) + cache_row(a, max(page, 0), 0, slot) * a.D + p.first;
-  for (int h = from; h < to; h += kHeads) {
+  for (int h = h0; h < h1; h += kHeads) {
     Chunk own[kHeads];
 #pragma unroll
-    for (int i = 0; i < kHeads; ++i)
-      if (h + i < to && page >= 0) own[i] = *reinterpret_cast<const Chunk*>(src + (h + i) * a.v_strides.head);
+    for (int i = 0; i < kHeads; ++i) own[i] = next[i];
+    load(h + kHeads);
 #pragma unroll
-    for (int i = 0; i < kHeads; ++i)
-      if (h + i < to && page >= 0) *reinterpret_cast<Chunk*>(dst + (int64_t)(h + i) * a.page_tokens * a.D) = own[i];
+    for (int i = 0; i < kHeads; ++i) {
+      const int head = h + i;
+      if (head >= h1) break;
+      if (head >= values) {
+        if (page >= 0) __builtin_nontemporal_store(own[i], reinterpret_cast<Chunk*>(static_cast<T*>(a.v) + in_page + (head - values) * page_head));
+        continue;
+      }
+      const bool key = head >= keys;
+      Chunk other;
+      if constexpr (kPairing == kHalves) other = exchange(own[i]);
+      if constexpr (kPairing == kApart) other = load_partner<T>(a, p, source(head));
+      float r = 1.f;
+      if constexpr (kNorm) {
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum += p.live ? (float)own[i][e] * (float)own[i][e] : 0.f;
+        r = rsqrtf(row_sum(sum, p.lanes_log2) / a.D + a.eps);
+      }
+      Chunk y;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float x = (float)own[i][e], xp = kPairing == kNeighbours ? (float)own[i][e ^ 1] : (float)other[e];
+        y[e] = (T)(r * ((key ? k_own[e] : q_own[e]) * x + from_partner(key ? k_other[e] : q_other[e], xp)));
+      }
+      if (key ? page >= 0 : live)
+        __builtin_nontemporal_store(y, reinterpret_cast<Chunk*>(key ? static_cast<T*>(a.k) + in_page + (head - keys) * page_head : q_out + head * (int64_t)a.D));
+    }
   }
 }
 

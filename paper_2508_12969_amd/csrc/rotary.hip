@@ -28,7 +28,7 @@ __device__ __forceinline__ void make_turn(const RowArgs& a, const Part& p, const
 #pragma unroll
     for (int i = 0; i < 3; ++i) at[i] += a.origin[i];
   }
-  make_turn<T, kHalf>(a, p, at, turn);
+  make_turn<T, kHalf>(a, p, at[0], at[1], at[2], turn);
 }
 
 // Forward calls and the transposed rotation.  Rows are walked in the order of dst; heads are split over blockIdx.y where there are few tokens.
