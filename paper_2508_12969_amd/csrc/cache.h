@@ -35,7 +35,7 @@ struct AppendArgs : CacheArgs, RowRule {
 
 struct KeepArgs : CacheArgs {
   const int32_t *kept, *counts;
-  int32_t width, row_bytes;
+  int32_t width, row_bytes, heads_per_block;
 };
 
 // How a launch is shared out among workgroups, see Share.
