@@ -2,8 +2,9 @@
 import ctypes
 
 from . import binding
-from .binding import CA_BF16, CA_ERR_ALLOC, CA_F32, CompactAttnError, _check, _lend, _stream_ptr, load_library
-from .rotary import _on, _on_current_device, _table, ca_strides, ca_where
+from .binding import CA_BF16, CA_ERR_ALLOC, CA_F32, CompactAttnError, _lend, _stream_ptr, load_library
+from .binding import _check as _check_status
+from .rotary import _on, _table, ca_strides, ca_where
 
 
 class ca_cache(ctypes.Structure):
@@ -24,14 +25,12 @@ class ca_reach(ctypes.Structure):
                 ("tree", ctypes.c_void_p)]
 
 
-def _check_ints(t, shape, name, device=None):
-    import torch
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the pages are on {device}")
-    if tuple(t.shape) != shape or t.dtype != torch.int32 or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape}")
+def _check(t, cache, shape, dtype, name):
+    """A contiguous tensor beside the pages."""
+    if t.get_device() != cache._device:   # (-1: not a device tensor)
+        raise ValueError(f"{name} is on {t.device}, the cache on cuda:{cache._device}")
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
 
 
 class Cache:
@@ -49,69 +48,95 @@ class Cache:
                 raise ValueError(f"pages of {name} must be a contiguous device tensor, those of k and v alike")
         if table.dim() != 2:
             raise ValueError("table has a row for every sequence")
-        sequences = table.shape[0]
-        for name, t, shape in (("table", table, tuple(table.shape)), ("lengths", lengths, (sequences,)), ("starts", starts, (sequences + 1,)), ("origins", origins, (sequences,))):
-            if t is not None:
-                _check_ints(t, shape, name, k.device)
         if len(frame) != 2:
             raise ValueError("frame has a height and a width")
+        self._device = k.get_device()
+        sequences = table.shape[0]
+        for name, t, shape in (("table", table, table.shape), ("lengths", lengths, (sequences,)), ("starts", starts, (sequences + 1,)), ("origins", origins, (sequences,))):
+            if t is not None:
+                _check(t, self, shape, torch.int32, name)
         self.k, self.v, self.table, self.lengths, self.starts, self.origins, self.frame = k, v, table, lengths, starts, origins, tuple(frame)
-        pages, kv_heads, page_tokens, head_dim = k.shape
-        self._args = (k.data_ptr(), v.data_ptr(), pages, page_tokens, kv_heads, head_dim, CA_BF16 if k.dtype == torch.bfloat16 else CA_F32, sequences, table.shape[1],
+        pages, self._kv_heads, page_tokens, self._head_dim = k.shape
+        self._dtype = k.dtype
+        self._args = (k.data_ptr(), v.data_ptr(), pages, page_tokens, self._kv_heads, self._head_dim, CA_BF16 if k.dtype == torch.bfloat16 else CA_F32, sequences, table.shape[1],
                       table.data_ptr(), lengths.data_ptr(), starts.data_ptr(), None if origins is None else origins.data_ptr())
+        self._of = {}          # ca_cache by tokens of a call
         self._workspace = {}   # bytes by (tokens, heads)
 
-    def _of(self, tokens):
-        return ca_cache(*self._args, tokens, *self.frame)
+
+def _of(cache, tokens):
+    """The ca_cache of a call of so many tokens, on the current device."""
+    import torch
+    if torch._C._cuda_getDevice() != cache._device:
+        raise ValueError(f"the cache is on cuda:{cache._device}, the current device is cuda:{torch.cuda.current_device()}")
+    args = cache._of.get(tokens)
+    if args is None:
+        if len(cache._of) >= 64:
+            cache._of.clear()
+            cache._workspace.clear()
+        args = cache._of[tokens] = ca_cache(*cache._args, tokens, *cache.frame)
+    return args
 
 
-def _packed(t, cache, heads, name):
+def _packed(t, cache, tokens, heads, name):
     """A packed tensor of rows; the strides to hand over, None where it is contiguous."""
-    _on_current_device(t, name)
-    if t.dtype != cache.k.dtype:
-        raise ValueError(f"{name} has dtype {t.dtype}, the cache {cache.k.dtype}")
-    if t.dim() != 3 or t.shape[2] != cache.k.shape[3] or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [tokens, {'heads' if heads is None else heads}, {cache.k.shape[3]}]")
+    if t.get_device() != cache._device:
+        raise ValueError(f"{name} is on {t.device}, the cache on cuda:{cache._device}")
+    if t.dtype is not cache._dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, the cache {cache._dtype}")
+    if t.shape != (tokens, heads, cache._head_dim):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(tokens, heads, cache._head_dim)}")
     if t.is_contiguous():
         return None
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    token, head, channel = t.stride()
+    if channel != 1 and cache._head_dim > 1:
         raise ValueError(f"channels of {name} must be contiguous")
-    return ca_strides(0, *(t.stride(i) if t.shape[i] > 1 else 0 for i in (1, 0)))
+    return ctypes.pointer(ca_strides(0, head if heads > 1 else 0, token if tokens > 1 else 0))
+
+
+def _rows(t, name):
+    """(tokens, heads) of a packed tensor."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected tokens, heads and channels")
+    return t.shape[:2]
 
 
 def compact_attn_cache_append(k, v, cache, q=None, norm=True, q_weight=None, k_weight=None, rotary=None, eps=1e-6, origin=(0, 0, 0), positions=None, out=None, stream=None):
     """Stores keys and values [tokens, kv_heads, D] of new tokens in their pages, keys with norm (times k_weight [D]) and rotation, and returns the queries q [tokens, heads, D] with theirs
     (None without q).  Any strides with contiguous channels.  Tokens are turned by origin + (frame, row, column), or by positions int32 [tokens, 3].  out: where to write the queries."""
-    _on_current_device(cache.k, "the cache")
-    tokens = k.shape[0]
-    kv_heads = cache.k.shape[1]
-    strides = [None if t is None else _packed(t, cache, heads, name) for name, t, heads in (("q", q, None), ("k", k, kv_heads), ("v", v, kv_heads))]
-    for name, t in (("q", q), ("v", v)):
-        if t is not None and t.shape[0] != tokens:
-            raise ValueError(f"{name} has {t.shape[0]} tokens, k has {tokens}")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _on_current_device(w, name)
-            if w.dtype != cache.k.dtype or tuple(w.shape) != (cache.k.shape[3],) or not w.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous {cache.k.dtype} tensor of {cache.k.shape[3]} elements")
+    tokens, heads = k.shape[0], 0
+    args = _of(cache, tokens)
+    append = ca_append(None, k.data_ptr(), v.data_ptr())
+    append.k_strides, append.v_strides = _packed(k, cache, tokens, cache._kv_heads, "k"), _packed(v, cache, tokens, cache._kv_heads, "v")
+    if q is not None:
+        heads = _rows(q, "q")[1]
+        append.q_strides = _packed(q, cache, tokens, heads, "q")
+        if out is None:
+            with _on(stream, q.device):
+                out = q.new_empty(q.shape)
+        elif _packed(out, cache, tokens, heads, "out") is not None:
+            raise ValueError("out must be contiguous")
+        append.q, append.q_out, append.heads = q.data_ptr(), out.data_ptr(), heads
+    elif out is not None:
+        raise ValueError("out without q")
+    append.normed, append.eps = bool(norm), eps
+    if q_weight is not None:
+        _check(q_weight, cache, (cache._head_dim,), cache._dtype, "q_weight")
+        append.q_weight = q_weight.data_ptr()
+    if k_weight is not None:
+        _check(k_weight, cache, (cache._head_dim,), cache._dtype, "k_weight")
+        append.k_weight = k_weight.data_ptr()
+    append.rotary = _table(rotary)
     if len(origin) != 3:
         raise ValueError("origin has a value for each of three axes")
-    if positions is not None:
-        _on_current_device(positions, "positions")
-        _check_ints(positions, (tokens, 3), "positions")
-    if q is None:
-        if out is not None:
-            raise ValueError("out without q")
-    elif out is None:
-        with _on(stream, q.device):
-            out = q.new_empty(q.shape)
-    elif _packed(out, cache, q.shape[1], "out") is not None or out.shape[0] != tokens:
-        raise ValueError("out must be contiguous, of the shape of q")
-    where = None if positions is None and tuple(origin) == (0, 0, 0) else ctypes.pointer(ca_where((ctypes.c_int32 * 3)(*origin), None if positions is None else positions.data_ptr()))
-    at = lambda t: None if t is None else t.data_ptr()
-    append = ca_append(at(q), at(k), at(v), *(None if s is None else ctypes.pointer(s) for s in strides), at(out), 0 if q is None else q.shape[1], int(bool(norm)), at(q_weight),
-                       at(k_weight), eps, _table(rotary), where)
-    _check(load_library().compact_attn_cache_append(append, cache._of(tokens), _stream_ptr(stream)))
+    if positions is not None or tuple(origin) != (0, 0, 0):
+        where = ca_where((ctypes.c_int32 * 3)(*origin), None)
+        if positions is not None:
+            import torch
+            _check(positions, cache, (tokens, 3), torch.int32, "positions")
+            where.positions = positions.data_ptr()
+        append.where = ctypes.pointer(where)
+    _check_status(load_library().compact_attn_cache_append(append, args, _stream_ptr(stream)))
     return out
 
 
@@ -120,53 +145,48 @@ def compact_attn_cache_attend(q, cache, scale=0.0, cap=0.0, slopes=None, causal=
     without) over the prompt and the frames up to their own (causal), the last `window` of them (0: all), or the drafts that the bits of tree (int64 or uint64 [tokens]) say.
     -> (out [tokens, heads, D], lse float32 [tokens, heads]); out: such a pair to write to."""
     import torch
-    _on_current_device(cache.k, "the cache")
-    strides = _packed(q, cache, None, "q")
-    tokens, heads = q.shape[:2]
+    tokens, heads = _rows(q, "q")
+    args, lib = _of(cache, tokens), load_library()
+    strides = _packed(q, cache, tokens, heads, "q")
+    reach = ca_reach(scale, cap, None, bool(causal), window)
     if slopes is not None:
-        _on_current_device(slopes, "slopes")
-        if tuple(slopes.shape) != (heads,) or slopes.dtype != torch.float32 or not slopes.is_contiguous():
-            raise ValueError(f"slopes must be a contiguous float32 tensor of shape {(heads,)}")
+        _check(slopes, cache, (heads,), torch.float32, "slopes")
+        reach.slopes = slopes.data_ptr()
     if tree is not None:
-        _on_current_device(tree, "tree")
-        if tuple(tree.shape) != (tokens,) or tree.dtype not in (torch.int64, torch.uint64) or not tree.is_contiguous():
-            raise ValueError(f"tree must be a contiguous int64 or uint64 tensor of shape {(tokens,)}")
+        _check(tree, cache, (tokens,), torch.int64 if tree.dtype is torch.int64 else torch.uint64, "tree")
+        reach.tree = tree.data_ptr()
     if out is None:
         with _on(stream, q.device):
             out = q.new_empty(q.shape), q.new_empty((tokens, heads), dtype=torch.float32)
     else:
-        if _packed(out[0], cache, heads, "out") is not None or out[0].shape[0] != tokens:
-            raise ValueError("out must be contiguous, of the shape of q")
-        _on_current_device(out[1], "lse of out")
-        if tuple(out[1].shape) != (tokens, heads) or out[1].dtype != torch.float32 or not out[1].is_contiguous():
-            raise ValueError(f"lse of out must be a contiguous float32 tensor of shape {(tokens, heads)}")
-    args, lib = cache._of(tokens), load_library()
+        if _packed(out[0], cache, tokens, heads, "out") is not None:
+            raise ValueError("out must be contiguous")
+        _check(out[1], cache, (tokens, heads), torch.float32, "lse of out")
     need = cache._workspace.get((tokens, heads))
     if need is None:
         size = ctypes.c_int64()
-        _check(lib.compact_attn_cache_workspace(args, heads, size))
+        _check_status(lib.compact_attn_cache_workspace(args, heads, size))
         need = cache._workspace[tokens, heads] = size.value
     workspace = None
     if need:
         workspace = _lend(q, need, stream)
         if workspace is None or workspace is NotImplemented:
             raise CompactAttnError(CA_ERR_ALLOC, f"no memory for a workspace of {need} bytes, or a capture that torch does not run")
-    reach = ca_reach(scale, cap, None if slopes is None else slopes.data_ptr(), int(bool(causal)), window, None if tree is None else tree.data_ptr())
-    _check(lib.compact_attn_cache_attend(q.data_ptr(), strides, heads, args, reach, out[0].data_ptr(), out[1].data_ptr(), None if workspace is None else workspace.data_ptr(), need,
-                                         _stream_ptr(stream)))
+    _check_status(lib.compact_attn_cache_attend(q.data_ptr(), strides, heads, args, reach, out[0].data_ptr(), out[1].data_ptr(),
+                                                None if workspace is None else workspace.data_ptr(), need, _stream_ptr(stream)))
     return tuple(out)
 
 
 def compact_attn_cache_keep(cache, kept, counts, stream=None):
     """Keeps some of the last call's new tokens (those of lengths and starts): new token kept[s, j] becomes new token j, for j < counts[s], in the pages.  kept: int32 [sequences, up to 64],
     counts: int32 [sequences]."""
-    _on_current_device(cache.k, "the cache")
+    import torch
+    args, sequences = _of(cache, 2 ** 31 - 1), cache.table.shape[0]
     if kept.dim() != 2:
         raise ValueError("kept has a row for every sequence")
-    sequences = cache.table.shape[0]
-    _check_ints(kept, (sequences, kept.shape[1]), "kept", cache.k.device)
-    _check_ints(counts, (sequences,), "counts", cache.k.device)
-    _check(load_library().compact_attn_cache_keep(cache._of(2 ** 31 - 1), kept.data_ptr(), kept.shape[1], counts.data_ptr(), _stream_ptr(stream)))
+    _check(kept, cache, (sequences, kept.shape[1]), torch.int32, "kept")
+    _check(counts, cache, (sequences,), torch.int32, "counts")
+    _check_status(load_library().compact_attn_cache_keep(args, kept.data_ptr(), kept.shape[1], counts.data_ptr(), _stream_ptr(stream)))
 
 
 def _declare(lib):
