@@ -5,7 +5,7 @@ namespace ca {
 namespace {
 
 constexpr int kManySlices = kManyStep / kSlice;
-constexpr int kManyItemCost = 2;     // steps that a workgroup does in the time that it takes to begin an item
+constexpr int kManyItemCost = 4;     // steps that a workgroup does in the time that it takes to begin an item; 16 trees with 2 / 3 / 4: 88 / 82 / 78 us
 constexpr int kPlacedSteps = 128;    // whose slices are looked up together
 
 template <class S, int kWaves, int kBuffers>
@@ -27,8 +27,8 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kWaves * 64, kWaves * 64),
   __shared__ Lds lds;
   __shared__ LineLds found;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
-  // neighbours on the line, or tiles of one key head, are on one XCD
-  const int64_t total = gridDim.x, workgroup = a.way == kShares ? blockIdx.x % 8 * (total / 8) + blockIdx.x / 8 : xcd_launch_order(blockIdx.x, total, xcd_chunk(total));
+  // Neighbours on the line, or tiles of one key head, are on one XCD (a frame of 13 tiles a head in chunks of 13 / as the ids come 391 / 418 us, 85 tiles in chunks of 64 / 8 4.90 / 5.09 ms).
+  const int64_t total = gridDim.x, workgroup = a.way == kShares ? blockIdx.x % 8 * (total / 8) + blockIdx.x / 8 : xcd_launch_order(blockIdx.x, total, min(a.tiles, kXcdChunk));
   Share<kRows, kManyStep, kThreads, kManyItemCost> share;
   if (!share.begin(a, found, workgroup)) {
     share.leave(a, false);
