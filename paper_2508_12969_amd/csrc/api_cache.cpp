@@ -158,7 +158,7 @@ int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // kItemSteps steps besides its own, and kPieceSteps more where its sums are joined.
 void cut_items(ca::AttendArgs& a, int64_t steps) {
   constexpr int64_t kItemSteps = 6, kPieceSteps = 4, kMostParts = 64, kMostPieceBytes = (int64_t)256 << 20;
-  const int64_t items = a.tiles * a.kv_heads, piece_bytes = (int64_t)a.tile_rows * ca::piece_row(a.D) * 4, places = ca::many_workgroups(a.tile_rows);
+  const int64_t items = a.tiles * a.kv_heads, piece_bytes = (int64_t)ca::kManyRows * ca::piece_row(a.D) * 4, places = ca::many_places(a.D);
   int64_t best = 1, best_end = 0;
   for (int64_t parts = 1; parts <= kMostParts; ++parts) {
     const int64_t size = (steps + parts - 1) / parts;
@@ -171,21 +171,23 @@ void cut_items(ca::AttendArgs& a, int64_t steps) {
   a.part_steps = (int32_t)((steps + best - 1) / best);
 }
 
-// Sizes of a call's launch.
-int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t heads) {
+// How a call's launch is shared out (Share).  Tiles that walk side by side cost their keys one reading, an even line cuts anything evenly: three frames over 75K tokens 4.9 / 6.0 ms, but 8 sequences
+// of very different lengths with 680 rows each 211 / 120 us.  So the former where all tiles are alike (one sequence, all of it seen), or so many that they are even without being cut.  What no
+// window takes up in the workspace, and what one does, is asked for alike.
+int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t heads, bool window) {
   fill_cache(a, c);
   a.heads = heads;
   a.group = heads / c->kv_heads;
   a.D = c->head_dim;
   const int64_t most_tokens = (int64_t)c->table_width * c->page_tokens, rows = (int64_t)((c->tokens + (int64_t)c->sequences - 1) / c->sequences) * a.group;
-  const bool many = rows > ca::kFewRows;
-  a.tile_rows = !many ? ca::kFewRows : rows > 128 && rows < kSideBySide ? 256 : 128;
-  const int64_t piece_bytes = (int64_t)a.tile_rows * ca::piece_row(a.D) * 4;
-  a.tiles = (int64_t)c->tokens * a.group / a.tile_rows + std::min(c->tokens, c->sequences);
+  a.many = rows > ca::kFewRows;
+  const int64_t tile = a.many ? ca::kManyRows : ca::kFewRows, piece_bytes = tile * ca::piece_row(a.D) * 4;
+  a.tiles = (int64_t)c->tokens * a.group / tile + std::min(c->tokens, c->sequences);
   if (a.tiles * c->kv_heads > 0xffffff / 64 || (int64_t)c->tokens * a.group > kMostTokens) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
   const int64_t items = a.tiles * c->kv_heads;
   a.way = ca::kItems;  // (items of a few steps are not worth a second launch)
-  if (rows >= kSideBySide) {
+  const bool side_by_side = rows >= kSideBySide && ((c->sequences == 1 && !window) || items >= 2 * ca::many_places(a.D));
+  if (side_by_side) {
     cut_items(a, (most_tokens + ca::kManyStep - 1) / ca::kManyStep);
     if (a.way == ca::kParts) {
       w.splits = padded256(items * (int64_t)sizeof(ca::CacheSplit));
@@ -193,8 +195,8 @@ int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t head
     }
   } else if (most_tokens > kWholeTokens) {
     a.way = ca::kShares;
-    a.workgroups = many ? ca::many_workgroups(a.tile_rows) : ca::few_workgroups(a.D);
-    a.least_steps = many ? kLeastManySteps : kLeastFewSteps;
+    a.workgroups = a.many ? ca::kManyWorkgroups : ca::few_workgroups(a.D);
+    a.least_steps = a.many ? kLeastManySteps : kLeastFewSteps;
     w.splits = padded256(a.workgroups * (int64_t)sizeof(ca::CacheSplit));
     w.pieces = (int64_t)a.workgroups * 2 * piece_bytes;
   }
@@ -250,9 +252,10 @@ int compact_attn_cache_workspace(const ca_cache* c, int32_t heads, int64_t* work
   int st = check_cache(c);
   if (st == CA_OK) st = check_attend(c, nullptr, heads);
   ca::AttendArgs a{};
-  Workspace w;
-  if (st == CA_OK) st = fill_attend(a, w, c, heads);
-  if (st == CA_OK) *workspace_bytes = w.bytes();
+  Workspace w, windowed;
+  if (st == CA_OK) st = fill_attend(a, w, c, heads, false);
+  if (st == CA_OK) st = fill_attend(a, windowed, c, heads, true);
+  if (st == CA_OK) *workspace_bytes = std::max(w.bytes(), windowed.bytes());
   return st;
 }
 
@@ -269,7 +272,7 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   int64_t q_bytes = 0;
   st = packed_strides(c, q_strides, heads, "q", a.q_strides, q_bytes);
   Workspace w;
-  if (st == CA_OK) st = fill_attend(a, w, c, heads);
+  if (st == CA_OK) st = fill_attend(a, w, c, heads, r->window > 0);
   if (st != CA_OK) return st;
   const int64_t need = c->tokens > 0 ? w.bytes() : 0, rows = (int64_t)c->tokens * heads, pages = page_bytes(c);
   if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) {
@@ -290,7 +293,7 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   a.causal = r->causal;
   a.window = r->window;
   a.tree = r->tree;
-  const hipError_t e = a.tile_rows > ca::kFewRows ? ca::launch_attend_many(a, (hipStream_t)stream) : ca::launch_attend_few(a, (hipStream_t)stream);
+  const hipError_t e = a.many ? ca::launch_attend_many(a, (hipStream_t)stream) : ca::launch_attend_few(a, (hipStream_t)stream);
   return e == hipSuccess ? CA_OK : hip_fail(e, "cache attention launch");
 }
 

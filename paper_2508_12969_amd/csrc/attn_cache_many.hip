@@ -4,32 +4,36 @@
 namespace ca {
 namespace {
 
-constexpr int kManySlices = kManyStep / kSlice;
+constexpr int kManyWaves = kManyRows / 32, kManyThreads = kManyWaves * 64, kManySlices = kManyStep / kSlice;
+static_assert(kManyWaves == kManySlices, "a wave copies a slice");
 constexpr int kManyItemCost = 4;     // steps that a workgroup does in the time that it takes to begin an item; 16 trees with 2 / 3 / 4: 88 / 82 / 78 us
 constexpr int kPlacedSteps = 128;    // whose slices are looked up together
 
-template <class S, int kWaves, int kBuffers>
+// Waves per SIMD that the registers leave room for: a third at head dim 64 (three frames over 75K tokens, 10 heads, two / three 2.74 / 2.50 ms, four prompts of 9K, 32 heads, 1104 / 982 us; with
+// shares of a line, whose launches are short, six sequences of 52 rows 35 / 44 us; four spill).
+constexpr int many_waves(int D, bool line) { return D == 64 && !line ? 3 : 2; }
+
+template <class S>
 struct ManyLds {
   static constexpr int kStepBytes = kManyStep * S::kRowBytes;
-  char x[kBuffers][kStepBytes], y[kBuffers][kStepBytes];
-  float frames[kWaves][kManyStep];
+  char x[2][kStepBytes], y[2][kStepBytes];
+  float frames[kManyWaves][kManyStep];
   int64_t places[kPlacedSteps * kManySlices];  // where slices lie, -1: not there
 };
 
-// A workgroup takes a tile of rows, 32 a wave, over steps of 64 tokens that the waves copy together, some slices each.  Copies are kBuffers - 1 steps ahead.
-template <int D, bool kLine, int kWaves, int kBuffers>
-__global__ __attribute__((amdgpu_flat_work_group_size(kWaves * 64, kWaves * 64), amdgpu_waves_per_eu(2, 2))) void many_rows_kernel(AttendArgs a) {
+// A workgroup takes a tile of 128 rows, 32 a wave, over steps of 64 tokens that the waves copy together, a slice each, while the step before is computed.  (Tiles of 256 rows, which read their keys
+// half as often, with copies three steps ahead: 100 rows a key head 90 / 91 us, 225 rows 160 / 160, 75 rows 81 / 71, a frame of 1560 rows 401 / 391.)
+template <int D, bool kLine>
+__global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads), amdgpu_waves_per_eu(many_waves(D, kLine), many_waves(D, kLine)))) void many_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
-  typedef ManyLds<S, kWaves, kBuffers> Lds;
-  constexpr int kRows = kWaves * 32, kThreads = kWaves * 64, kBlocks = kManyStep / 32, kAhead = kBuffers - 1;
-  static_assert(kWaves == 4 || kWaves == 8, "a wave copies a slice of keys and one of values, or one of either");
-  constexpr int kCopies = (kWaves == 4 ? 2 : 1) * S::kSliceLoads;  // of a step, a wave's
+  typedef ManyLds<S> Lds;
+  constexpr int kBlocks = kManyStep / 32;
   __shared__ Lds lds;
   __shared__ LineLds found;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   // Neighbours on the line, or tiles of one key head, are on one XCD (a frame of 13 tiles a head in chunks of 13 / as the ids come 391 / 418 us, 85 tiles in chunks of 64 / 8 4.90 / 5.09 ms).
   const int64_t total = gridDim.x, workgroup = a.way == kShares ? blockIdx.x % 8 * (total / 8) + blockIdx.x / 8 : xcd_launch_order(blockIdx.x, total, min(a.tiles, kXcdChunk));
-  Share<kRows, kManyStep, kThreads, kManyItemCost> share;
+  Share<kManyRows, kManyStep, kManyThreads, kManyItemCost> share;
   if (!share.begin(a, found, workgroup)) {
     share.leave(a, false);
     return;
@@ -37,16 +41,15 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kWaves * 64, kWaves * 64),
   const CacheRule rule(a);
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
-  const int slice = wave % kManySlices;
-  const uint32_t lds_x = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.x[0] + slice * S::kSliceBytes;
-  const uint32_t lds_y = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.y[0] + slice * S::kSliceBytes;
+  const uint32_t lds_x = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.x[0] + wave * S::kSliceBytes;
+  const uint32_t lds_y = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.y[0] + wave * S::kSliceBytes;
   while (true) {
     const Sequence& q = share.q;
     const Walk<kManyStep> walk = share.walk;
     const int32_t from = min(walk.count, share.done), to = min(walk.count, share.done + share.steps);
     // Places of the slices from `first` on.
     auto look_up = [&](int32_t first) {
-      for (int at = threadIdx.x; at < kPlacedSteps * kManySlices; at += kThreads) {
+      for (int at = threadIdx.x; at < kPlacedSteps * kManySlices; at += kManyThreads) {
         const int32_t step = first + at / kManySlices;
         const int64_t token = step < to ? (int64_t)walk.token(step) + at % kManySlices * kSlice : q.length;
         int64_t place = -1;
@@ -58,26 +61,22 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kWaves * 64, kWaves * 64),
         if (step >= to) break;
       }
     };
-    uint32_t there = 0;  // four bits a step that is asked for: which of its slices are there
-    int asked = 0;
+    uint32_t there = 0;  // of the step that was asked for last: which of its slices are there
     auto issue = [&](int32_t step) {
       const int64_t mine = lds.places[((step - from) % kPlacedSteps) * kManySlices + lane % kManySlices];
-      there |= ((uint32_t)__builtin_amdgcn_ballot_w64(mine >= 0) & 15u) << (4 * asked);
-      ++asked;
-      const int64_t place = max((int64_t)0, (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), slice) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)mine, slice)));
-      const uint32_t buffer = (uint32_t)(step % kBuffers) * Lds::kStepBytes;
-      if (kWaves == 4 || wave < kManySlices) copy(static_cast<const char*>(a.k) + place, lds_x + buffer);
-      if (kWaves == 4 || wave >= kManySlices) copy(static_cast<const char*>(a.v) + place, lds_y + buffer);
+      there = (uint32_t)__builtin_amdgcn_ballot_w64(mine >= 0) & 15u;
+      const int64_t place = max((int64_t)0, (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), wave) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)mine, wave)));
+      const uint32_t buffer = (uint32_t)(step & 1) * Lds::kStepBytes;
+      copy(static_cast<const char*>(a.k) + place, lds_x + buffer);
+      copy(static_cast<const char*>(a.v) + place, lds_y + buffer);
     };
     if (from < to) {
       look_up(from);
       __syncthreads();
-#pragma unroll
-      for (int ahead = 0; ahead < kAhead; ++ahead)
-        if (from + ahead < to) issue(from + ahead);
+      issue(from);
     }
     // The wave's rows, loaded while the first copies are on their way, and what all of them, or any, see, in scalar registers.
-    const int32_t first_row = share.tile * kRows + wave * 32, rows = max(0, min(32, q.count * a.group - first_row));
+    const int32_t first_row = share.tile * kManyRows + wave * 32, rows = max(0, min(32, q.count * a.group - first_row));
     CacheRow own(a, rule, q, share.key_head, first_row + i);
     const int32_t own_row = own.row >= 0 ? own.row : q.first, own_head = own.row >= 0 ? own.head : share.key_head * a.group;
     const OwnOperand<S, S::kContraction> query(static_cast<const char*>(a.q) + (own_row * a.q_strides.token + own_head * a.q_strides.head) * 2, g, nullptr);
@@ -95,24 +94,20 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kWaves * 64, kWaves * 64),
     }
     Softmax soft;
     for (int32_t step = from; step < to; ++step) {
-      const int buffer = step % kBuffers;
+      const int buffer = step & 1;
       const int32_t token = walk.token(step);
-      const uint32_t here = there & 15u;
+      const uint32_t here = there;
       const bool full = here == 15u && token + kManyStep <= q.length;
-      if (kAhead > 1 && step + kAhead <= to) WAIT_VMCNT((kAhead - 1) * kCopies);
-      else WAIT_VMCNT(0);
-      if (!full && (kWaves == 4 || wave >= kManySlices))
-        clear_rows<S>(lds.y[buffer], (here >> slice) & 1u ? max(slice * kSlice, q.length - token) : slice * kSlice, (slice + 1) * kSlice, lane);
+      WAIT_VMCNT(0);
+      if (!full) clear_rows<S>(lds.y[buffer], (here >> wave) & 1u ? max(wave * kSlice, q.length - token) : wave * kSlice, (wave + 1) * kSlice, lane);
       WAIT_LGKMCNT0();
-      BARRIER();  // the step is there, and nobody reads the buffer before it any more
-      there >>= 4;
-      --asked;
-      if (step + kAhead < to) {
-        if ((step + kAhead - from) % kPlacedSteps == 0) {
-          look_up(step + kAhead);
+      BARRIER();  // the step is there, and nobody reads the other buffer any more
+      if (step + 1 < to) {
+        if ((step + 1 - from) % kPlacedSteps == 0) {
+          look_up(step + 1);
           __syncthreads();
         }
-        issue(step + kAhead);
+        issue(step + 1);
       }
       if (rows > 0 && (token < sure_prompt || (token < any_hi && token + kManyStep > any_lo))) {
         const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
@@ -164,21 +159,21 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kWaves * 64, kWaves * 64),
   share.leave(a, true);
 }
 
-template <int D, int kRows>
-__global__ __launch_bounds__(256) void many_rows_join_kernel(AttendArgs a) {
-  join_pieces<D, kRows, 256, 1>(a);
+template <int D>
+__global__ __launch_bounds__(kManyThreads) void many_rows_join_kernel(AttendArgs a) {
+  join_pieces<D, kManyRows, kManyThreads, 1>(a);
 }
 
-template <int D, int kWaves, int kBuffers>
+template <int D>
 hipError_t launch_many_rows(const AttendArgs& a, hipStream_t stream) {
-  constexpr int kRows = kWaves * 32, kRowsAtOnce = 1024 / D;  // of a workgroup that joins
+  constexpr int kRowsAtOnce = kManyThreads / (D / 4);  // of a workgroup that joins
   const int64_t items = a.tiles * a.kv_heads, workgroups = a.way == kShares ? a.workgroups : items * (a.way == kParts ? a.most_parts : 1);
   if (workgroups < 1 || workgroups > 0xffffff || (a.way == kShares && workgroups % 8 != 0)) return hipErrorInvalidValue;  // (2^32 threads)
-  if (a.way == kShares) many_rows_kernel<D, true, kWaves, kBuffers><<<(unsigned)workgroups, kWaves * 64, 0, stream>>>(a);
-  else many_rows_kernel<D, false, kWaves, kBuffers><<<(unsigned)workgroups, kWaves * 64, 0, stream>>>(a);
+  if (a.way == kShares) many_rows_kernel<D, true><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a);
+  else many_rows_kernel<D, false><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a);
   if (a.way != kItems) {
-    const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group, row_groups = ((rows < kRows ? rows : kRows) + kRowsAtOnce - 1) / kRowsAtOnce;
-    many_rows_join_kernel<D, kRows><<<dim3((unsigned)(a.way == kShares ? workgroups : items), (unsigned)row_groups), 256, 0, stream>>>(a);
+    const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group, row_groups = ((rows < kManyRows ? rows : kManyRows) + kRowsAtOnce - 1) / kRowsAtOnce;
+    many_rows_join_kernel<D><<<dim3((unsigned)(a.way == kShares ? workgroups : items), (unsigned)row_groups), kManyThreads, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
@@ -186,9 +181,7 @@ hipError_t launch_many_rows(const AttendArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attend_many(const AttendArgs& a, hipStream_t stream) {
-  if (a.tile_rows == 256) return a.D == 64 ? launch_many_rows<64, 8, 4>(a, stream) : launch_many_rows<128, 8, 4>(a, stream);
-  if (a.tile_rows == 128) return a.D == 64 ? launch_many_rows<64, 4, 4>(a, stream) : launch_many_rows<128, 4, 2>(a, stream);
-  return hipErrorInvalidValue;
+  return a.D == 64 ? launch_many_rows<64>(a, stream) : launch_many_rows<128>(a, stream);
 }
 
 }  // namespace ca

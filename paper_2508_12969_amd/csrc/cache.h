@@ -57,7 +57,7 @@ struct AttendArgs : CacheArgs {
   const float* slopes;         // [heads] or null
   int32_t causal, window;
   const uint64_t* tree;        // [tokens] or null
-  int32_t tile_rows;           // kFewRows, or 128 or 256 of many rows
+  bool many;                   // rows a sequence: tiles of kManyRows, else of kFewRows
   int64_t tiles;               // most row tiles that the sequences can have together
   CacheWay way;
   int32_t workgroups, least_steps;  // kShares: workgroups, least steps of a share
@@ -68,11 +68,13 @@ struct AttendArgs : CacheArgs {
 
 // A few rows a sequence are taken in tiles of 32, which read their keys and values in steps of 32 tokens.
 constexpr int kFewRows = 32, kFewStep = 32;
-// Many rows are taken in tiles of 128 or 256, with steps of 64 tokens that the waves of a workgroup share.
-constexpr int kManyStep = 64;
-constexpr int many_workgroups(int tile_rows) { return tile_rows == 128 ? 512 : 256; }  // that the device holds at a time
 // Workgroups that the device holds at a time: one per compute unit at head dim 128 (its buffers fill the LDS), two at 64.
 constexpr int few_workgroups(int D) { return D == 128 ? 256 : 512; }
+// Many rows are taken in tiles of 128, with steps of 64 tokens that the waves of a workgroup share.
+constexpr int kManyRows = 128, kManyStep = 64;
+// Workgroups that the device holds at a time: with shares of a line, and of items or parts (many_waves).
+constexpr int kManyWorkgroups = 512;
+constexpr int many_places(int D) { return D == 64 ? 768 : 512; }
 // Sums of a row: D, then the reference of the exponent and the sum of weights; rows begin at 16 bytes, and in different banks of LDS.
 constexpr int piece_row(int D) { return D + 4; }
 
