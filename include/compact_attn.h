@@ -552,7 +552,7 @@ typedef struct {
  *   k' = R(p) (w * k * (mean(k^2) + eps)^-1/2),  q' likewise,  v as it is.
  * Positions: where->positions (int32[tokens][3], as compact_attn_rotate), or else where->origin + (frame, row, column) of the token; prompts are not rotated then.  A position past the
  * rotary table gives NaN.  Sums are fp32, results rounded once.  A page that is written must be in one place of the table only.  bf16 and f32; head_dim up to 512 (bf16) or 256
- * (f32), CA_ERR_UNSUPPORTED beyond.  q_out and the pages must not overlap the inputs or each other. */
+ * (f32) and fewer than 2^26 tokens, CA_ERR_UNSUPPORTED beyond.  q_out and the pages must not overlap the inputs or each other. */
 int compact_attn_cache_append(const ca_append* append, const ca_cache* cache, void* stream);
 
 /* How scores are bent and what is seen, as in ca_scores.
@@ -579,7 +579,8 @@ int compact_attn_cache_workspace(const ca_cache* cache, int32_t heads, int64_t* 
  *   out, lse   [tokens, heads, head_dim] of the cache's type and float [tokens, heads], contiguous.  A row that sees nothing has a zero result and minus infinity.
  *   workspace  16-byte aligned, not overlapping the tensors; must not be used by anything else until the call's work on `stream` has run.
  * Tokens below a sequence's length must have finite values unless all rows of their sequence see them; slots that hold no token may hold anything.  Weights are rounded to
- * bf16 before the product with v, sums are fp32 in an order that depends on the sizes and lengths alone.  bf16 with head_dim 64 and 128, otherwise CA_ERR_UNSUPPORTED. */
+ * bf16 before the product with v, sums are fp32 in an order that depends on the sizes and lengths alone.  bf16 with head_dim 64 and 128 and at most 2^30 rows (tokens x heads / kv_heads),
+ * otherwise CA_ERR_UNSUPPORTED. */
 int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_t heads, const ca_cache* cache, const ca_reach* reach, void* out, float* lse, void* workspace,
                               int64_t workspace_bytes, void* stream);
 

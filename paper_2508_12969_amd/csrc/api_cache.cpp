@@ -22,6 +22,8 @@ constexpr int64_t kMostTokens = (int64_t)1 << 30, kMostBytes = (int64_t)1 << 46;
 constexpr int32_t kMostSequences = 1 << 20;
 constexpr int64_t kWholeTokens = 512;  // sequences of at most so many are not cut
 constexpr int64_t kLeastFewSteps = 8, kLeastManySteps = 8;  // of a workgroup's share: 256 and 512 tokens
+constexpr int32_t kItemSequences = 512;  // every workgroup looks through all sequences for its own: of more, only as many workgroups as the device holds do
+constexpr int64_t kMostItems = 0xffffff / 64;  // 64 parts of each are a launch
 constexpr int64_t kSideBySide = 512;   // rows of a sequence from which on tiles walk side by side
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -157,7 +159,7 @@ int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // Equal parts of items of up to `steps` steps: launches of few items would leave compute units without work, or end with a round that is not full.  A workgroup takes as long as
 // kItemSteps steps besides its own, and kPieceSteps more where its sums are joined.
 void cut_items(ca::AttendArgs& a, int64_t steps) {
-  constexpr int64_t kItemSteps = 6, kPieceSteps = 4, kMostParts = 64, kMostPieceBytes = (int64_t)256 << 20;
+  constexpr int64_t kItemSteps = 6, kPieceSteps = 4, kMostParts = 63, kMostPieceBytes = (int64_t)256 << 20;
   const int64_t items = a.tiles * a.kv_heads, piece_bytes = (int64_t)ca::kManyRows * ca::piece_row(a.D) * 4, places = ca::many_places(a.D);
   int64_t best = 1, best_end = 0;
   for (int64_t parts = 1; parts <= kMostParts; ++parts) {
@@ -183,17 +185,17 @@ int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t head
   a.many = rows > ca::kFewRows;
   const int64_t tile = a.many ? ca::kManyRows : ca::kFewRows, piece_bytes = tile * ca::piece_row(a.D) * 4;
   a.tiles = (int64_t)c->tokens * a.group / tile + std::min(c->tokens, c->sequences);
-  if (a.tiles * c->kv_heads > 0xffffff / 64 || (int64_t)c->tokens * a.group > kMostTokens) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
+  if ((int64_t)c->tokens * a.group > kMostTokens) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
   const int64_t items = a.tiles * c->kv_heads;
   a.way = ca::kItems;  // (items of a few steps are not worth a second launch)
-  const bool side_by_side = rows >= kSideBySide && ((c->sequences == 1 && !window) || items >= 2 * ca::many_places(a.D));
+  const bool itemized = c->sequences <= kItemSequences && items <= kMostItems, side_by_side = itemized && rows >= kSideBySide && ((c->sequences == 1 && !window) || items >= 2 * ca::many_places(a.D));
   if (side_by_side) {
     cut_items(a, (most_tokens + ca::kManyStep - 1) / ca::kManyStep);
     if (a.way == ca::kParts) {
       w.splits = padded256(items * (int64_t)sizeof(ca::CacheSplit));
       w.pieces = items * a.most_parts * piece_bytes;
     }
-  } else if (most_tokens > kWholeTokens) {
+  } else if (most_tokens > kWholeTokens || !itemized) {
     a.way = ca::kShares;
     a.workgroups = a.many ? ca::kManyWorkgroups : ca::few_workgroups(a.D);
     a.least_steps = a.many ? kLeastManySteps : kLeastFewSteps;
@@ -219,6 +221,7 @@ int compact_attn_cache_append(const ca_append* p, const ca_cache* c, void* strea
   if (st == CA_OK) st = packed_strides(c, p->k_strides, c->kv_heads, "k", a.k_strides, k_bytes);
   if (st == CA_OK) st = packed_strides(c, p->v_strides, c->kv_heads, "v", a.v_strides, v_bytes);
   if (st != CA_OK) return st;
+  if (c->tokens >= 1 << 26) return fail(CA_ERR_UNSUPPORTED, "more than 2^26 - 1 new tokens");
   const int64_t row = (int64_t)c->head_dim * elem_size(c->dtype), out_bytes = (int64_t)c->tokens * heads * row, pages = page_bytes(c);
   const void* const positions = p->rotary && p->where ? p->where->positions : nullptr;
   st = check_apart(c, {{p->q_out, out_bytes}, {c->k, pages}, {c->v, pages}},

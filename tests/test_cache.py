@@ -87,6 +87,7 @@ def test_append_refusals():
                       (dict(q_out=P[6]), "overlap the inputs"), (dict(q_out=P[0]), "each other"), (dict(q_out=P[3]), "arrays"), (dict(k=P[0] + 4096), "overlap the inputs")):
         st, message = _append_call(**bad)
         assert st == -1 and text in message, (bad, st, message)
+    assert _append_call(_raw_cache(tokens=1 << 26))[0] == -2
     assert _append_call(_raw_cache(v=P[0]))[0] == -1 and _append_call(_raw_cache(kv_heads=33000))[0] == -2
     assert _append_call(_raw_cache(tokens=0), k=None, v=None, q=None, q_out=None)[0] == 0   # nothing to do
 
@@ -259,6 +260,11 @@ ATTEND = {
     "rows-cut-frames": dict(sequences=[(4000, 140), (70, 70)], kv=2, group=1, D=128, page=256, frame=(7, 10), origins=[333, 5], window=30, slopes=True),
     "rows-cut-tree": dict(sequences=[(5000, 64), (300, 33)], kv=1, group=4, D=64, page=64, tree=True),
     "few-cut-tree": dict(sequences=[(5000, 9), (300, 5), (0, 0), (777, 8)], kv=3, group=3, D=128, page=64, tree=True, slopes=True),
+    "many-sequences": dict(sequences=[((i * 53) % 40 + 20, 20 if i % 4 else 0) for i in range(530)], kv=1, group=3, D=64, page=32),
+    "side-by-side": dict(sequences=[(3000, 600)], kv=2, group=1, D=128, page=64),
+    "side-by-side-64": dict(sequences=[(2600, 700)], kv=1, group=2, D=64, page=48, frame=(7, 10), origins=[77], cap=20.0, slopes=True),
+    "side-by-side-window": dict(sequences=[(5000, 600)], kv=2, group=1, D=64, page=64, window=300),
+    "side-by-side-ragged": dict(sequences=[(900, 400), (3, 1), (700, 700), (0, 0), (650, 650)], kv=40, group=3, D=64, page=128),
     "more-new-than-tokens": dict(sequences=[(20, 30), (40, 10)], kv=1, group=2, D=64, page=16),
     "many": dict(sequences=[((i * 37) % 90 + 1, (i * 37) % 90 % 2 + (i % 3 > 0)) if (i * 37) % 90 > 3 else (3, 0) for i in range(700)], kv=1, group=1, D=64, page=16),
 }
@@ -730,11 +736,12 @@ def test_accepted_drafts_are_a_sequence_without_the_others():
 
 
 @pytest.mark.gpu
-def test_a_captured_step_goes_by_what_lies_in_the_arrays():
+@pytest.mark.parametrize("kv,group", [(2, 2), (1, 17)])   # few rows a sequence, many
+def test_a_captured_step_goes_by_what_lies_in_the_arrays(kv, group):
     """Append, attend and keep in one graph, replayed with other lengths, rows and drafts, with eager work in between: every replay gives what eager calls give."""
-    eager, graph = (Stream(64, 2, 2, (1, 1), None, [0, 0, 0], 90) for _ in range(2))
+    eager, graph = (Stream(64, kv, group, (1, 1), None, [0, 0, 0], 90) for _ in range(2))
     rows = 12
-    x, words = torch.zeros(rows, 8, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(rows, dtype=torch.int64, device=DEV)
+    x, words = torch.zeros(rows, kv * (group + 2), 64, dtype=torch.bfloat16, device=DEV), torch.zeros(rows, dtype=torch.int64, device=DEV)
     kept, counts = torch.zeros(3, 4, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
     ca.compact_attn_rotary_upload(eager.rotary)
     ca.compact_attn_rotary_upload(graph.rotary)
