@@ -192,12 +192,12 @@ struct Share {
     tile = done = 0;
     if (a.way == kShares) {
       const SequenceLine<kThreads> line(a, lds, all_places);
-      size = max((int64_t)a.least_steps, (line.all + a.workgroups - 1) / a.workgroups);
+      size = max((int64_t)a.least_steps, divided64(line.all + a.workgroups - 1, a.workgroups));
       left = min(size, line.all - workgroup * size);
       if (left < 1 || !line.find(a, lds, workgroup * size, sequence, q, takes, rest, all_places)) return false;
       tiles = row_tiles(a, q, kRows);
-      const int64_t per_head = a.kv_heads == 1 ? takes : takes / a.kv_heads;
-      key_head = a.kv_heads == 1 ? 0 : (int32_t)(rest / per_head);
+      const int64_t per_head = a.kv_heads == 1 ? takes : divided64(takes, a.kv_heads);
+      key_head = a.kv_heads == 1 ? 0 : (int32_t)divided64(rest, per_head);
       rest -= key_head * per_head;
       for (int32_t c; (c = kItemCost + max(1, tile_walk<kRows, kStep>(a, q, tile).count)) <= rest; ++tile) rest -= c;
       return take_share(a, (int32_t)rest);
@@ -254,7 +254,9 @@ struct Share {
   // What the second kernel has to know: of an item that begins here, in how many pieces it lies.
   __device__ __forceinline__ void leave(const AttendArgs& a, bool any) const {
     if (a.way == kItems || (a.way == kParts && part > 0)) return;
-    if (threadIdx.x == 0) a.splits[place] = any && begun > 1 ? CacheSplit{sequence, key_head, tile, begun} : CacheSplit{0, 0, 0, 0};
+    if (threadIdx.x != 0) return;
+    const int32_t first_row = tile * kRows;
+    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun} : CacheSplit{0, 0, 0, 0, 0};
   }
 };
 
@@ -442,9 +444,9 @@ __device__ __forceinline__ float frame_of_token(const AttendArgs& a, const Seque
 
 // Writes a row's four channels from the joined sums.
 template <int D>
-__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, const Sequence& q, int32_t key_head, int32_t row, int channel, const floatx4& o, float ref, float total) {
+__device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, int32_t first, int32_t key_head, int32_t row, int channel, const floatx4& o, float ref, float total) {
   const int32_t t = divided(row, a.group), head = key_head * a.group + (row - t * a.group);
-  const int64_t at = (int64_t)(q.first + t) * a.heads + head;
+  const int64_t at = (int64_t)(first + t) * a.heads + head;
   const bool real = total != 0.f;
   bf16x4 v;
 #pragma unroll
@@ -475,14 +477,12 @@ __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
   __shared__ float2 stats[kParts > 1 ? kRowsAtOnce : 1][kParts];
   const CacheSplit split = a.splits[blockIdx.x];
   if (split.pieces == 0) return;
-  const Sequence q = sequence_at(a, split.sequence);
   const CacheRule rule(a);
-  const int32_t first_row = split.tile * kRows, rows = min(kRows, q.count * a.group - first_row);
   const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns % kParts, within = threadIdx.x / kColumns / kParts;
-  for (int r0 = blockIdx.y * kRowsAtOnce; r0 < rows; r0 += gridDim.y * kRowsAtOnce) {
+  for (int r0 = blockIdx.y * kRowsAtOnce; r0 < split.rows; r0 += gridDim.y * kRowsAtOnce) {
     const int r = r0 + within;
     Joined j;
-    if (r < rows) {
+    if (r < split.rows) {
 #pragma unroll 4
       for (int k = part; k < split.pieces; k += kParts) {
         const int64_t piece = a.way == kShares ? ((int64_t)blockIdx.x + k) * 2 + (k > 0) : (int64_t)blockIdx.x * a.most_parts + k;
@@ -498,7 +498,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
       if (part == 0)
         for (int k = 1; k < kParts && k < split.pieces; ++k) j.add(rule, stats[within][k].x, stats[within][k].y, sums[within][k][column]);
     }
-    if (r < rows && part == 0) store_row<D>(a, rule, q, split.key_head, first_row + r, column * 4, j.o, j.ref, j.total);
+    if (r < split.rows && part == 0) store_row<D>(a, rule, split.first, split.key_head, split.first_row + r, column * 4, j.o, j.ref, j.total);
     if constexpr (kParts > 1) __syncthreads();
   }
 }

@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
       const int r = item / (D / 4), c = item % (D / 4) * 4;
       const Joined j = join_waves<D>(rule, lds, r, c);
       if (whole) {
-        store_row<D>(a, rule, q, key_head, first_row + r, c, j.o, j.ref, j.total);
+        store_row<D>(a, rule, q.first, key_head, first_row + r, c, j.o, j.ref, j.total);
       } else {
         *reinterpret_cast<floatx4*>(piece + r * piece_row(D) + c) = j.o;
         if (c == 0) *reinterpret_cast<float2*>(piece + r * piece_row(D) + D) = float2{j.ref, j.total};

@@ -43,8 +43,9 @@ enum CacheWay { kItems, kShares, kParts };
 
 // An item (a tile of rows and a key head) that is cut.
 struct CacheSplit {
-  int32_t sequence, key_head, tile;
-  int32_t pieces;  // 0: there is none at this place
+  int32_t first;            // row of the packed tensors of its sequence's first new token
+  int32_t key_head, first_row, rows;
+  int32_t pieces;           // 0: there is none at this place
 };
 
 struct AttendArgs : CacheArgs {

@@ -26,6 +26,9 @@ __device__ __forceinline__ Sequence sequence_at(const CacheArgs& a, int32_t s) {
 // x / by, in 32 bits; plain tokens and ungrouped heads divide by one.
 __device__ __forceinline__ int32_t divided(int32_t x, int32_t by) { return by == 1 ? x : (int32_t)((uint32_t)x / (uint32_t)by); }
 
+// The same in 64 bits, of which most calls need 32.
+__device__ __forceinline__ int64_t divided64(int64_t x, int64_t by) { return (uint64_t)(x | by) >> 32 ? x / by : (int64_t)((uint32_t)x / (uint32_t)by); }
+
 // Page of a token that the table has an entry for, -1 where it is not there.
 __device__ __forceinline__ int32_t page_at(const CacheArgs& a, int32_t s, int32_t token) {
   const int32_t page = a.table[(int64_t)s * a.table_width + divided(token, a.page_tokens)];
