@@ -134,8 +134,8 @@ int check_append(const ca_append* p, const ca_cache* c) {
 }
 
 int check_attend(const ca_cache* c, const ca_reach* r, int32_t heads) {
-  if (c->dtype != CA_BF16 || (c->head_dim != 64 && c->head_dim != 128)) {
-    set_error("attention over a cache supports bf16 with head_dim 64 and 128; got dtype=%d D=%d", c->dtype, c->head_dim);
+  if (c->head_dim != 64 && c->head_dim != 128) {
+    set_error("attention over a cache supports head_dim 64 and 128; got D=%d", c->head_dim);
     return CA_ERR_UNSUPPORTED;
   }
   if (heads < 1 || heads > 65535 || heads % c->kv_heads != 0) return fail(CA_ERR_INVALID_ARG, "heads must be a multiple of kv_heads, at most 65535");
@@ -182,13 +182,13 @@ int fill_attend(ca::AttendArgs& a, Workspace& w, const ca_cache* c, int32_t head
   a.group = heads / c->kv_heads;
   a.D = c->head_dim;
   const int64_t most_tokens = (int64_t)c->table_width * c->page_tokens, rows = (int64_t)((c->tokens + (int64_t)c->sequences - 1) / c->sequences) * a.group;
-  a.many = rows > ca::kFewRows;
+  a.many = rows > ca::kFewRows && c->dtype == CA_BF16;
   const int64_t tile = a.many ? ca::kManyRows : ca::kFewRows, piece_bytes = tile * ca::piece_row(a.D) * 4;
   a.tiles = (int64_t)c->tokens * a.group / tile + std::min(c->tokens, c->sequences);
   if ((int64_t)c->tokens * a.group > kMostTokens) return fail(CA_ERR_UNSUPPORTED, "more rows than a launch takes");
   const int64_t items = a.tiles * c->kv_heads;
   a.way = ca::kItems;  // (items of a few steps are not worth a second launch)
-  const bool itemized = c->sequences <= kItemSequences && items <= kMostItems, side_by_side = itemized && rows >= kSideBySide && ((c->sequences == 1 && !window) || items >= 2 * ca::many_places(a.D));
+  const bool itemized = c->sequences <= kItemSequences && items <= kMostItems, side_by_side = itemized && a.many && rows >= kSideBySide && ((c->sequences == 1 && !window) || items >= 2 * ca::many_places(a.D));
   if (side_by_side) {
     cut_items(a, (most_tokens + ca::kManyStep - 1) / ca::kManyStep);
     if (a.way == ca::kParts) {
@@ -282,7 +282,7 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
     set_error("the call needs a 16-byte aligned workspace of %lld bytes; got %lld", (long long)need, (long long)(workspace ? workspace_bytes : 0));
     return CA_ERR_INVALID_ARG;
   }
-  st = check_apart(c, {{out, rows * c->head_dim * 2}, {lse, rows * 4}, {workspace, need}},
+  st = check_apart(c, {{out, rows * c->head_dim * elem_size(c->dtype)}, {lse, rows * 4}, {workspace, need}},
                    {{q, q_bytes}, {c->k, pages}, {c->v, pages}, {r->slopes, (int64_t)heads * 4}, {r->tree, (int64_t)c->tokens * 8}});
   if (st != CA_OK || c->tokens == 0) return st;
   a.splits = static_cast<ca::CacheSplit*>(workspace);
@@ -296,7 +296,8 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   a.causal = r->causal;
   a.window = r->window;
   a.tree = r->tree;
-  const hipError_t e = a.many ? ca::launch_attend_many(a, (hipStream_t)stream) : ca::launch_attend_few(a, (hipStream_t)stream);
+  const auto launch = c->dtype == CA_F32 ? ca::launch_attend_f32 : a.many ? ca::launch_attend_many : ca::launch_attend_few;
+  const hipError_t e = launch(a, (hipStream_t)stream);
   return e == hipSuccess ? CA_OK : hip_fail(e, "cache attention launch");
 }
 

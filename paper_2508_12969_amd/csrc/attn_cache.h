@@ -339,6 +339,17 @@ __device__ __forceinline__ void soften(const CacheRule& rule, Softmax& soft, flo
     }
 }
 
+// What rows first_token to last_token of a sequence see in any case: of the prompt, and from lo to hi.
+struct Sure {
+  int32_t prompt, lo, hi;
+  __device__ __forceinline__ Sure(const AttendArgs& a, const Sequence& q, int32_t first_token, int32_t last_token) {
+    prompt = prompt_end(a, q);
+    hi = q.base < 0 ? 0 : a.tree ? q.base : view_at(a, q, q.base + first_token).hi;
+    lo = view_at(a, q, a.tree ? max(q.length - 1, 0) : max(q.base + last_token, 0)).lo;
+  }
+  __device__ __forceinline__ bool sees(int32_t token, int32_t end) const { return end <= hi && (token >= lo || end <= prompt); }
+};
+
 // Copies a slice (16 rows of a page) into LDS, asynchronously; logical chunks lie where swizzle() puts them.
 template <class S>
 struct SliceCopy {
@@ -420,6 +431,13 @@ __device__ __forceinline__ void clear_rows(char* y, int first_row, int rows, int
     if (lane < S::kChunksPerRow) *reinterpret_cast<intx4*>(y + r * S::kRowBytes + lane * 16) = intx4{0, 0, 0, 0};
 }
 
+// Does a row see a token that is there?
+__device__ __forceinline__ bool sees_token(const AttendArgs& a, const Sequence& q, const CacheRow& own, int32_t token) {
+  const int32_t draft = token - q.base;
+  const bool drafted = a.tree && draft >= 0 && draft < kMostDrafts && (own.drafts >> draft) & 1u;
+  return (int)(token < own.prompt) | ((int)(token >= own.view.lo) & (int)(token < own.view.hi)) | (int)drafted;
+}
+
 // Hides what a row does not see in a block of 32 tokens from `token` on; slices: which of its two are there.
 __device__ __forceinline__ void hide_tokens(const AttendArgs& a, const Sequence& q, const CacheRow& own, floatx16& s, int32_t token, uint32_t slices, int g) {
   const int32_t at = token + 4 * g, lo = own.view.lo - at, hi = own.view.hi - at, prompt = own.prompt - at;
@@ -442,16 +460,17 @@ __device__ __forceinline__ float frame_of_token(const AttendArgs& a, const Seque
   return (float)frame_at(a, q, draft ? draft_place(q, draft_bits(a, q, q.first + (token - q.base))) : token);
 }
 
-// Writes a row's four channels from the joined sums.
-template <int D>
+// Writes a row's four channels from the joined sums.  T: of the results.
+template <int D, class T>
 __device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& rule, int32_t first, int32_t key_head, int32_t row, int channel, const floatx4& o, float ref, float total) {
+  typedef T Four __attribute__((ext_vector_type(4)));
   const int32_t t = divided(row, a.group), head = key_head * a.group + (row - t * a.group);
   const int64_t at = (int64_t)(first + t) * a.heads + head;
   const bool real = total != 0.f;
-  bf16x4 v;
+  Four v;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (__bf16)(real ? o[e] / total : 0.f);
-  *reinterpret_cast<bf16x4*>(static_cast<char*>(a.out) + (at * D + channel) * 2) = v;
+  for (int e = 0; e < 4; ++e) v[e] = (T)(real ? o[e] / total : 0.f);
+  *reinterpret_cast<Four*>(static_cast<T*>(a.out) + at * D + channel) = v;
   if (channel == 0) a.lse[at] = real ? (__builtin_fmaf(ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInf;
 }
 
@@ -468,9 +487,27 @@ struct Joined {
   }
 };
 
+// Joins what the waves of a workgroup have summed up for a tile of `rows` rows, each row by row in its own part of LDS (lds[wave].sums), and writes the results, or a piece of them.
+template <int D, class T, int kWaves, class Wave, class Shared>
+__device__ __forceinline__ void finish_rows(const AttendArgs& a, const CacheRule& rule, const Shared& share, const Wave* lds, int32_t first_row, int rows) {
+  float* const piece = share.whole ? nullptr : share.piece(a, D);
+  for (int item = threadIdx.x; item < rows * (D / 4); item += kWaves * 64) {
+    const int r = item / (D / 4), c = item % (D / 4) * 4;
+    Joined j;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) j.add(rule, lds[w].sums[r][D], lds[w].sums[r][D + 1], *reinterpret_cast<const floatx4*>(&lds[w].sums[r][c]));
+    if (share.whole) {
+      store_row<D, T>(a, rule, share.q.first, share.key_head, first_row + r, c, j.o, j.ref, j.total);
+    } else {
+      *reinterpret_cast<floatx4*>(piece + r * piece_row(D) + c) = j.o;
+      if (c == 0) *reinterpret_cast<float2*>(piece + r * piece_row(D) + D) = float2{j.ref, j.total};
+    }
+  }
+}
+
 // Joins the pieces of the item that begins at place blockIdx.x, in their order.  Threads take four channels of a row each, and kParts of them together a part of the
 // pieces.  Bound: latency, and the pieces once.
-template <int D, int kRows, int kThreads, int kParts>
+template <int D, class T, int kRows, int kThreads, int kParts>
 __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
   constexpr int kColumns = D / 4, kRowsAtOnce = kThreads / kColumns / kParts;
   __shared__ floatx4 sums[kParts > 1 ? kRowsAtOnce : 1][kParts][kColumns];
@@ -498,7 +535,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
       if (part == 0)
         for (int k = 1; k < kParts && k < split.pieces; ++k) j.add(rule, stats[within][k].x, stats[within][k].y, sums[within][k][column]);
     }
-    if (r < split.rows && part == 0) store_row<D>(a, rule, split.first, split.key_head, split.first_row + r, column * 4, j.o, j.ref, j.total);
+    if (r < split.rows && part == 0) store_row<D, T>(a, rule, split.first, split.key_head, split.first_row + r, column * 4, j.o, j.ref, j.total);
     if constexpr (kParts > 1) __syncthreads();
   }
 }

@@ -18,15 +18,6 @@ struct FewWave {
   float frames[kFewStep];
 };
 
-// Where an item's sums go: LDS holds those of the waves.
-template <int D>
-__device__ __forceinline__ Joined join_waves(const CacheRule& rule, const FewWave<CacheShape<D>>* lds, int row, int channel) {
-  Joined j;
-#pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) j.add(rule, lds[w].sums[row][D], lds[w].sums[row][D + 1], *reinterpret_cast<const floatx4*>(&lds[w].sums[row][channel]));
-  return j;
-}
-
 // Of an item the waves of a workgroup take a quarter of the steps each; they join their sums at the end.
 template <int D>
 __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2))) void few_rows_kernel(AttendArgs a) {
@@ -52,9 +43,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
     const int32_t first_token = divided(first_row, a.group), last_token = divided(first_row + rows - 1, a.group);
     CacheRow own(a, rule, q, key_head, first_row + i);
     const int32_t own_row = own.row >= 0 ? own.row : q.first + first_token, own_head = own.row >= 0 ? own.head : key_head * a.group;
-    // what all rows of the tile see, in scalar registers
-    const int32_t sure_prompt = prompt_end(a, q), sure_hi = q.base < 0 ? 0 : a.tree ? q.base : view_at(a, q, q.base + first_token).hi;
-    const int32_t sure_lo = view_at(a, q, a.tree ? max(q.length - 1, 0) : max(q.base + last_token, 0)).lo;
+    const Sure sure(a, q, first_token, last_token);
 
     floatx16 sum[S::kDBlocks];
 #pragma unroll
@@ -102,8 +91,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
         __builtin_amdgcn_wave_barrier();
         bias_scores(own, p, mine.frames, 0, g);
       }
-      const bool sure = token + kFewStep <= sure_hi && (token >= sure_lo || token + kFewStep <= sure_prompt) && there == 3;
-      if (!sure) hide_tokens(a, q, own, p, token, there, g);
+      if (there != 3 || !sure.sees(token, token + kFewStep)) hide_tokens(a, q, own, p, token, there, g);
       soften<1, S::kDBlocks>(rule, soft, reinterpret_cast<floatx16(&)[1]>(p), sum);
       bf16x8 weights[2];
       rounded(p, weights);
@@ -121,18 +109,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
         *reinterpret_cast<floatx4*>(&mine.sums[i][db * 32 + 8 * j + 4 * g]) = floatx4{sum[db][4 * j], sum[db][4 * j + 1], sum[db][4 * j + 2], sum[db][4 * j + 3]};
     if (g == 0) mine.sums[i][D] = soft.ref, mine.sums[i][D + 1] = total;
     __syncthreads();
-    const bool whole = share.whole;
-    float* const piece = whole ? nullptr : share.piece(a, D);
-    for (int item = threadIdx.x; item < rows * (D / 4); item += kFewThreads) {
-      const int r = item / (D / 4), c = item % (D / 4) * 4;
-      const Joined j = join_waves<D>(rule, lds, r, c);
-      if (whole) {
-        store_row<D>(a, rule, q.first, key_head, first_row + r, c, j.o, j.ref, j.total);
-      } else {
-        *reinterpret_cast<floatx4*>(piece + r * piece_row(D) + c) = j.o;
-        if (c == 0) *reinterpret_cast<float2*>(piece + r * piece_row(D) + D) = float2{j.ref, j.total};
-      }
-    }
+    finish_rows<D, __bf16, kFewWaves>(a, rule, share, lds, first_row, rows);
     if (!share.next(a)) break;
     __syncthreads();  // (the sums lie where the next steps go)
   }
@@ -141,7 +118,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
 
 template <int D>
 __global__ __launch_bounds__(kFewThreads) void few_rows_join_kernel(AttendArgs a) {
-  join_pieces<D, kFewRows, kFewThreads, kFewThreads / (D / 4)>(a);
+  join_pieces<D, __bf16, kFewRows, kFewThreads, kFewThreads / (D / 4)>(a);
 }
 
 template <int D>

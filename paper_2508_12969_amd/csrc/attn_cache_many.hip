@@ -83,7 +83,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
     asm volatile("" : "+v"(own.slope), "+v"(own.drafts));  // (waited for here, not in the loop)
     const int32_t first_token = divided(first_row, a.group), last_token = divided(first_row + max(rows, 1) - 1, a.group);
     const View least = view_at(a, q, max(a.tree ? q.base : q.base + first_token, 0)), most = view_at(a, q, max(a.tree ? q.length - 1 : q.base + last_token, 0));
-    const int32_t sure_prompt = prompt_end(a, q), sure_hi = q.base < 0 ? 0 : a.tree ? q.base : least.hi, sure_lo = most.lo;
+    const Sure sure(a, q, first_token, last_token);
     const int32_t any_lo = a.tree ? min(least.lo, max(q.base, 0)) : least.lo, any_hi = a.tree ? q.length : most.hi;
 
     floatx16 sum[S::kDBlocks];
@@ -109,7 +109,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
         }
         issue(step + 1);
       }
-      if (rows > 0 && (token < sure_prompt || (token < any_hi && token + kManyStep > any_lo))) {
+      if (rows > 0 && (token < sure.prompt || (token < any_hi && token + kManyStep > any_lo))) {
         const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
         floatx16 p[kBlocks];
 #pragma unroll
@@ -123,8 +123,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
 #pragma unroll
           for (int b = 0; b < kBlocks; ++b) bias_scores(own, p[b], lds.frames[wave], b, g);
         }
-        const bool sure = token + kManyStep <= sure_hi && (token >= sure_lo || token + kManyStep <= sure_prompt) && full;
-        if (!sure)
+        if (!full || !sure.sees(token, token + kManyStep))
 #pragma unroll
           for (int b = 0; b < kBlocks; ++b) hide_tokens(a, q, own, p[b], token + b * 32, (here >> (2 * b)) & 3u, g);
         soften<kBlocks, S::kDBlocks>(rule, soft, p, sum);
@@ -161,7 +160,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
 
 template <int D>
 __global__ __launch_bounds__(kManyThreads) void many_rows_join_kernel(AttendArgs a) {
-  join_pieces<D, kManyRows, kManyThreads, 1>(a);
+  join_pieces<D, __bf16, kManyRows, kManyThreads, 1>(a);
 }
 
 template <int D>

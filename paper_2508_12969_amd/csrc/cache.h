@@ -83,5 +83,6 @@ hipError_t launch_append(const AppendArgs& a, bool bf16, bool normed, hipStream_
 hipError_t launch_keep(const KeepArgs& a, hipStream_t stream);
 hipError_t launch_attend_few(const AttendArgs& a, hipStream_t stream);
 hipError_t launch_attend_many(const AttendArgs& a, hipStream_t stream);
+hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t stream);
 
 }  // namespace ca

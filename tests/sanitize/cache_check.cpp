@@ -121,6 +121,10 @@ hipError_t launch_keep(const KeepArgs& a, hipStream_t) {
 }
 hipError_t launch_attend_few(const AttendArgs& a, hipStream_t) { return attend(a, false); }
 hipError_t launch_attend_many(const AttendArgs& a, hipStream_t) { return attend(a, true); }
+hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t) {
+  CHECK(g_cache->dtype == CA_F32 && a.way != kParts);
+  return attend(a, false);
+}
 int fill_rotation(RowRule& a, ca_rotary* r, hipStream_t) {
   a.angles = reinterpret_cast<const float*>(r);
   return CA_OK;

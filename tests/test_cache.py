@@ -1,9 +1,10 @@
 """A paged cache of keys and values: appending with norm and rotation, attention over it, keeping accepted drafts; against oracle/cache.py and oracle/rotary.py in 64 bits.
 
 Tolerances.  u = 2^-24 and h = half a step of the type (bf16 2^-8, fp32 2^-24), relative to the value rounded.
-Attention: products of bf16 values are exact in fp32, so a score is off by at most (D + 8) u times the sum of its products' sizes (their sum, the scale), with a cap by 2^-21 of it more, with
-a bias by 4 u of it; call the largest of a row delta.  Weights and their sum are off by 2 delta and, for n keys, (n + 64) u (sums, rescaled up to once a step, and the exponential); weights are rounded as operands (2^-8), results once more.
-So |error| <= sum p |v| (2^-8 + 2 delta + (n + 64) u) (1 + 2^-7) + 2^-8 |result|, and the log-sum-exp is off by delta + (n + 64) u + 8 u (1 + |lse|).
+Attention: products of bf16 values are exact in fp32, so a score is off by at most (D + 8) u times the sum of its products' sizes (their sum, the scale, the exponent's argument), in fp32 by (2 D + 12) u, with
+a cap by 2^-21 of it more, with a bias by 4 u of it; call the largest of a row delta.  Weights and their sum are off by 2 delta and, for n keys, (n + 64) u (sums, rescaled up to once a step, and the exponential);
+bf16 weights are rounded as operands (w = 2^-8; fp32: 0), results once more.  So |error| <= sum p |v| (w + 2 delta + (n + 64) u) (1 + 2^-7) + h |result|, and the log-sum-exp is off by
+delta + (n + 64) u + 8 u (1 + |lse|).
 Appending: a norm's sum of D squares and its root are off by (D + 8) u, a rotated value by 4 u of both of its terms; rounded once: |error| <= h |y| + (D + 16) u (|a| + |b|) with the terms a, b."""
 import ctypes
 import math
@@ -103,8 +104,7 @@ def test_attend_refusals():
         assert st == -1 and text in message, (bad, st, message)
     lib = ca.load_library()
     assert lib.compact_attn_cache_attend(P[6], None, 4, _raw_cache(), None, P[9], P[10], P[11], 1 << 40, None) == -1
-    for how in (dict(dtype=0), dict(head_dim=96)):
-        assert _attend_call(_raw_cache(**how))[0] == -2
+    assert _attend_call(_raw_cache(head_dim=96))[0] == -2 and _attend_call(_raw_cache(head_dim=32, dtype=0))[0] == -2
     assert _attend_call(_raw_cache(tokens=2 ** 31 - 1, kv_heads=1), heads=64)[0] == -2
     assert _attend_call(_raw_cache(tokens=0), q=None, out=None, lse=None)[0] == 0
     size = ctypes.c_int64()
@@ -196,11 +196,11 @@ def check_attend(p, q, got, scale=0.0, cap=0.0, slopes=None, causal=True, window
             slope = None if slopes is None else float(slopes[h])
             want, want_lse, weights, size = OC.attend(qh[row:row + m, h], k[:, h // group], v[:, h // group], seen, scale, cap, slope, row_frame, token_frame)
             some = seen.any(1)
-            delta = np.max(np.where(seen, size, 0), axis=1, initial=0) * (p.D + 8) * U + cap * 2.0 ** -21
+            delta = np.max(np.where(seen, size, 0), axis=1, initial=0) * (p.D + 8 if p.dtype == "bf16" else 2 * p.D + 12) * U + cap * 2.0 ** -21
             if slope is not None:
                 delta = delta + 4 * U * slope * np.max(np.abs(row_frame[:, None] - token_frame[None, :]) * seen, axis=1, initial=0)
             lost = (n + 64) * U
-            bound = (weights @ np.abs(np.where(seen.any(0)[:, None], v[:, h // group], 0))) * (2.0 ** -8 + 2 * delta + lost)[:, None] * (1 + 2.0 ** -7) + 2.0 ** -8 * np.abs(want)
+            bound = (weights @ np.abs(np.where(seen.any(0)[:, None], v[:, h // group], 0))) * ((2.0 ** -8 if p.dtype == "bf16" else 0) + 2 * delta + lost)[:, None] * (1 + 2.0 ** -7) + HALF[p.dtype] * np.abs(want)
             o, l = out[row:row + m, h], lse[row:row + m, h]
             assert np.all(o[~some] == 0) and np.all(l[~some] == -math.inf), (s, h)
             if some.any():
@@ -270,9 +270,9 @@ ATTEND = {
 }
 
 
-def attend_case(name, seed=3):
+def attend_case(name, seed=3, dtype="bf16"):
     c = dict(dict(causal=True, window=0, cap=0.0, scale=0.0, slopes=None, tree=False, frame=(1, 1), origins=None), **ATTEND[name])
-    p = Paged(c["sequences"], c["kv"], c["D"], c["page"], origins=c["origins"], frame=c["frame"], seed=seed)
+    p = Paged(c["sequences"], c["kv"], c["D"], c["page"], dtype=dtype, origins=c["origins"], frame=c["frame"], seed=seed)
     heads = c["kv"] * c["group"]
     q = p.randn(p.rows, heads, c["D"]).mul(2).to(DEV)
     slopes = np.linspace(0.02, 0.3, heads).astype(np.float32) if c["slopes"] else None
@@ -286,10 +286,11 @@ def run_attend(p, q, slopes, words, how, **more):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("name", list(ATTEND))
-def test_attend(name):
-    print("attend", name, flush=True)
-    p, q, slopes, words, how = attend_case(name)
+def test_attend(name, dtype):
+    print("attend", name, dtype, flush=True)
+    p, q, slopes, words, how = attend_case(name, dtype=dtype)
     got = run_attend(p, q, slopes, words, how)
     again = run_attend(p, q, slopes, words, how)
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
@@ -297,10 +298,11 @@ def test_attend(name):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D,frame,tree", [(64, (1, 1), False), (128, (3, 5), False), (128, (1, 1), True)])
-def test_pages_that_are_not_there(D, frame, tree):
+def test_pages_that_are_not_there(D, frame, tree, dtype):
     """Entries below 0 and past the pages: their tokens are seen by none, and nothing is read there; a sequence without any page has empty rows."""
-    p = Paged([(200, 30), (300, 1), (50, 2), (90, 40)], 2, D, 16, frame=frame, seed=8)
+    p = Paged([(200, 30), (300, 1), (50, 2), (90, 40)], 2, D, 16, dtype=dtype, frame=frame, seed=8)
     p.table[0, 1], p.table[0, 2], p.table[0, 7] = -1, p.num_pages, 2 ** 31 - 1
     p.table[1, 0:9], p.table[1, 18] = -2 ** 31, -5
     p.table[2, :] = -1
@@ -322,10 +324,11 @@ def test_sequences_may_share_pages():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
-def test_infinities_and_nan_stay_in_their_sequence(bad):
+def test_infinities_and_nan_stay_in_their_sequence(bad, dtype):
     """A key or value that is not finite reaches the rows of its sequence that see it, and no other sequence's."""
-    p = Paged([(100, 1), (120, 1), (64, 1)], 2, 128, 32, seed=10)
+    p = Paged([(100, 1), (120, 1), (64, 1)], 2, 128, 32, dtype=dtype, seed=10)
     for t in p.pages:
         t[int(p.table[1, 2]), 1, 3, 5] = bad
     p.upload()
@@ -338,7 +341,7 @@ def test_infinities_and_nan_stay_in_their_sequence(bad):
     p.pages = [torch.where(torch.isfinite(t), t, torch.full_like(t, math.nan)) for t in p.pages]
     keep = [s for s in range(3) if s != 1]
     rows = torch.tensor(keep, device=DEV)
-    some = Paged([p.sequences[s] for s in keep], 2, 128, 32, seed=10)
+    some = Paged([p.sequences[s] for s in keep], 2, 128, 32, dtype=dtype, seed=10)
     some.table, some.pages, some.num_pages = p.table[keep], p.pages, p.num_pages
     some.upload()
     check_attend(some, q[rows], (out[rows], lse[rows]))
