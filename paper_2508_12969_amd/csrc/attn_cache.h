@@ -252,24 +252,29 @@ struct Share {
     return take_share(a, 0);
   }
   // What the second kernel has to know: of an item that begins here, in how many pieces it lies.
-  __device__ __forceinline__ void leave(const AttendArgs& a, bool any) const {
+  __device__ __forceinline__ void leave(const AttendArgs& a, bool any, bool fine) const {
     if (a.way == kItems || (a.way == kParts && part > 0)) return;
     if (threadIdx.x != 0) return;
     const int32_t first_row = tile * kRows;
-    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun} : CacheSplit{0, 0, 0, 0, 0};
+    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun, fine} : CacheSplit{0, 0, 0, 0, 0, 0};
   }
 };
 
-// The unit of scores, see ScoreRule; a lane's query head has its own slope.
+// Scores are held in a unit of their own, x, with s = unit x + offset.  Without a cap x is the product q.k itself.  With one it is tanh(s / cap) (fine), or (tanh - 1) / 2 (as ScoreRule has it), which
+// saves a few instructions a score but is off by 2^-24 however small the score is.  The log-sum-exp of a few tokens shows that (some 10^-6 of it); of many it averages out beside the rounding of the
+// sum.  Three frames over 75K tokens, all fine / none: 5.35 / 4.83 ms.  A lane's query head has its own slope.
 struct CacheRule {
-  float bend, c2, offset;
-  bool capped;
-  __device__ __forceinline__ explicit CacheRule(const AttendArgs& a) {
-    capped = a.cap > 0.f;
-    bend = capped ? 2.f * a.scale * kLog2e / a.cap : 0.f;
-    c2 = (capped ? 2.f * a.cap : a.scale) * kLog2e;
-    offset = capped ? a.cap * kLog2e : 0.f;
+  float unit, offset, c2;  // log2(e) (s - offset) = c2 x
+  float inner, bend;       // of a cap: s / cap = inner q.k; in powers of two, twice that
+  bool capped, fine;
+  __device__ __forceinline__ CacheRule(const AttendArgs& a, bool fine_) : capped(a.cap > 0.f), fine(fine_) {
+    unit = !capped ? a.scale : fine ? a.cap : 2.f * a.cap;
+    offset = capped && !fine ? a.cap : 0.f;
+    c2 = unit * kLog2e;
+    inner = capped ? a.scale / a.cap : 0.f;
+    bend = 2.f * kLog2e * inner;
   }
+  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(ref, unit, __builtin_fmaf(__builtin_amdgcn_logf(total), 0.6931471805599453f, offset)); }
 };
 
 // A lane's row.
@@ -290,11 +295,30 @@ struct CacheRow {
     prompt = prompt_end(a, q);
     if (a.tree) view.hi = min(view.hi, max(q.base, 0));
     if (!there) view.lo = view.hi = prompt = 0;
-    slope = a.slopes ? -a.slopes[head] / (rule.capped ? 2.f * a.cap : a.scale) : 0.f;
+    slope = a.slopes ? -a.slopes[head] / rule.unit : 0.f;
   }
 };
 
-__device__ __forceinline__ void cap_scores(const CacheRule& rule, floatx16& s) {
+// q.k -> x.  Fine, z = inner q.k: where all of a wave's are at most half, z + z u (c0 + u (c1 + u (c2 + u c3))), u = z^2, which is off by less than 2^-23 of it (coefficients: least largest relative
+// error over |z| <= 1/2, found by weighted least squares on Chebyshev nodes); else 1 - 2 / (2^(2 log2(e) z) + 1), off by 2^-24 of one.
+template <int kScores, class Scores>
+__device__ __forceinline__ void cap_scores(const CacheRule& rule, Scores& s) {
+  float most = 0.f;
+#pragma unroll
+  for (int r = 0; r < kScores; ++r) most = fmaxf(most, __builtin_fabsf(s[r]));
+  if (__builtin_amdgcn_ballot_w64(most * rule.inner > 0.5f) == 0) {
+#pragma unroll
+    for (int r = 0; r < kScores; ++r) {
+      const float z = s[r] * rule.inner, u = z * z;
+      const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.0172569938f, -0.0530529507f), 0.133259878f), -0.333331496f);
+      s[r] = __builtin_fmaf(z * u, p, z);
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < kScores; ++r) s[r] = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[r] * rule.bend)), 1.f);
+  }
+}
+__device__ __forceinline__ void cap_scores_fast(const CacheRule& rule, floatx16& s) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
 }
@@ -471,7 +495,7 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, const CacheRule& 
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = (T)(real ? o[e] / total : 0.f);
   *reinterpret_cast<Four*>(static_cast<T*>(a.out) + at * D + channel) = v;
-  if (channel == 0) a.lse[at] = real ? (__builtin_fmaf(ref, rule.c2, rule.offset) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInf;
+  if (channel == 0) a.lse[at] = real ? rule.log_sum_exp(ref, total) : kMinusInf;
 }
 
 // Sums of a row of which parts were made with references of their own.
@@ -514,7 +538,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
   __shared__ float2 stats[kParts > 1 ? kRowsAtOnce : 1][kParts];
   const CacheSplit split = a.splits[blockIdx.x];
   if (split.pieces == 0) return;
-  const CacheRule rule(a);
+  const CacheRule rule(a, split.fine != 0);
   const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns % kParts, within = threadIdx.x / kColumns / kParts;
   for (int r0 = blockIdx.y * kRowsAtOnce; r0 < split.rows; r0 += gridDim.y * kRowsAtOnce) {
     const int r = r0 + within;

@@ -27,10 +27,10 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   Share<kFewRows, kFewStep, kFewThreads, kFewItemCost> share;
   if (!share.begin(a, found, blockIdx.x)) {
-    share.leave(a, false);
+    share.leave(a, false, true);
     return;
   }
-  const CacheRule rule(a);
+  const CacheRule rule(a, true);
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   FewWave<S>& mine = lds[wave];
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
       if (there != 3) clear_rows<S>(mine.steps[step & 1][1], there & 1 ? kSlice : 0, there & 2 ? kSlice : kFewStep, lane);
       if (token + kFewStep > q.length) clear_rows<S>(mine.steps[step & 1][1], q.length - token, kFewStep, lane);
       floatx16 p = block_product<S>(frag, x, 0, query, splat(0.f));
-      if (rule.capped) cap_scores(rule, p);
+      if (rule.capped) cap_scores<16>(rule, p);
       if (a.slopes) {
         if (lane < kFewStep) mine.frames[lane] = frame_of_token(a, q, token + lane);
         __builtin_amdgcn_wave_barrier();
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
     if (!share.next(a)) break;
     __syncthreads();  // (the sums lie where the next steps go)
   }
-  share.leave(a, true);
+  share.leave(a, true, true);
 }
 
 template <int D>

@@ -75,10 +75,10 @@ __global__ __launch_bounds__(kF32Threads) __attribute__((amdgpu_waves_per_eu(D =
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   Share<kFewRows, kF32Step, kF32Threads, kF32ItemCost> share;
   if (!share.begin(a, found, blockIdx.x)) {
-    share.leave(a, false);
+    share.leave(a, false, true);
     return;
   }
-  const CacheRule rule(a);
+  const CacheRule rule(a, true);
   const F32Copy<S> copy(lane);
   F32Wave<S>& mine = lds[wave];
   const uint32_t lds_steps = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine.steps[0][0];
@@ -154,10 +154,7 @@ __global__ __launch_bounds__(kF32Threads) __attribute__((amdgpu_waves_per_eu(D =
 #pragma unroll
       for (int c = 0; c < kF32Columns; ++c) {
         if (c >= columns) break;
-        if (rule.capped) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) p[c][r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(p[c][r] * rule.bend));
-        }
+        if (rule.capped) cap_scores<4>(rule, p[c]);
         if (a.slopes) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[c][r] = __builtin_fmaf(__builtin_fabsf((float)own[c].view.frame - mine.frames[4 * g + r]), own[c].slope, p[c][r]);
@@ -213,7 +210,7 @@ __global__ __launch_bounds__(kF32Threads) __attribute__((amdgpu_waves_per_eu(D =
     if (!share.next(a)) break;
     __syncthreads();  // (the sums lie where the next steps go)
   }
-  share.leave(a, true);
+  share.leave(a, true, true);
 }
 
 template <int D>
