@@ -265,6 +265,9 @@ ATTEND = {
     "side-by-side-64": dict(sequences=[(2600, 700)], kv=1, group=2, D=64, page=48, frame=(7, 10), origins=[77], cap=20.0, slopes=True),
     "side-by-side-window": dict(sequences=[(5000, 600)], kv=2, group=1, D=64, page=64, window=300),
     "side-by-side-ragged": dict(sequences=[(900, 400), (3, 1), (700, 700), (0, 0), (650, 650)], kv=40, group=3, D=64, page=128),
+    "side-by-side-cap": dict(sequences=[(5000, 600)], kv=2, group=1, D=128, page=64, cap=20.0),
+    "rows-cut-cap": dict(sequences=[(9000, 35), (300, 33), (4100, 40)], kv=2, group=2, D=64, page=64, cap=20.0),
+    "tiles-cap": dict(sequences=[((i * 53) % 40 + 20, 20) for i in range(530)] + [(4500, 20)], kv=1, group=3, D=64, page=64, cap=20.0),
     "more-new-than-tokens": dict(sequences=[(20, 30), (40, 10)], kv=1, group=2, D=64, page=16),
     "many": dict(sequences=[((i * 37) % 90 + 1, (i * 37) % 90 % 2 + (i % 3 > 0)) if (i * 37) % 90 > 3 else (3, 0) for i in range(700)], kv=1, group=1, D=64, page=16),
 }
@@ -295,6 +298,28 @@ def test_attend(name, dtype):
     again = run_attend(p, q, slopes, words, how)
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
     print("worst", check_attend(p, q, got, slopes=slopes, words=words, **how))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv,group", [(2, 2), (1, 40)])   # few rows a sequence, many
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_small_capped_scores_are_precise(tokens, kv, group, dtype):
+    """Inputs are multiples of 1/8 whose products' sums are exact.  Then a score s is off by the roundings of scale / cap (2 u), of z (2 u), of the polynomial (it and its last terms, 8 u) and of the way
+    back (4 u): 16 u |s|.  Of one token the log-sum-exp is the score; of n the weights' sum (n + 8) u and the logarithm 4 u (1 + |lse|) join it."""
+    p = Paged([(tokens, 1)] * 50, kv, 64, 16, dtype=dtype, seed=8)
+    p.pages[0] = (p.pages[0].float() * 4).round().div(4).to(DTYPES[dtype])
+    p.upload()
+    q = p.randn(p.rows, kv * group, 64).float().round().div(8).to(DTYPES[dtype]).to(DEV)
+    lse = ca.compact_attn_cache_attend(q, p.cache, scale=0.125, cap=30.0)[1].double().cpu().numpy()
+    for s in range(50):
+        k, _ = p.host(s, 0)
+        for h in range(kv * group):
+            x = 30.0 * np.tanh(k[:, h // group] @ q[s, h].double().cpu().numpy() * 0.125 / 30.0)
+            assert np.abs(x).max() < 15
+            want = np.log(np.exp(x).sum())
+            bound = 16 * U * np.abs(x).max() + (0 if tokens == 1 else (tokens + 8) * U + 4 * U * (1 + abs(want)))
+            assert abs(lse[s, h] - want) <= bound, (s, h, lse[s, h], want)
 
 
 @pytest.mark.gpu
