@@ -252,29 +252,33 @@ struct Share {
     return take_share(a, 0);
   }
   // What the second kernel has to know: of an item that begins here, in how many pieces it lies.
-  __device__ __forceinline__ void leave(const AttendArgs& a, bool any, bool fine) const {
+  __device__ __forceinline__ void leave(const AttendArgs& a, bool any) const {
     if (a.way == kItems || (a.way == kParts && part > 0)) return;
     if (threadIdx.x != 0) return;
     const int32_t first_row = tile * kRows;
-    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun, fine} : CacheSplit{0, 0, 0, 0, 0, 0};
+    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun} : CacheSplit{0, 0, 0, 0, 0};
   }
 };
 
-// Scores are held in a unit of their own, x, with s = unit x + offset.  Without a cap x is the product q.k itself.  With one it is tanh(s / cap) (fine), or (tanh - 1) / 2 (as ScoreRule has it), which
-// saves a few instructions a score but is off by 2^-24 however small the score is.  The log-sum-exp of a few tokens shows that (some 10^-6 of it); of many it averages out beside the rounding of the
-// sum.  Three frames over 75K tokens, all fine / none: 5.35 / 4.83 ms.  A lane's query head has its own slope.
+// Scores are held in the unit of q.k, x, with s = scale x, under a cap too: x = tanh(inner q.k) / inner, inner = scale / cap.  Where the products of a wave's block are small, |z| <= 0.35, it is
+// q.k (1 + t (c0 + t (c1 + t c2))) with t = (q.k)^2 and powers of inner in the coefficients (for z: least largest error of tanh(z) relative to it, 2^-24.5, by weighted least squares on Chebyshev nodes);
+// else (1 - 2 / (2^(2 log2(e) z) + 1)) / inner, off by 2^-24 of the cap, as is the first where powers of inner could leave the numbers' range.
+// Three frames over 75K tokens: 4.95 ms, all by the second form 5.35, without a cap 4.05; (tanh - 1) / 2 as the unit, off by 2^-24 of the cap for all scores, 4.87.
+constexpr float kSmall = 0.35f;
 struct CacheRule {
-  float unit, offset, c2;  // log2(e) (s - offset) = c2 x
-  float inner, bend;       // of a cap: s / cap = inner q.k; in powers of two, twice that
-  bool capped, fine;
-  __device__ __forceinline__ CacheRule(const AttendArgs& a, bool fine_) : capped(a.cap > 0.f), fine(fine_) {
-    unit = !capped ? a.scale : fine ? a.cap : 2.f * a.cap;
-    offset = capped && !fine ? a.cap : 0.f;
-    c2 = unit * kLog2e;
-    inner = capped ? a.scale / a.cap : 0.f;
+  float scale, c2;  // log2(e) s = c2 x
+  float bend, back, most, at0, at1, at2;
+  bool capped;
+  __device__ __forceinline__ explicit CacheRule(const AttendArgs& a) : scale(a.scale), c2(a.scale * kLog2e), capped(a.cap > 0.f) {
+    const float inner = capped ? a.scale / a.cap : 1.f, square = inner * inner;
     bend = 2.f * kLog2e * inner;
+    back = 1.f / inner;
+    most = inner >= 0x1p-18f && inner <= 0x1p18f ? kSmall * back : -1.f;
+    at0 = -0.3333267f * square;
+    at1 = 0.1330001f * square * square;
+    at2 = -0.0491593f * square * square * square;
   }
-  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(ref, unit, __builtin_fmaf(__builtin_amdgcn_logf(total), 0.6931471805599453f, offset)); }
+  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(ref, scale, __builtin_amdgcn_logf(total) * 0.6931471805599453f); }
 };
 
 // A lane's row.
@@ -295,32 +299,26 @@ struct CacheRow {
     prompt = prompt_end(a, q);
     if (a.tree) view.hi = min(view.hi, max(q.base, 0));
     if (!there) view.lo = view.hi = prompt = 0;
-    slope = a.slopes ? -a.slopes[head] / rule.unit : 0.f;
+    slope = a.slopes ? -a.slopes[head] / a.scale : 0.f;
   }
 };
 
-// q.k -> x.  Fine, z = inner q.k: where all of a wave's are at most half, z + z u (c0 + u (c1 + u (c2 + u c3))), u = z^2, which is off by less than 2^-23 of it (coefficients: least largest relative
-// error over |z| <= 1/2, found by weighted least squares on Chebyshev nodes); else 1 - 2 / (2^(2 log2(e) z) + 1), off by 2^-24 of one.
+// q.k -> x
 template <int kScores, class Scores>
 __device__ __forceinline__ void cap_scores(const CacheRule& rule, Scores& s) {
   float most = 0.f;
 #pragma unroll
   for (int r = 0; r < kScores; ++r) most = fmaxf(most, __builtin_fabsf(s[r]));
-  if (__builtin_amdgcn_ballot_w64(most * rule.inner > 0.5f) == 0) {
+  if (__builtin_amdgcn_ballot_w64(!(most <= rule.most)) == 0) {
 #pragma unroll
     for (int r = 0; r < kScores; ++r) {
-      const float z = s[r] * rule.inner, u = z * z;
-      const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.0172569938f, -0.0530529507f), 0.133259878f), -0.333331496f);
-      s[r] = __builtin_fmaf(z * u, p, z);
+      const float t = s[r] * s[r];
+      s[r] = __builtin_fmaf(s[r], t * __builtin_fmaf(t, __builtin_fmaf(t, rule.at2, rule.at1), rule.at0), s[r]);
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < kScores; ++r) s[r] = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[r] * rule.bend)), 1.f);
+    for (int r = 0; r < kScores; ++r) s[r] = __builtin_fmaf(__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[r] * rule.bend)), -2.f * rule.back, rule.back);
   }
-}
-__device__ __forceinline__ void cap_scores_fast(const CacheRule& rule, floatx16& s) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
 }
 
 // frames: of the step's tokens
@@ -538,7 +536,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
   __shared__ float2 stats[kParts > 1 ? kRowsAtOnce : 1][kParts];
   const CacheSplit split = a.splits[blockIdx.x];
   if (split.pieces == 0) return;
-  const CacheRule rule(a, split.fine != 0);
+  const CacheRule rule(a);
   const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns % kParts, within = threadIdx.x / kColumns / kParts;
   for (int r0 = blockIdx.y * kRowsAtOnce; r0 < split.rows; r0 += gridDim.y * kRowsAtOnce) {
     const int r = r0 + within;

@@ -27,10 +27,10 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, g = lane >> 5;
   Share<kFewRows, kFewStep, kFewThreads, kFewItemCost> share;
   if (!share.begin(a, found, blockIdx.x)) {
-    share.leave(a, false, true);
+    share.leave(a, false);
     return;
   }
-  const CacheRule rule(a, true);
+  const CacheRule rule(a);
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   FewWave<S>& mine = lds[wave];
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
     if (!share.next(a)) break;
     __syncthreads();  // (the sums lie where the next steps go)
   }
-  share.leave(a, true, true);
+  share.leave(a, true);
 }
 
 template <int D>

@@ -75,10 +75,10 @@ __global__ __launch_bounds__(kF32Threads) __attribute__((amdgpu_waves_per_eu(D =
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   Share<kFewRows, kF32Step, kF32Threads, kF32ItemCost> share;
   if (!share.begin(a, found, blockIdx.x)) {
-    share.leave(a, false, true);
+    share.leave(a, false);
     return;
   }
-  const CacheRule rule(a, true);
+  const CacheRule rule(a);
   const F32Copy<S> copy(lane);
   F32Wave<S>& mine = lds[wave];
   const uint32_t lds_steps = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine.steps[0][0];
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kF32Threads) __attribute__((amdgpu_waves_per_eu(D =
     if (!share.next(a)) break;
     __syncthreads();  // (the sums lie where the next steps go)
   }
-  share.leave(a, true, true);
+  share.leave(a, true);
 }
 
 template <int D>

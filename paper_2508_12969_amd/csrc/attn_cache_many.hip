@@ -9,10 +9,6 @@ namespace {
 constexpr int kManyWaves = kManyRows / 32, kManyThreads = kManyWaves * 64, kManySlices = kManyStep / kSlice;
 static_assert(kManyWaves == kManySlices, "a wave copies a slice");
 constexpr int kManyItemCost = 4;     // steps that a workgroup does in the time that it takes to begin an item; 16 trees with 2 / 3 / 4: 88 / 82 / 78 us
-constexpr int kFineSteps = 64;       // of an item, up to which capped scores are held fine
-// What a kernel can do with scores: no cap; one, held fine where an item is short; one, never held fine, for pages of more tokens
-// than that, where rows are many (three frames over 75K tokens, with / without the choice 4.95 / 4.87 ms, without a cap 4.03).
-enum Caps { kNone, kEither, kFast };
 constexpr int kPlacedSteps = 128;    // whose slices are looked up together
 
 // Waves per SIMD that the registers leave room for: a third at head dim 64 (three frames over 75K tokens, 10 heads, two / three 2.74 / 2.50 ms, four prompts of 9K, 32 heads, 1104 / 982 us; with
@@ -29,7 +25,7 @@ struct ManyLds {
 
 // A workgroup takes a tile of 128 rows, 32 a wave, over steps of 64 tokens that the waves copy together, a slice each, while the step before is computed.  (Tiles of 256 rows, which read their keys
 // half as often, with copies three steps ahead: 100 rows a key head 90 / 91 us, 225 rows 160 / 160, 75 rows 81 / 71, a frame of 1560 rows 401 / 391.)
-template <int D, bool kLine, Caps kCaps>
+template <int D, bool kLine, bool kCapped>
 __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads), amdgpu_waves_per_eu(many_waves(D, kLine), many_waves(D, kLine)))) void many_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
   typedef ManyLds<S> Lds;
@@ -41,19 +37,17 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
   const int64_t total = gridDim.x, workgroup = a.way == kShares ? blockIdx.x % 8 * (total / 8) + blockIdx.x / 8 : xcd_launch_order(blockIdx.x, total, min(a.tiles, kXcdChunk));
   Share<kManyRows, kManyStep, kManyThreads, kManyItemCost> share;
   if (!share.begin(a, found, workgroup)) {
-    share.leave(a, false, false);
+    share.leave(a, false);
     return;
   }
+  const CacheRule rule(a);
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   const uint32_t lds_x = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.x[0] + wave * S::kSliceBytes;
   const uint32_t lds_y = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.y[0] + wave * S::kSliceBytes;
-  bool fine = false;
   while (true) {
     const Sequence& q = share.q;
     const Walk<kManyStep> walk = share.walk;
-    fine = kCaps != kFast && walk.count <= kFineSteps;
-    const CacheRule rule(a, fine);
     const int32_t from = min(walk.count, share.done), to = min(walk.count, share.done + share.steps);
     // Places of the slices from `first` on.
     auto look_up = [&](int32_t first) {
@@ -122,9 +116,9 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
         floatx16 p[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) p[b] = block_product<S>(frag, x, b, query, splat(0.f));
-        if constexpr (kCaps != kNone) {
+        if constexpr (kCapped) {
 #pragma unroll
-          for (int b = 0; b < kBlocks; ++b) kCaps != kFast && rule.fine ? cap_scores<16>(rule, p[b]) : cap_scores_fast(rule, p[b]);
+          for (int b = 0; b < kBlocks; ++b) cap_scores<16>(rule, p[b]);
         }
         if (a.slopes) {
           lds.frames[wave][lane] = frame_of_token(a, q, token + lane);
@@ -164,7 +158,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
     if (!kLine || !share.next(a)) break;
     __syncthreads();  // nobody reads the buffers any more
   }
-  share.leave(a, true, fine);
+  share.leave(a, true);
 }
 
 template <int D>
@@ -177,14 +171,9 @@ hipError_t launch_many_rows(const AttendArgs& a, hipStream_t stream) {
   constexpr int kRowsAtOnce = kManyThreads / (D / 4);  // of a workgroup that joins
   const int64_t items = a.tiles * a.kv_heads, workgroups = a.way == kShares ? a.workgroups : items * (a.way == kParts ? a.most_parts : 1);
   if (workgroups < 1 || workgroups > 0xffffff || (a.way == kShares && workgroups % 8 != 0)) return hipErrorInvalidValue;  // (2^32 threads)
-  using std::integral_constant;
-  const auto launch = [&](auto line, auto caps) { many_rows_kernel<D, line, caps><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a); };
-  const bool capped = a.cap > 0.f, is_long = (int64_t)a.table_width * a.page_tokens > kFineSteps * kManyStep;
-  const integral_constant<Caps, kNone> none;
-  const integral_constant<Caps, kEither> either;
-  if (a.way == kShares) capped ? launch(std::true_type(), either) : launch(std::true_type(), none);
-  else if (!capped) launch(std::false_type(), none);
-  else is_long ? launch(std::false_type(), integral_constant<Caps, kFast>()) : launch(std::false_type(), either);
+  const auto launch = [&](auto line, auto capped) { many_rows_kernel<D, line, capped><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a); };
+  if (a.way == kShares) a.cap > 0.f ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
+  else a.cap > 0.f ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
   if (a.way != kItems) {
     const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group, row_groups = ((rows < kManyRows ? rows : kManyRows) + kRowsAtOnce - 1) / kRowsAtOnce;
     many_rows_join_kernel<D><<<dim3((unsigned)(a.way == kShares ? workgroups : items), (unsigned)row_groups), kManyThreads, 0, stream>>>(a);

@@ -46,7 +46,6 @@ struct CacheSplit {
   int32_t first;            // row of the packed tensors of its sequence's first new token
   int32_t key_head, first_row, rows;
   int32_t pieces;           // 0: there is none at this place
-  int32_t fine;             // how its scores are held, see CacheRule
 };
 
 struct AttendArgs : CacheArgs {
