@@ -260,25 +260,26 @@ struct Share {
   }
 };
 
-// Scores are held in the unit of q.k, x, with s = scale x, under a cap too: x = tanh(inner q.k) / inner, inner = scale / cap.  Where the products of a wave's block are small, |z| <= 0.35, it is
-// q.k (1 + t (c0 + t (c1 + t c2))) with t = (q.k)^2 and powers of inner in the coefficients (for z: least largest error of tanh(z) relative to it, 2^-24.5, by weighted least squares on Chebyshev nodes);
-// else (1 - 2 / (2^(2 log2(e) z) + 1)) / inner, off by 2^-24 of the cap, as is the first where powers of inner could leave the numbers' range.
-// Three frames over 75K tokens: 4.95 ms, all by the second form 5.35, without a cap 4.05; (tanh - 1) / 2 as the unit, off by 2^-24 of the cap for all scores, 4.87.
+// Scores are held in a unit of their own, x, with s = unit x + offset.  Without a cap that is the product q.k itself.  With one, z = scale / cap q.k, it is one of two:
+// fine, tanh(z): where the |z| of a wave's block are at most 0.35, z + z u (c0 + u (c1 + u c2)), u = z^2 (least largest relative error, 2^-24.5, by weighted least squares on Chebyshev nodes), else
+//   1 - 2 / (2^(2 log2(e) z) + 1), off by 2^-24 of one.  Its constants are literals or in scalar registers (coefficients with powers of scale / cap in them, an operation less: 16 capped trees 94 / 85 us).
+// fast, (tanh(z) - 1) / 2 (as ScoreRule has it), off by 2^-24 of one however small z is: the log-sum-exp of a few tokens shows that, of more it averages out.  For many rows a sequence in tables of more
+//   than kFineTokens tokens: two forms and a branch between them take registers that those kernels do not have (fast / fine: 16 trees over 9K tokens 80 / 85 us, three frames over 75K 4.83 / 4.95 ms and
+//   3.29 / 3.80 at head dim 64; kernels of few rows are the same).
 constexpr float kSmall = 0.35f;
+__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 struct CacheRule {
-  float scale, c2;  // log2(e) s = c2 x
-  float bend, back, most, at0, at1, at2;
+  float unit, offset, c2;  // log2(e) (s - offset) = c2 x
+  float inner, bend;       // z = inner q.k, 2 log2(e) z = bend q.k
   bool capped;
-  __device__ __forceinline__ explicit CacheRule(const AttendArgs& a) : scale(a.scale), c2(a.scale * kLog2e), capped(a.cap > 0.f) {
-    const float inner = capped ? a.scale / a.cap : 1.f, square = inner * inner;
-    bend = 2.f * kLog2e * inner;
-    back = 1.f / inner;
-    most = inner >= 0x1p-18f && inner <= 0x1p18f ? kSmall * back : -1.f;
-    at0 = -0.3333267f * square;
-    at1 = 0.1330001f * square * square;
-    at2 = -0.0491593f * square * square * square;
+  __device__ __forceinline__ explicit CacheRule(const AttendArgs& a) : capped(a.cap > 0.f) {
+    unit = !capped ? a.scale : a.fine ? a.cap : 2.f * a.cap;
+    offset = capped && !a.fine ? a.cap : 0.f;
+    c2 = uniform(unit * kLog2e);
+    inner = uniform(capped ? a.scale / a.cap : 1.f);
+    bend = uniform(2.f * kLog2e * inner);
   }
-  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(ref, scale, __builtin_amdgcn_logf(total) * 0.6931471805599453f); }
+  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(ref, unit, __builtin_fmaf(__builtin_amdgcn_logf(total), 0.6931471805599453f, offset)); }
 };
 
 // A lane's row.
@@ -299,7 +300,7 @@ struct CacheRow {
     prompt = prompt_end(a, q);
     if (a.tree) view.hi = min(view.hi, max(q.base, 0));
     if (!there) view.lo = view.hi = prompt = 0;
-    slope = a.slopes ? -a.slopes[head] / a.scale : 0.f;
+    slope = a.slopes ? -a.slopes[head] / rule.unit : 0.f;
   }
 };
 
@@ -309,16 +310,21 @@ __device__ __forceinline__ void cap_scores(const CacheRule& rule, Scores& s) {
   float most = 0.f;
 #pragma unroll
   for (int r = 0; r < kScores; ++r) most = fmaxf(most, __builtin_fabsf(s[r]));
-  if (__builtin_amdgcn_ballot_w64(!(most <= rule.most)) == 0) {
+  if (__builtin_amdgcn_ballot_w64(!(most * rule.inner <= kSmall)) == 0) {
 #pragma unroll
     for (int r = 0; r < kScores; ++r) {
-      const float t = s[r] * s[r];
-      s[r] = __builtin_fmaf(s[r], t * __builtin_fmaf(t, __builtin_fmaf(t, rule.at2, rule.at1), rule.at0), s[r]);
+      const float z = s[r] * rule.inner, u = z * z;
+      s[r] = __builtin_fmaf(z, u * __builtin_fmaf(u, __builtin_fmaf(u, -0.0491593f, 0.1330001f), -0.3333267f), z);
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < kScores; ++r) s[r] = __builtin_fmaf(__builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[r] * rule.bend)), -2.f * rule.back, rule.back);
+    for (int r = 0; r < kScores; ++r) s[r] = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[r] * rule.bend)), 1.f);
   }
+}
+
+__device__ __forceinline__ void cap_scores_fast(const CacheRule& rule, floatx16& s) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[r] * rule.bend));
 }
 
 // frames: of the step's tokens

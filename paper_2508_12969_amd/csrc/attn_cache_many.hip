@@ -25,7 +25,7 @@ struct ManyLds {
 
 // A workgroup takes a tile of 128 rows, 32 a wave, over steps of 64 tokens that the waves copy together, a slice each, while the step before is computed.  (Tiles of 256 rows, which read their keys
 // half as often, with copies three steps ahead: 100 rows a key head 90 / 91 us, 225 rows 160 / 160, 75 rows 81 / 71, a frame of 1560 rows 401 / 391.)
-template <int D, bool kLine, bool kCapped>
+template <int D, bool kLine, bool kFine>
 __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads), amdgpu_waves_per_eu(many_waves(D, kLine), many_waves(D, kLine)))) void many_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
   typedef ManyLds<S> Lds;
@@ -116,10 +116,12 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
         floatx16 p[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) p[b] = block_product<S>(frag, x, b, query, splat(0.f));
-        if constexpr (kCapped) {
+        if (rule.capped)
 #pragma unroll
-          for (int b = 0; b < kBlocks; ++b) cap_scores<16>(rule, p[b]);
-        }
+          for (int b = 0; b < kBlocks; ++b) {
+            if constexpr (kFine) cap_scores<16>(rule, p[b]);
+            else cap_scores_fast(rule, p[b]);
+          }
         if (a.slopes) {
           lds.frames[wave][lane] = frame_of_token(a, q, token + lane);
           __builtin_amdgcn_wave_barrier();
@@ -171,9 +173,10 @@ hipError_t launch_many_rows(const AttendArgs& a, hipStream_t stream) {
   constexpr int kRowsAtOnce = kManyThreads / (D / 4);  // of a workgroup that joins
   const int64_t items = a.tiles * a.kv_heads, workgroups = a.way == kShares ? a.workgroups : items * (a.way == kParts ? a.most_parts : 1);
   if (workgroups < 1 || workgroups > 0xffffff || (a.way == kShares && workgroups % 8 != 0)) return hipErrorInvalidValue;  // (2^32 threads)
-  const auto launch = [&](auto line, auto capped) { many_rows_kernel<D, line, capped><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a); };
-  if (a.way == kShares) a.cap > 0.f ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
-  else a.cap > 0.f ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
+  const auto launch = [&](auto line, auto fine) { many_rows_kernel<D, line, fine><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a); };
+  const bool fine = a.cap > 0.f && a.fine;
+  if (a.way == kShares) fine ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
+  else fine ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
   if (a.way != kItems) {
     const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group, row_groups = ((rows < kManyRows ? rows : kManyRows) + kRowsAtOnce - 1) / kRowsAtOnce;
     many_rows_join_kernel<D><<<dim3((unsigned)(a.way == kShares ? workgroups : items), (unsigned)row_groups), kManyThreads, 0, stream>>>(a);

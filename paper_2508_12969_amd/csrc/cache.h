@@ -55,6 +55,7 @@ struct AttendArgs : CacheArgs {
   float* lse;
   int32_t heads, group, D;     // group: query heads of a key head
   float scale, cap;            // cap 0: none
+  bool fine;                   // how capped scores are held, see CacheRule
   const float* slopes;         // [heads] or null
   int32_t causal, window;
   const uint64_t* tree;        // [tokens] or null
