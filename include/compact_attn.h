@@ -586,7 +586,7 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
 
 /* Keeps some of the new tokens, the accepted path of a tree of drafts: new token kept[s][j] of sequence s becomes new token j, for j below counts[s], in the pages.  The program then goes
  * on with lengths[s] less the others.  kept: int32 [sequences][width], width up to 64; counts: int32 [sequences]; device memory.  Everything is read before it is written, so any order of
- * kept is right; an entry that is no new token's number leaves its target as it was.  f32 and bf16, head_dim as compact_attn_cache_append. */
+ * kept is right; an entry that is no new token's number leaves its target as it was.  Pages that are written must be in one place of the table only.  f32 and bf16, head_dim as compact_attn_cache_append. */
 int compact_attn_cache_keep(const ca_cache* cache, const int32_t* kept, int32_t width, const int32_t* counts, void* stream);
 
 /* Message of the last failure on the calling thread ("" if none); valid until the next call. */
