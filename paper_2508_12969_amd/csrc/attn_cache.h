@@ -279,7 +279,8 @@ struct CacheRule {
     inner = uniform(capped ? a.scale / a.cap : 1.f);
     bend = uniform(2.f * kLog2e * inner);
   }
-  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(ref, unit, __builtin_fmaf(__builtin_amdgcn_logf(total), 0.6931471805599453f, offset)); }
+  // (the reference's own score first: beside the offset alone a logarithm loses places)
+  __device__ __forceinline__ float log_sum_exp(float ref, float total) const { return __builtin_fmaf(__builtin_amdgcn_logf(total), 0.6931471805599453f, __builtin_fmaf(ref, unit, offset)); }
 };
 
 // A lane's row.
