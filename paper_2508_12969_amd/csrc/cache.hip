@@ -12,7 +12,7 @@
 namespace ca {
 namespace {
 
-constexpr int kKeepThreads = 256, kKeepItems = 16;  // rows of a thread: 64 of 64 chunks are four at once
+constexpr int kKeepThreads = 256, kKeepItems = 16, kKeepFewItems = 4;  // rows of a thread: 64 of 64 chunks are four at once
 
 // The sequence that a row of the packed tensors belongs to: the last one that starts at or before it.  A wave's rows, first to last, follow each other: its lanes look at 64 sequences at a time
 // for that of the first row, those of the others are among the next ones.
@@ -154,16 +154,18 @@ __global__ __launch_bounds__(kRowThreads) void append_kernel(AppendArgs a, int h
 
 // A workgroup moves the rows of some heads of one sequence, keys or values: where they go is looked up once, then all are loaded before the first is stored.  Bound: latency (counts, drafts, table
 // and rows, one after the other).
+template <int kItems>
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a) {
   __shared__ int64_t moves[kMostDrafts][2];  // rows of head 0: from, to; -1: this one stays
   const int32_t s = blockIdx.x, chunks = a.row_bytes / 16, rows_at_once = kKeepThreads / chunks, first_head = blockIdx.y * a.heads_per_block;
   const int32_t row = divided(threadIdx.x, chunks), chunk = threadIdx.x - row * chunks;
   char* const pages = static_cast<char*>(blockIdx.z ? a.v : a.k) + chunk * 16;
+  const int32_t from = threadIdx.x < (unsigned)a.width ? a.kept[(int64_t)s * a.width + threadIdx.x] : -1;  // (asked for beside the counts)
   const Sequence seq = sequence_at(a, s);
   const int32_t count = max(0, min(min(a.counts[s], a.width), seq.count)), rows = min(a.heads_per_block, a.kv_heads - first_head) * count;
   if (count == 0) return;
   if (threadIdx.x < count) {
-    const int32_t j = threadIdx.x, from = a.kept[(int64_t)s * a.width + j];
+    const int32_t j = threadIdx.x;
     const bool moving = from >= 0 && from < seq.count && from != j && seq.base + j >= 0 && seq.base + from >= 0;
     const int32_t source = moving ? seq.base + from : 0, target = moving ? seq.base + j : 0;
     const int32_t source_page = page_at(a, s, source), target_page = page_at(a, s, target);
@@ -173,11 +175,11 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a) {
   }
   __syncthreads();
   typedef __attribute__((ext_vector_type(4))) int intx4;
-  intx4 held[kKeepItems];
-  char* to[kKeepItems];
+  intx4 held[kItems];
+  char* to[kItems];
   int32_t head = divided(row, count), j = row - head * count;  // of the thread's row; the next one is rows_at_once further on
 #pragma unroll
-  for (int i = 0; i < kKeepItems; ++i) {
+  for (int i = 0; i < kItems; ++i) {
     to[i] = nullptr;
     if (i * rows_at_once >= rows) continue;
     if (row < rows_at_once && row + i * rows_at_once < rows && moves[j][0] >= 0) {
@@ -187,10 +189,10 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a) {
     for (j += rows_at_once; j >= count; j -= count) ++head;
   }
 #pragma unroll
-  for (int i = 0; i < kKeepItems; ++i) asm volatile("" : "+v"(held[i]));  // (loaded before the barrier)
+  for (int i = 0; i < kItems; ++i) asm volatile("" : "+v"(held[i]));  // (loaded before the barrier)
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kKeepItems; ++i)
+  for (int i = 0; i < kItems; ++i)
     if (to[i]) *reinterpret_cast<intx4*>(to[i]) = held[i];
 }
 
@@ -216,9 +218,11 @@ hipError_t launch_keep(const KeepArgs& args, hipStream_t stream) {
   const int chunks = a.row_bytes / 16, rows_at_once = kKeepThreads / chunks;
   if (a.width > kMostDrafts || rows_at_once * kKeepItems < kMostDrafts || a.sequences > 0xffffff || a.kv_heads > 65535) return hipErrorInvalidValue;
   // four rows a thread, if all of the width is used: 256 sequences x 20 heads, one / eight heads a workgroup 19.6 / 8.4 us, 16 sequences x 8 heads 3.2 / 4.4
-  a.heads_per_block = std::max(1, std::min(a.kv_heads, 4 * rows_at_once / a.width));
+  a.heads_per_block = std::max(1, std::min(a.kv_heads, kKeepFewItems * rows_at_once / a.width));
   const dim3 grid((unsigned)a.sequences, (unsigned)((a.kv_heads + a.heads_per_block - 1) / a.heads_per_block), 2);
-  keep_kernel<<<grid, kKeepThreads, 0, stream>>>(a);
+  // where four are all there are, more waves have registers: 256 sequences x 20 heads with room for sixteen / four 7.7 / 6.5 us
+  if (a.heads_per_block * a.width <= kKeepFewItems * rows_at_once) keep_kernel<kKeepFewItems><<<grid, kKeepThreads, 0, stream>>>(a);
+  else keep_kernel<kKeepItems><<<grid, kKeepThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
