@@ -564,7 +564,7 @@ int compact_attn_cache_append(const ca_append* append, const ca_cache* cache, vo
  * none; bits past the sequence's new tokens are not read).  These bits alone decide among the new tokens.  A draft stands as many tokens behind the last one that is not new as bits are set, whatever its row: its frame, for distances and
  * windows, is the one of that place.  tree is device memory, uint64[tokens], 8-byte aligned, or NULL. */
 typedef struct {
-  float scale;          /* <= 0: head_dim^-1/2 */
+  float scale;          /* 2^-100 to 2^100; <= 0: head_dim^-1/2 */
   float cap;            /* 0 (none) or 2^-16 to 4096 */
   const float* slopes;  /* device, [heads], or NULL */
   int32_t causal, window;

@@ -141,7 +141,8 @@ int check_attend(const ca_cache* c, const ca_reach* r, int32_t heads) {
   }
   if (heads < 1 || heads > 65535 || heads % c->kv_heads != 0) return fail(CA_ERR_INVALID_ARG, "heads must be a multiple of kv_heads, at most 65535");
   if (!r) return CA_OK;
-  if (std::isnan(r->scale) || std::isinf(r->scale)) return fail(CA_ERR_INVALID_ARG, "scale must be finite");
+  if (std::isnan(r->scale) || std::isinf(r->scale) || (r->scale > 0.f && (r->scale < 0x1p-100f || r->scale > 0x1p100f)))  // (what is made of it, and of it and the cap, stays a number)
+    return fail(CA_ERR_INVALID_ARG, "scale must be finite, and between 2^-100 and 2^100 where it is positive");
   if (r->cap != 0.f && !(r->cap >= ca::kLeastCap && r->cap <= ca::kMostCap)) return fail(CA_ERR_INVALID_ARG, "cap must be 0 or between 2^-16 and 4096");
   if (r->causal != 0 && r->causal != 1) return fail(CA_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (r->window < 0) return fail(CA_ERR_INVALID_ARG, "window must not be negative");

@@ -97,7 +97,7 @@ def test_attend_refusals():
     step = lambda token, head: R.ca_strides(0, head, token)
     for bad, text in ((dict(q=None), "null"), (dict(out=None), "null"), (dict(lse=None), "null"), (dict(out=P[9] + 8), "16-byte"), (dict(lse=P[10] + 2), "4-byte"), (dict(heads=3), "multiple"),
                       (dict(heads=0), "multiple"), (dict(cap=-1.0), "cap"), (dict(cap=5000.0), "cap"), (dict(cap=float("nan")), "cap"), (dict(scale=float("nan")), "scale"),
-                      (dict(scale=float("inf")), "scale"), (dict(causal=2), "causal"), (dict(window=-1), "window"), (dict(slopes=P[12] + 2), "4-byte"), (dict(tree=P[12] + 4), "8-byte"),
+                      (dict(scale=float("inf")), "scale"), (dict(scale=1e-38), "scale"), (dict(scale=2.0 ** 101), "scale"), (dict(causal=2), "causal"), (dict(window=-1), "window"), (dict(slopes=P[12] + 2), "4-byte"), (dict(tree=P[12] + 4), "8-byte"),
                       (dict(strides=step(512, 4)), "16 bytes"), (dict(out=P[6]), "overlap"), (dict(out=P[1]), "overlap"), (dict(lse=P[9]), "each other"), (dict(lse=P[4]), "arrays"),
                       (dict(tree=P[9]), "overlap"), (dict(slopes=P[10]), "overlap")):
         st, message = _attend_call(**bad)
@@ -249,6 +249,9 @@ ATTEND = {
     "bias": dict(sequences=[(333, 1), (128, 128)], kv=2, group=2, D=64, page=32, slopes=True),
     "bias-frames-cap": dict(sequences=[(333, 30), (128, 128)], kv=2, group=2, D=128, page=32, frame=(2, 11), origins=[50, 3], slopes=True, cap=20.0),
     "scale": dict(sequences=[(100, 3)], kv=2, group=2, D=64, page=32, scale=0.31),
+    "scale-least": dict(sequences=[(100, 3), (90, 90)], kv=2, group=2, D=64, page=32, scale=2.0 ** -100),
+    "scale-least-cap": dict(sequences=[(100, 3), (90, 90)], kv=1, group=2, D=128, page=32, scale=2.0 ** -100, cap=4096.0),
+    "cap-least": dict(sequences=[(100, 3), (90, 90)], kv=1, group=2, D=64, page=32, scale=2.0 ** 100, cap=2.0 ** -16),
     "tree": dict(sequences=[(100, 64), (64, 64), (1, 1), (500, 37), (33, 2)], kv=2, group=2, D=128, page=16, tree=True),
     "tree-window-bias": dict(sequences=[(100, 40), (47, 33), (200, 9)], kv=1, group=3, D=64, page=48, tree=True, window=20, slopes=True),
     "tree-frames": dict(sequences=[(100, 40), (47, 33), (30, 20)], kv=1, group=3, D=64, page=48, tree=True, frame=(2, 3), origins=[31, 47, 29], window=2, slopes=True),
