@@ -578,6 +578,7 @@ int compact_attn_cache_workspace(const ca_cache* cache, int32_t heads, int64_t* 
  *   q          [tokens, heads, head_dim], strides as in ca_append; heads is a multiple of kv_heads, and query heads h * heads / kv_heads .. of a key head h are neighbours.
  *   out, lse   [tokens, heads, head_dim] of the cache's type and float [tokens, heads], contiguous.  A row that sees nothing has a zero result and minus infinity.
  *   workspace  16-byte aligned, not overlapping the tensors; must not be used by anything else until the call's work on `stream` has run.
+ * Scores are fp32.  Only those with a cap of up to 64, in bf16, of rows that see more than 4096 tokens (counted by position), may be off by cap 2^-22 whatever their size.
  * Tokens below a sequence's length must have finite values unless all rows of their sequence see them; slots that hold no token may hold anything.  bf16: weights are
  * rounded to it before the product with v; sums are fp32 in an order that depends on the sizes and lengths alone.  bf16 and f32 with head_dim 64 and 128, at most 2^30 rows (tokens x heads /
  * kv_heads), otherwise CA_ERR_UNSUPPORTED. */

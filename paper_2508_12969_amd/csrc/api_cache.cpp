@@ -21,7 +21,6 @@ namespace {
 constexpr int64_t kMostTokens = (int64_t)1 << 30, kMostBytes = (int64_t)1 << 46;
 constexpr int32_t kMostSequences = 1 << 20;
 constexpr int64_t kWholeTokens = 1024;  // sequences of at most so many are not cut: 16 of up to 600 / 900 / 2000 tokens, cut / whole, 17.6 / 12.8, 18.5 / 16.9, 19.4 / 27.0 us
-constexpr int64_t kFineTokens = 4096;   // see CacheRule
 constexpr int64_t kLeastFewSteps = 8, kLeastManySteps = 8;  // of a workgroup's share: 256 and 512 tokens
 constexpr int32_t kItemSequences = 512;  // every workgroup looks through all sequences for its own: of more, only as many workgroups as the device holds do
 constexpr int64_t kMostItems = 0xffffff / 64;  // 64 parts of each are a launch
@@ -294,7 +293,6 @@ int compact_attn_cache_attend(const void* q, const ca_strides* q_strides, int32_
   a.lse = lse;
   a.scale = r->scale > 0.f ? r->scale : 1.f / std::sqrt((float)c->head_dim);
   a.cap = r->cap;
-  a.fine = !a.many || (int64_t)c->table_width * c->page_tokens <= kFineTokens;
   a.slopes = r->slopes;
   a.causal = r->causal;
   a.window = r->window;

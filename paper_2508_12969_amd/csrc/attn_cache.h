@@ -177,6 +177,7 @@ struct Share {
   int64_t size, left, place;   // kShares: places of a share, those not taken yet, its number; kParts: place of the item
   int32_t part, parts;         // kParts
   int32_t begun = 0;           // pieces of an item that begins here
+  bool fine = true;            // how the item's capped scores are held, see CacheRule
 
   __device__ __forceinline__ static int64_t places_of(const AttendArgs& a, const Sequence& q) {
     int64_t all = 0;
@@ -256,25 +257,26 @@ struct Share {
     if (a.way == kItems || (a.way == kParts && part > 0)) return;
     if (threadIdx.x != 0) return;
     const int32_t first_row = tile * kRows;
-    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun} : CacheSplit{0, 0, 0, 0, 0};
+    a.splits[place] = any && begun > 1 ? CacheSplit{q.first, key_head, first_row, min(kRows, q.count * a.group - first_row), begun, fine} : CacheSplit{0, 0, 0, 0, 0, 0};
   }
 };
 
 // Scores are held in a unit of their own, x, with s = unit x + offset.  Without a cap that is the product q.k itself.  With one, z = scale / cap q.k, it is one of two:
 // fine, tanh(z): where the |z| of a wave's block are at most 0.35, z + z u (c0 + u (c1 + u c2)), u = z^2 (least largest relative error, 2^-24.5, by weighted least squares on Chebyshev nodes), else
 //   1 - 2 / (2^(2 log2(e) z) + 1), off by 2^-24 of one.  Its constants are literals or in scalar registers (coefficients with powers of scale / cap in them, an operation less: 16 capped trees 94 / 85 us).
-// fast, (tanh(z) - 1) / 2 (as ScoreRule has it), off by 2^-24 of one however small z is: the log-sum-exp of a few tokens shows that, of more it averages out.  For many rows a sequence in tables of more
-//   than kFineTokens tokens: two forms and a branch between them take registers that those kernels do not have (fast / fine: 16 trees over 9K tokens 80 / 85 us, three frames over 75K 4.83 / 4.95 ms and
-//   3.29 / 3.80 at head dim 64; kernels of few rows are the same).
-constexpr float kSmall = 0.35f;
+// fast, (tanh(z) - 1) / 2 (as ScoreRule has it), off by 2^-23 at most however small z is, which puts a score off by cap 2^-22 at most: the log-sum-exp of a few tokens shows that, of more it averages out.
+//   For tiles of many rows that all see more than kFineTokens tokens, with caps up to kMostFastCap (2^-16 then): two forms and a branch between them take registers that those kernels do not have
+//   (fast / fine: 16 trees over 9K tokens 80 / 85 us, three frames over 75K 4.83 / 4.95 ms and 3.29 / 3.80 at head dim 64; kernels of few rows are the same, and have the fine form alone).
+constexpr float kSmall = 0.35f, kMostFastCap = 64.f;
+constexpr int32_t kFineTokens = 4096;
 __device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 struct CacheRule {
   float unit, offset, c2;  // log2(e) (s - offset) = c2 x
   float inner, bend;       // z = inner q.k, 2 log2(e) z = bend q.k
   bool capped;
-  __device__ __forceinline__ explicit CacheRule(const AttendArgs& a) : capped(a.cap > 0.f) {
-    unit = !capped ? a.scale : a.fine ? a.cap : 2.f * a.cap;
-    offset = capped && !a.fine ? a.cap : 0.f;
+  __device__ __forceinline__ CacheRule(const AttendArgs& a, bool fine) : capped(a.cap > 0.f) {
+    unit = !capped ? a.scale : fine ? a.cap : 2.f * a.cap;
+    offset = capped && !fine ? a.cap : 0.f;
     c2 = uniform(unit * kLog2e);
     inner = uniform(capped ? a.scale / a.cap : 1.f);
     bend = uniform(2.f * kLog2e * inner);
@@ -377,6 +379,7 @@ struct Sure {
     lo = view_at(a, q, a.tree ? max(q.length - 1, 0) : max(q.base + last_token, 0)).lo;
   }
   __device__ __forceinline__ bool sees(int32_t token, int32_t end) const { return end <= hi && (token >= lo || end <= prompt); }
+  __device__ __forceinline__ int32_t tokens() const { return prompt + max(0, hi - max(lo, prompt)); }
 };
 
 // Copies a slice (16 rows of a page) into LDS, asynchronously; logical chunks lie where swizzle() puts them.
@@ -543,7 +546,7 @@ __device__ __forceinline__ void join_pieces(const AttendArgs& a) {
   __shared__ float2 stats[kParts > 1 ? kRowsAtOnce : 1][kParts];
   const CacheSplit split = a.splits[blockIdx.x];
   if (split.pieces == 0) return;
-  const CacheRule rule(a);
+  const CacheRule rule(a, split.fine != 0);
   const int column = threadIdx.x % kColumns, part = threadIdx.x / kColumns % kParts, within = threadIdx.x / kColumns / kParts;
   for (int r0 = blockIdx.y * kRowsAtOnce; r0 < split.rows; r0 += gridDim.y * kRowsAtOnce) {
     const int r = r0 + within;

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(D =
     share.leave(a, false);
     return;
   }
-  const CacheRule rule(a);
+  const CacheRule rule(a, true);
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   FewWave<S>& mine = lds[wave];

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kF32Threads) __attribute__((amdgpu_waves_per_eu(D =
     share.leave(a, false);
     return;
   }
-  const CacheRule rule(a);
+  const CacheRule rule(a, true);
   const F32Copy<S> copy(lane);
   F32Wave<S>& mine = lds[wave];
   const uint32_t lds_steps = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine.steps[0][0];

@@ -25,7 +25,9 @@ struct ManyLds {
 
 // A workgroup takes a tile of 128 rows, 32 a wave, over steps of 64 tokens that the waves copy together, a slice each, while the step before is computed.  (Tiles of 256 rows, which read their keys
 // half as often, with copies three steps ahead: 100 rows a key head 90 / 91 us, 225 rows 160 / 160, 75 rows 81 / 71, a frame of 1560 rows 401 / 391.)
-template <int D, bool kLine, bool kFine>
+// kCapped: both forms of capped scores are there, as two loops, and a tile takes one of them, by what its rows see (the table's room, known before the launch, says nothing of that; a kernel for each
+// form and one with both, all tiles in the fast form: three frames over 75K tokens 4.92 / 5.01 ms, 16 trees over 9K 82 / 84 us).
+template <int D, bool kLine, bool kCapped>
 __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads), amdgpu_waves_per_eu(many_waves(D, kLine), many_waves(D, kLine)))) void many_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
   typedef ManyLds<S> Lds;
@@ -40,7 +42,6 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
     share.leave(a, false);
     return;
   }
-  const CacheRule rule(a);
   const SliceCopy<S> copy(lane);
   const Fragments<S> frag(lane);
   const uint32_t lds_x = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds.x[0] + wave * S::kSliceBytes;
@@ -49,6 +50,11 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
     const Sequence& q = share.q;
     const Walk<kManyStep> walk = share.walk;
     const int32_t from = min(walk.count, share.done), to = min(walk.count, share.done + share.steps);
+    if constexpr (kCapped) {
+      const int32_t first = share.tile * kManyRows, last = min(first + kManyRows, q.count * a.group) - 1;
+      share.fine = a.cap > kMostFastCap || Sure(a, q, divided(first, a.group), divided(last, a.group)).tokens() <= kFineTokens;
+    }
+    const CacheRule rule(a, share.fine);
     // Places of the slices from `first` on.
     auto look_up = [&](int32_t first) {
       for (int at = threadIdx.x; at < kPlacedSteps * kManySlices; at += kManyThreads) {
@@ -95,51 +101,55 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads
       asm volatile("" : "+v"(t));  // (a known zero has the sums copied in every step, 64 moves: three frames over 75K tokens 5.37 / 5.06 ms)
     }
     Softmax soft;
-    for (int32_t step = from; step < to; ++step) {
-      const int buffer = step & 1;
-      const int32_t token = walk.token(step);
-      const uint32_t here = there;
-      const bool full = here == 15u && token + kManyStep <= q.length;
-      WAIT_VMCNT(0);
-      if (!full) clear_rows<S>(lds.y[buffer], (here >> wave) & 1u ? max(wave * kSlice, q.length - token) : wave * kSlice, (wave + 1) * kSlice, lane);
-      WAIT_LGKMCNT0();
-      BARRIER();  // the step is there, and nobody reads the other buffer any more
-      if (step + 1 < to) {
-        if ((step + 1 - from) % kPlacedSteps == 0) {
-          look_up(step + 1);
-          __syncthreads();
+    const auto take_steps = [&](auto fine) {
+      for (int32_t step = from; step < to; ++step) {
+        const int buffer = step & 1;
+        const int32_t token = walk.token(step);
+        const uint32_t here = there;
+        const bool full = here == 15u && token + kManyStep <= q.length;
+        WAIT_VMCNT(0);
+        if (!full) clear_rows<S>(lds.y[buffer], (here >> wave) & 1u ? max(wave * kSlice, q.length - token) : wave * kSlice, (wave + 1) * kSlice, lane);
+        WAIT_LGKMCNT0();
+        BARRIER();  // the step is there, and nobody reads the other buffer any more
+        if (step + 1 < to) {
+          if ((step + 1 - from) % kPlacedSteps == 0) {
+            look_up(step + 1);
+            __syncthreads();
+          }
+          issue(step + 1);
         }
-        issue(step + 1);
-      }
-      if (rows > 0 && (token < sure.prompt || (token < any_hi && token + kManyStep > any_lo))) {
-        const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
-        floatx16 p[kBlocks];
+        if (rows > 0 && (token < sure.prompt || (token < any_hi && token + kManyStep > any_lo))) {
+          const LdsTile x = (LdsTile)lds.x[buffer], y = (LdsTile)lds.y[buffer];
+          floatx16 p[kBlocks];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) p[b] = block_product<S>(frag, x, b, query, splat(0.f));
-        if (rule.capped)
+          for (int b = 0; b < kBlocks; ++b) p[b] = block_product<S>(frag, x, b, query, splat(0.f));
+          if constexpr (kCapped)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+              if constexpr (fine) cap_scores<16>(rule, p[b]);
+              else cap_scores_fast(rule, p[b]);
+            }
+          if (a.slopes) {
+            lds.frames[wave][lane] = frame_of_token(a, q, token + lane);
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) bias_scores(own, p[b], lds.frames[wave], b, g);
+          }
+          if (!full || !sure.sees(token, token + kManyStep))
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) hide_tokens(a, q, own, p[b], token + b * 32, (here >> (2 * b)) & 3u, g);
+          soften<kBlocks, S::kDBlocks>(rule, soft, p, sum);
 #pragma unroll
           for (int b = 0; b < kBlocks; ++b) {
-            if constexpr (kFine) cap_scores<16>(rule, p[b]);
-            else cap_scores_fast(rule, p[b]);
+            bf16x8 weights[2];
+            rounded(p[b], weights);
+            block_sums<S>(frag, y, b, weights, sum);
           }
-        if (a.slopes) {
-          lds.frames[wave][lane] = frame_of_token(a, q, token + lane);
-          __builtin_amdgcn_wave_barrier();
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b) bias_scores(own, p[b], lds.frames[wave], b, g);
-        }
-        if (!full || !sure.sees(token, token + kManyStep))
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b) hide_tokens(a, q, own, p[b], token + b * 32, (here >> (2 * b)) & 3u, g);
-        soften<kBlocks, S::kDBlocks>(rule, soft, p, sum);
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-          bf16x8 weights[2];
-          rounded(p[b], weights);
-          block_sums<S>(frag, y, b, weights, sum);
         }
       }
-    }
+    };
+    if (kCapped && share.fine) take_steps(std::true_type());
+    else take_steps(std::false_type());
 
     const float weight = sum_with_partner(soft.sum);
     if (i < rows) {
@@ -173,10 +183,10 @@ hipError_t launch_many_rows(const AttendArgs& a, hipStream_t stream) {
   constexpr int kRowsAtOnce = kManyThreads / (D / 4);  // of a workgroup that joins
   const int64_t items = a.tiles * a.kv_heads, workgroups = a.way == kShares ? a.workgroups : items * (a.way == kParts ? a.most_parts : 1);
   if (workgroups < 1 || workgroups > 0xffffff || (a.way == kShares && workgroups % 8 != 0)) return hipErrorInvalidValue;  // (2^32 threads)
-  const auto launch = [&](auto line, auto fine) { many_rows_kernel<D, line, fine><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a); };
-  const bool fine = a.cap > 0.f && a.fine;
-  if (a.way == kShares) fine ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
-  else fine ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
+  const auto launch = [&](auto line, auto capped) { many_rows_kernel<D, line, capped><<<(unsigned)workgroups, kManyThreads, 0, stream>>>(a); };
+  const bool capped = a.cap > 0.f;
+  if (a.way == kShares) capped ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
+  else capped ? launch(std::false_type(), std::true_type()) : launch(std::false_type(), std::false_type());
   if (a.way != kItems) {
     const int64_t rows = (int64_t)((a.tokens + a.sequences - 1) / a.sequences) * a.group, row_groups = ((rows < kManyRows ? rows : kManyRows) + kRowsAtOnce - 1) / kRowsAtOnce;
     many_rows_join_kernel<D><<<dim3((unsigned)(a.way == kShares ? workgroups : items), (unsigned)row_groups), kManyThreads, 0, stream>>>(a);

@@ -46,6 +46,7 @@ struct CacheSplit {
   int32_t first;            // row of the packed tensors of its sequence's first new token
   int32_t key_head, first_row, rows;
   int32_t pieces;           // 0: there is none at this place
+  int32_t fine;             // how its capped scores are held, see CacheRule
 };
 
 struct AttendArgs : CacheArgs {
@@ -55,7 +56,6 @@ struct AttendArgs : CacheArgs {
   float* lse;
   int32_t heads, group, D;     // group: query heads of a key head
   float scale, cap;            // cap 0: none
-  bool fine;                   // how capped scores are held, see CacheRule
   const float* slopes;         // [heads] or null
   int32_t causal, window;
   const uint64_t* tree;        // [tokens] or null

@@ -1,0 +1,85 @@
+"""What the paged cache promises beside its formulas: how precise capped scores are wherever a row's tokens lie, which attributes of a Cache may change, workspaces that do not fit, and runs long
+enough that the kernels look up where pages lie more than once."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_12969_amd as ca
+from test_cache import DEV, DTYPES, U, Paged
+
+# ---------------------------------------------------------------- capped scores
+
+
+def _exact_products(sequences, kv, D, page, dtype, seed, **more):
+    """A cache whose keys, and queries to go with them, are multiples of 1/8 and 1/4: sums of their products are exact in fp32."""
+    p = Paged(sequences, kv, D, page, dtype=dtype, seed=seed, **more)
+    p.pages[0] = (p.pages[0].float() * 4).round().div(4).to(DTYPES[dtype])
+    p.upload()
+    return p
+
+
+def _wider(p, tokens):
+    """The same cache with a table that has room for so many tokens a sequence."""
+    table = np.full((p.table.shape[0], tokens // p.page), -1, np.int32)
+    table[:, :p.table.shape[1]] = p.table
+    return ca.Cache(p.k, p.v, torch.from_numpy(table).to(DEV), p.lengths, p.starts, origins=p.dev_origins, frame=p.frame)
+
+
+def _capped(p, q, s, h, group, scale, cap):
+    """Scores of all new tokens and all tokens of a sequence in 64 bits."""
+    k, _ = p.host(s, 0)
+    return cap * np.tanh(k[:, h // group] @ q.double().cpu().numpy().T * scale / cap).T
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap", [30.0, 4096.0])
+@pytest.mark.parametrize("kind", ["causal", "window", "prompt"])
+def test_capped_scores_of_few_tokens_are_precise_in_wide_tables(kind, cap, D, dtype):
+    """Rows that see one to five tokens, beside 32 rows and more of their sequence, in tables with room for 100 000 tokens and for few.  Products are exact, so a score s is off by the roundings of
+    scale / cap (2 u), of z (2 u), of the polynomial (8 u) and of the way back (4 u): 16 u |s|.  Of one token the log-sum-exp is the score; of n, (n + 8) u of the weights' sum and 4 u (1 + |lse|) of
+    the logarithm join it.  (Off by cap 2^-22, a score of 8 at cap 4096 would miss that by a factor of 100.)"""
+    print("capped", kind, cap, D, dtype, flush=True)
+    how = dict(causal=dict(sequences=[(60, 60), (70, 70)]), window=dict(sequences=[(600, 60), (5000, 70)]),
+               prompt=dict(sequences=[(5 + 7000, 7005)], frame=(70, 100), origins=[5]))[kind]
+    kv, group = (1, 1) if kind == "prompt" else (2, 2)
+    p = _exact_products(how.pop("sequences"), kv, D, 16, dtype, 8, **how)
+    q = p.randn(p.rows, kv * group, D).float().round().div(8).to(DTYPES[dtype]).to(DEV)
+    for tokens in (7168, 100000):
+        lse = ca.compact_attn_cache_attend(q, _wider(p, tokens), scale=0.125, cap=cap, window=3 if kind == "window" else 0)[1].double().cpu().numpy()
+        row = 0
+        for s, (n, m) in enumerate(p.sequences):
+            rows = range(m) if kind == "window" else range(5)
+            for h in range(kv * group):
+                x = _capped(p, q[row:row + m, h][list(rows)], s, h, group, 0.125, cap)
+                for i in rows:
+                    seen = x[i, n - m + i - 2:n - m + i + 1] if kind == "window" else x[i, :5] if kind == "prompt" else x[i, :i + 1]
+                    assert np.abs(seen).max() < 15
+                    want = np.log(np.exp(seen).sum())
+                    bound = 16 * U * np.abs(seen).max() + (0 if len(seen) == 1 else (len(seen) + 8) * U + 4 * U * (1 + abs(want)))
+                    assert abs(lse[row + i, h] - want) <= bound, (tokens, s, h, i, lse[row + i, h], want, bound)
+            row += m
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [30.0, 4096.0])
+def test_capped_scores_of_many_tokens(cap, dtype):
+    """Rows that see 5000 tokens and more, of which one has all of the weight that counts (its score is 40 above the others' largest), so that the log-sum-exp is that score.  It is off by 16 u |s| as
+    above and by u (1 + |s|) from the others (5100 e^-40 is below u); with a cap of at most 64 by cap 2^-22 more."""
+    p = _exact_products([(5100, 40)], 2, 64, 16, dtype, 9)
+    q = torch.zeros(p.rows, 4, 64, dtype=DTYPES[dtype], device=DEV)
+    q[:, :, 0] = 8
+    for h in range(2):
+        page, slot = int(p.table[0, 700 // 16]), 700 % 16
+        p.pages[0][:, h, :, 0] = torch.where(torch.isnan(p.pages[0][:, h, :, 0]), p.pages[0][:, h, :, 0], torch.tensor(-2.0, dtype=DTYPES[dtype]))
+        p.pages[0][page, h, slot, 0] = 2.0
+    p.upload()
+    top, other = (cap * math.tanh(x * 2.0 / cap) for x in (16.0, -16.0))
+    assert top - other > 40
+    lse = ca.compact_attn_cache_attend(q, p.cache, scale=2.0, cap=cap)[1].double().cpu().numpy()
+    bound = 16 * U * abs(top) + U * (1 + abs(top)) + 4 * U * (1 + abs(top)) + (cap * 2.0 ** -22 if cap <= 64 else 0)
+    assert np.abs(lse - top).max() <= bound, (np.abs(lse - top).max(), bound)
