@@ -1,5 +1,6 @@
 """A paged cache of keys and values: argument marshalling for the entry points of that part of include/compact_attn.h, as binding.py does it for the others."""
 import ctypes
+import operator
 
 from . import binding
 from .binding import CA_BF16, CA_ERR_ALLOC, CA_F32, CompactAttnError, _lend, load_library
@@ -33,11 +34,20 @@ def _check(t, cache, shape, dtype, name):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
 
 
+def _fixed(name):
+    """An attribute that calls know by its address: it stays what the Cache was made with."""
+    def refuse(self, value):
+        raise AttributeError(f"{name} of a Cache cannot be replaced: change it in place, or make another Cache of the same pages")
+    return property(operator.attrgetter("_" + name), refuse)
+
+
 class Cache:
     """Pages of keys and values, and whose tokens lie where: k, v [num_pages, kv_heads, page_tokens, head_dim]; table int32 [sequences, pages of the longest], -1 where there is
     none; lengths int32 [sequences], tokens with those of the next call; starts int32 [sequences + 1], rows of the next call's packed tensors; origins int32
-    [sequences] or None, tokens of the prompts; frame: (height, width) of a frame.  Device tensors, which a program changes in place from call to call, or it makes
-    another Cache of the same pages."""
+    [sequences] or None, tokens of the prompts; frame: (height, width) of a frame.  Device tensors, which a program changes in place from call to call (their
+    memory stays where it is), or it makes another Cache of the same pages; as attributes they can be read, not replaced."""
+
+    k, v, table, lengths, starts, origins, frame = map(_fixed, ("k", "v", "table", "lengths", "starts", "origins", "frame"))
 
     def __init__(self, k, v, table, lengths, starts, origins=None, frame=(1, 1)):
         import torch
@@ -55,8 +65,9 @@ class Cache:
         for name, t, shape in (("table", table, table.shape), ("lengths", lengths, (sequences,)), ("starts", starts, (sequences + 1,)), ("origins", origins, (sequences,))):
             if t is not None:
                 _check(t, self, shape, torch.int32, name)
-        self.k, self.v, self.table, self.lengths, self.starts, self.origins, self.frame = k, v, table, lengths, starts, origins, tuple(frame)
+        self._k, self._v, self._table, self._lengths, self._starts, self._origins, self._frame = k, v, table, lengths, starts, origins, tuple(frame)
         pages, self._kv_heads, page_tokens, self._head_dim = k.shape
+        self._sequences = sequences
         self._dtype = k.dtype
         self._args = (k.data_ptr(), v.data_ptr(), pages, page_tokens, self._kv_heads, self._head_dim, CA_BF16 if k.dtype == torch.bfloat16 else CA_F32, sequences, table.shape[1],
                       table.data_ptr(), lengths.data_ptr(), starts.data_ptr(), None if origins is None else origins.data_ptr())
@@ -74,7 +85,7 @@ def _of(cache, tokens):
         if len(cache._of) >= 64:
             cache._of.clear()
             cache._workspace.clear()
-        args = cache._of[tokens] = ca_cache(*cache._args, tokens, *cache.frame)
+        args = cache._of[tokens] = ca_cache(*cache._args, tokens, *cache._frame)
     return args
 
 
@@ -192,7 +203,7 @@ def compact_attn_cache_keep(cache, kept, counts, stream=None):
     """Keeps some of the last call's new tokens (those of lengths and starts): new token kept[s, j] becomes new token j, for j < counts[s], in the pages.  kept: int32 [sequences, up to 64],
     counts: int32 [sequences]."""
     import torch
-    args, sequences = _of(cache, 2 ** 31 - 1), cache.table.shape[0]
+    args, sequences = _of(cache, 2 ** 31 - 1), cache._sequences
     if kept.dim() != 2:
         raise ValueError("kept has a row for every sequence")
     _check(kept, cache, (sequences, kept.shape[1]), torch.int32, "kept")

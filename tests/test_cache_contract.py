@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2508_12969_amd as ca
-from test_cache import DEV, DTYPES, U, Paged
+from test_cache import DEV, DTYPES, U, Paged, check_attend
 
 # ---------------------------------------------------------------- capped scores
 
@@ -83,3 +83,34 @@ def test_capped_scores_of_many_tokens(cap, dtype):
     lse = ca.compact_attn_cache_attend(q, p.cache, scale=2.0, cap=cap)[1].double().cpu().numpy()
     bound = 16 * U * abs(top) + U * (1 + abs(top)) + 4 * U * (1 + abs(top)) + (cap * 2.0 ** -22 if cap <= 64 else 0)
     assert np.abs(lse - top).max() <= bound, (np.abs(lse - top).max(), bound)
+
+
+# ---------------------------------------------------------------- what a Cache holds
+
+
+@pytest.mark.parametrize("name", ["k", "v", "table", "lengths", "starts", "origins", "frame"])
+def test_attributes_of_a_cache_cannot_be_replaced(name):
+    cache = ca.Cache.__new__(ca.Cache)   # (one that is made needs device tensors)
+    with pytest.raises(AttributeError, match=name):
+        setattr(cache, name, None)
+    with pytest.raises(AttributeError):
+        delattr(cache, name)
+
+
+@pytest.mark.gpu
+def test_a_cache_keeps_the_tensors_that_calls_read():
+    """What a program may try to go on with: new tensors for old ones.  They are refused, the calls' tensors stay alive and are what the attributes give."""
+    p = Paged([(40, 2), (30, 1)], 2, 64, 16, seed=5, origins=[3, 4], frame=(2, 3))
+    q = p.randn(p.rows, 4, 64).to(DEV)
+    want = ca.compact_attn_cache_attend(q, p.cache)
+    own = dict(k=p.k, v=p.v, table=p.dev_table, lengths=p.lengths, starts=p.starts, origins=p.dev_origins, frame=(2, 3))
+    for name, value in own.items():
+        other = (1, 1) if name == "frame" else value + 1
+        with pytest.raises(AttributeError, match=name):
+            setattr(p.cache, name, other)
+        assert getattr(p.cache, name) is value or name == "frame" and p.cache.frame == value
+    got = ca.compact_attn_cache_attend(q, p.cache)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    p.lengths += 1   # in place: the next call goes by it
+    p.lengths -= 1
+    check_attend(p, q, ca.compact_attn_cache_attend(q, p.cache))
