@@ -552,7 +552,7 @@ typedef struct {
  *   k' = R(p) (w * k * (mean(k^2) + eps)^-1/2),  q' likewise,  v as it is.
  * Positions: where->positions (int32[tokens][3], as compact_attn_rotate), or else where->origin + (frame, row, column) of the token; prompts are not rotated then.  A position past the
  * rotary table gives NaN.  Sums are fp32, results rounded once.  A page that is written must be in one place of the table only.  bf16 and f32; head_dim up to 512 (bf16) or 256
- * (f32) and fewer than 2^26 tokens, CA_ERR_UNSUPPORTED beyond.  q_out and the pages must not overlap the inputs or each other. */
+ * (f32) and fewer than 2^26 tokens (2^26 - 3 of rows of more than 512 bytes), CA_ERR_UNSUPPORTED beyond.  q_out and the pages must not overlap the inputs or each other. */
 int compact_attn_cache_append(const ca_append* append, const ca_cache* cache, void* stream);
 
 /* How scores are bent and what is seen, as in ca_scores.

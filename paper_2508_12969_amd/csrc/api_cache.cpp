@@ -222,8 +222,10 @@ int compact_attn_cache_append(const ca_append* p, const ca_cache* c, void* strea
   if (st == CA_OK) st = packed_strides(c, p->k_strides, c->kv_heads, "k", a.k_strides, k_bytes);
   if (st == CA_OK) st = packed_strides(c, p->v_strides, c->kv_heads, "v", a.v_strides, v_bytes);
   if (st != CA_OK) return st;
-  if (c->tokens >= 1 << 26) return fail(CA_ERR_UNSUPPORTED, "more than 2^26 - 1 new tokens");
-  const int64_t row = (int64_t)c->head_dim * elem_size(c->dtype), out_bytes = (int64_t)c->tokens * heads * row, pages = page_bytes(c);
+  const int64_t row = (int64_t)c->head_dim * elem_size(c->dtype);
+  if (c->tokens >= (1 << 26) - (row > 512 ? 3 : 0))  // (a launch has fewer than 2^32 threads; rows of more than 512 bytes are a wave's)
+    return fail(CA_ERR_UNSUPPORTED, "2^26 new tokens and more, or 2^26 - 3 of rows of more than 512 bytes");
+  const int64_t out_bytes = (int64_t)c->tokens * heads * row, pages = page_bytes(c);
   const void* const positions = p->rotary && p->where ? p->where->positions : nullptr;
   st = check_apart(c, {{p->q_out, out_bytes}, {c->k, pages}, {c->v, pages}},
                    {{p->q, q_bytes}, {p->k, k_bytes}, {p->v, v_bytes}, {p->q_weight, row}, {p->k_weight, row}, {positions, (int64_t)c->tokens * 12}});

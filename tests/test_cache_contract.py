@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2508_12969_amd as ca
-from test_cache import DEV, DTYPES, U, Paged, check_attend
+from test_cache import DEV, DTYPES, U, P, Paged, _append_call, _attend_call, _raw_cache, check_attend
 
 # ---------------------------------------------------------------- capped scores
 
@@ -114,3 +114,14 @@ def test_a_cache_keeps_the_tensors_that_calls_read():
     p.lengths += 1   # in place: the next call goes by it
     p.lengths -= 1
     check_attend(p, q, ca.compact_attn_cache_attend(q, p.cache))
+
+
+# ---------------------------------------------------------------- sizes and workspaces that do not fit (nothing is launched)
+
+
+@pytest.mark.parametrize("D,dtype", [(512, 1), (264, 1), (256, 0), (132, 0)])
+def test_appending_more_tokens_than_a_launch_takes_is_refused(D, dtype):
+    """Rows of more than 512 bytes are four a workgroup, and 2^24 workgroups of 256 threads are past what a launch takes: the three sizes below 2^26 are refused like 2^26 is, before a launch."""
+    for tokens in (2 ** 26 - 3, 2 ** 26 - 1, 2 ** 26):
+        status, message = _append_call(_raw_cache(head_dim=D, dtype=dtype, tokens=tokens))
+        assert status == -2 and "2^26" in message, (tokens, status, message)
