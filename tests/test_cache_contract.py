@@ -1,5 +1,6 @@
 """What the paged cache promises beside its formulas: how precise capped scores are wherever a row's tokens lie, which attributes of a Cache may change, workspaces that do not fit, and runs long
 enough that the kernels look up where pages lie more than once."""
+import ctypes
 import math
 
 import numpy as np
@@ -125,3 +126,23 @@ def test_appending_more_tokens_than_a_launch_takes_is_refused(D, dtype):
     for tokens in (2 ** 26 - 3, 2 ** 26 - 1, 2 ** 26):
         status, message = _append_call(_raw_cache(head_dim=D, dtype=dtype, tokens=tokens))
         assert status == -2 and "2^26" in message, (tokens, status, message)
+
+
+NEEDY = {   # calls that need a workspace: few and many rows on a line of shares, one sequence cut into parts, fp32
+    "few": dict(table_width=100), "many": dict(table_width=100, tokens=200), "parts": dict(table_width=800, sequences=1, tokens=1000, page_tokens=64), "f32": dict(table_width=100, dtype=0),
+}
+
+
+@pytest.mark.parametrize("name", list(NEEDY))
+def test_workspaces_that_do_not_fit_are_refused(name):
+    """Too small, absent, not aligned, or over anything that the call reads or writes.  (A table of items is 256 bytes at least, and sums follow it.)"""
+    cache, size = _raw_cache(**NEEDY[name]), ctypes.c_int64()
+    assert ca.load_library().compact_attn_cache_workspace(cache, 4, size) == 0 and size.value > 256
+    need = size.value
+    for workspace, given in ((None, need), (None, 1 << 40), (P[11], 0), (P[11], 1), (P[11], 256), (P[11] + 8, need), (P[11] + 4, 1 << 40)):
+        status, message = _attend_call(cache, workspace=workspace, size=given)
+        assert status == -1 and "workspace of" in message and "bytes" in message, (workspace, given, status, message)
+    tree = P[12]
+    for over in (P[6], P[0], P[1], P[2], P[3], P[4], P[9], P[10], tree, P[13], P[2] - 256):
+        status, message = _attend_call(cache, workspace=over, size=need, tree=tree, slopes=P[13])
+        assert status == -1 and "overlap" in message, (over, status, message)
