@@ -146,3 +146,43 @@ def test_workspaces_that_do_not_fit_are_refused(name):
     for over in (P[6], P[0], P[1], P[2], P[3], P[4], P[9], P[10], tree, P[13], P[2] - 256):
         status, message = _attend_call(cache, workspace=over, size=need, tree=tree, slopes=P[13])
         assert status == -1 and "overlap" in message, (over, status, message)
+
+
+# ---------------------------------------------------------------- long runs
+
+LONG = {
+    # Where pages lie is looked up for 32 steps of a wave (bf16, 32 tokens each), 64 (fp32, 16 each) or 128 of a workgroup (many rows, 64 each).  `alike`: so many sequences share one table row, for
+    # lines of which every workgroup takes several such runs: few rows 400 steps of 639 for each item (100 a wave) at head dim 128, 197 a wave in fp32; many rows 490 of 629
+    "few": dict(tokens=20000, new=1, kv=2, group=2, D=128, alike=80),
+    "few-64": dict(tokens=20000, new=3, kv=2, group=1, D=64, alike=160),
+    "few-f32": dict(tokens=20000, new=1, kv=2, group=2, D=128, alike=80, dtype="f32"),
+    "few-f32-64": dict(tokens=20000, new=20, kv=2, group=1, D=64, alike=80, dtype="f32"),
+    "many": dict(tokens=40000, new=40, kv=2, group=1, D=128, alike=200),
+    "many-64": dict(tokens=40000, new=20, kv=2, group=2, D=64, alike=200),
+    # 505 items of 313 steps, which 512 places take whole; 768 places take 505 items of 625 steps in three parts each
+    "items": dict(tokens=20000, new=640, kv=5, group=20, D=128, alike=1),
+    "parts": dict(tokens=40000, new=640, kv=5, group=20, D=64, alike=1),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(LONG))
+def test_runs_that_look_up_pages_more_than_once(name):
+    """Walks so long that the kernels refill what they know of the table; pages lie in random order.  A few sequences and key heads, two query heads of each, against the oracle."""
+    print("long", name, flush=True)
+    c = dict(dict(dtype="bf16"), **LONG[name])
+    p = Paged([(c["tokens"], c["new"])], c["kv"], c["D"], 16, dtype=c["dtype"], seed=70)
+    alike, new, group = c["alike"], c["new"], c["group"]
+    ints = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(DEV)
+    cache = ca.Cache(p.k, p.v, ints(np.repeat(p.table, alike, axis=0)), ints([c["tokens"]] * alike), ints(np.arange(alike + 1) * new))
+    q = p.randn(alike * new, c["kv"] * group, c["D"]).mul(2).to(DEV)
+    out, lse = ca.compact_attn_cache_attend(q, cache)
+    again = ca.compact_attn_cache_attend(q, cache)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    pages = p.pages
+    for s in sorted({0, alike // 3, alike - 1}):
+        for key_head in sorted({0, c["kv"] - 1}):
+            heads = [key_head * group] if group == 1 else [key_head * group, key_head * group + group - 1]
+            p.pages, p.kv = [t[:, key_head:key_head + 1] for t in pages], 1
+            rows = slice(s * new, (s + 1) * new)
+            check_attend(p, q[rows][:, heads], (out[rows][:, heads], lse[rows][:, heads]))
