@@ -566,7 +566,7 @@ int compact_attn_cache_append(const ca_append* append, const ca_cache* cache, vo
 typedef struct {
   float scale;          /* 2^-100 to 2^100; <= 0: head_dim^-1/2 */
   float cap;            /* 0 (none) or 2^-16 to 4096 */
-  const float* slopes;  /* device, [heads], or NULL */
+  const float* slopes;  /* device, [heads], or NULL; they, and what they are over the scale (over a cap where there is one), are finite */
   int32_t causal, window;
   const uint64_t* tree;
 } ca_reach;
