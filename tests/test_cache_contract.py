@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2508_12969_amd as ca
-from test_cache import DEV, DTYPES, U, P, Paged, _append_call, _attend_call, _raw_cache, check_attend
+from test_cache import DEV, DTYPES, U, P, Paged, _append_call, _attend_call, _raw_cache, chain_words, check_attend, run_attend
 
 # ---------------------------------------------------------------- capped scores
 
@@ -84,6 +84,23 @@ def test_capped_scores_of_many_tokens(cap, dtype):
     lse = ca.compact_attn_cache_attend(q, p.cache, scale=2.0, cap=cap)[1].double().cpu().numpy()
     bound = 16 * U * abs(top) + U * (1 + abs(top)) + 4 * U * (1 + abs(top)) + (cap * 2.0 ** -22 if cap <= 64 else 0)
     assert np.abs(lse - top).max() <= bound, (np.abs(lse - top).max(), bound)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", ["side-by-side", "shares", "tree"])
+def test_capped_tiles_of_both_forms_in_one_launch(kind, D):
+    """Prompts whose first tiles see few tokens and whose last see more than 4096, drafts over long and short caches: tiles of both forms, whole and cut, with a distance bias; every row against the oracle."""
+    print("both forms", kind, D, flush=True)
+    sequences = {"side-by-side": [(6000, 6000)], "shares": [(6000, 6000), (300, 40), (5000, 700), (4100, 33)], "tree": [(6000, 40), (300, 40), (4200, 64), (4100, 33)]}[kind]
+    p = Paged(sequences, 1, D, 16, seed=17, origins=[3] * len(sequences))
+    q = p.randn(p.rows, 2, D).mul(2).to(DEV)
+    slopes, words = np.array([0.02, 0.001], dtype=np.float32), [w for _, m in sequences for w in chain_words(p.rng, m)] if kind == "tree" else None
+    how = dict(cap=20.0)
+    got = run_attend(p, q, slopes, words, how)
+    again = run_attend(p, q, slopes, words, how)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    check_attend(p, q, got, slopes=slopes, words=words, **how)
 
 
 # ---------------------------------------------------------------- what a Cache holds
