@@ -26,7 +26,8 @@ struct ManyLds {
 // A workgroup takes a tile of 128 rows, 32 a wave, over steps of 64 tokens that the waves copy together, a slice each, while the step before is computed.  (Tiles of 256 rows, which read their keys
 // half as often, with copies three steps ahead: 100 rows a key head 90 / 91 us, 225 rows 160 / 160, 75 rows 81 / 71, a frame of 1560 rows 401 / 391.)
 // kCapped: both forms of capped scores are there, as two loops, and a tile takes one of them, by what its rows see (the table's room, known before the launch, says nothing of that; a kernel for each
-// form and one with both, all tiles in the fast form: three frames over 75K tokens 4.92 / 5.01 ms, 16 trees over 9K 82 / 84 us).
+// form and one with both, all tiles in the fast form: three frames over 75K tokens 4.92 / 5.01 ms, 16 trees over 9K 82 / 84 us).  All waves of a workgroup take the same one, whose barriers they share; with the
+// choice in a scalar register the loops' registers spill (41 of them at head dim 128, three frames 5.33 / 7.64 ms).
 template <int D, bool kLine, bool kCapped>
 __global__ __attribute__((amdgpu_flat_work_group_size(kManyThreads, kManyThreads), amdgpu_waves_per_eu(many_waves(D, kLine), many_waves(D, kLine)))) void many_rows_kernel(AttendArgs a) {
   typedef CacheShape<D> S;
